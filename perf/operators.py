@@ -176,7 +176,7 @@ def prepare(case, seed):
         free[:n_blocks - sum(need)] = order[sum(need):].int()
         state.update(rows=torch.tensor(rows, dtype=torch.int32, device=dev), add=torch.tensor(add, dtype=torch.int32, device=dev),
                      table=torch.nn.functional.pad(table, (0, width - table.shape[1]), value=-1).contiguous(), free=free,
-                     count=torch.tensor([n_blocks - sum(need), 0], dtype=torch.int32, device=dev),
+                     count=torch.tensor([n_blocks - sum(need), 0, 0, 0], dtype=torch.int32, device=dev),
                      slots=torch.empty(sum(add), dtype=torch.int32, device=dev), start=torch.empty(n + 1, dtype=torch.int32, device=dev))
         state["drop"] = -state["add"]
         return state
