@@ -32,6 +32,13 @@ class LaqError(RuntimeError):
         self.code = code
 
 
+class _Fp4Cache(ctypes.Structure):
+    _fields_ = ([(name, ctypes.c_void_p) for name in ("k", "k_scale", "v", "v_scale")]
+                + [(name, ctypes.c_int32) for name in ("n_blocks", "Hkv", "block_rows", "d")]
+                + [(name, ctypes.c_int64) for name in ("stride_block", "stride_head", "stride_row", "scale_stride_block",
+                                                       "scale_stride_head", "scale_stride_row")])
+
+
 class _Shape(ctypes.Structure):
     _fields_ = [("n_inst", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("L", ctypes.c_int32), ("W", ctypes.c_int32),
@@ -96,6 +103,19 @@ def load_library() -> ctypes.CDLL:
     lib.laq_workspace_status.restype = i32
     lib.laq_score_kernel.argtypes = [sp]
     lib.laq_score_kernel.restype = i32
+    cp, i64 = ctypes.POINTER(_Fp4Cache), ctypes.c_int64
+    lib.laq_block_map.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.laq_block_map.restype = i32
+    lib.laq_fp4_store.argtypes = [cp, i32, i64, vp, vp, i64, i64, vp, vp]
+    lib.laq_fp4_store.restype = i32
+    lib.laq_fp4_compact.argtypes = [sp, vp, vp, vp, bp, cp, vp, vp]
+    lib.laq_fp4_compact.restype = i32
+    lib.laq_fp4_load.argtypes = [cp, i32, i64, vp, vp, vp, vp]
+    lib.laq_fp4_load.restype = i32
+    lib.laq_fp4_attention_workspace_bytes.argtypes = [cp, i32, i32, i32, i64, i32]
+    lib.laq_fp4_attention_workspace_bytes.restype = sz
+    lib.laq_fp4_attention.argtypes = [cp, i32, i32, ctypes.c_float, i32, i64, vp, vp, i64, i64, vp, i32, vp, i32, vp, vp, vp, sz, vp]
+    lib.laq_fp4_attention.restype = i32
     try:
         from . import _native as native
     except ImportError as exc:          # not built, or built against another torch: ctypes serves every call

@@ -180,6 +180,12 @@ static bool budgets_ok(const laq_shape* s, const ScoreGeom& g, const int32_t* bu
   return true;
 }
 
+int check_source(const laq_shape* shape, const int32_t* budget, ScoreGeom* g, KvLayout* lay) {
+  const int rc = make_geom(shape, g);
+  if (rc != LAQ_OK) return rc;
+  return budgets_ok(shape, *g, budget) ? make_layout(shape, *g, lay) : LAQ_ERR_INVALID;
+}
+
 // ---- per-device set-up ---------------------------------------------------------------------
 // Kernel attributes and residency of the scoring kernels on the current device, and the address of
 // the library's own scratch array there.  `scratch` is the workspace of laq_evict_static: in host

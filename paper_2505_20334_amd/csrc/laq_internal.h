@@ -187,6 +187,9 @@ inline int uniform_rows(int L, const int32_t* budget, int i0, int n) {
   return bk;
 }
 
+// The checks of a call that gathers rows of a cache by an index list: LAQ_OK with the geometry and the layout of k and v, or the error.
+int check_source(const laq_shape* shape, const int32_t* budget, ScoreGeom* g, KvLayout* lay);
+
 // launchers (each returns hipGetLastError() after its last launch); `raw` receives unpooled scores
 hipError_t launch_score_tile(const ScoreGeom& g, const WindowPos& qp, const KvLayout& lay, int dtype, const void* q,
                              const void* k, float* raw, const Workspace& ws, hipStream_t st);
