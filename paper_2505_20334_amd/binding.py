@@ -1,8 +1,8 @@
 """Binding of ``liblaq.so`` -- argument marshalling only.
 
-The three calls that sit in a model's loop (laq_evict, laq_decode_attention, laq_qcache_store) are
-marshalled by the extension module ``_native`` (csrc/laq_native.cpp); ctypes serves the others, and
-these three where an argument is out of the ordinary or the module cannot be loaded.
+The calls that sit in a model's loop (laq_evict, laq_decode_attention, laq_qcache_store, and those of
+``fp4``) are marshalled by the extension module ``_native`` (csrc/laq_native.cpp); ctypes serves the others, and
+these where an argument is out of the ordinary or the module cannot be loaded.
 
 Function names and argument meaning follow ``include/laq.h``.  Tensors are torch
 tensors that already live on the GPU (torch supplies device memory and the
@@ -127,6 +127,8 @@ def load_library() -> ctypes.CDLL:
         native.bind(address("laq_evict"), address("laq_workspace_bytes"), address("laq_decode_attention"),
                     address("laq_decode_workspace_bytes"), address("laq_qcache_store"),
                     torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        native.bind_fp4(address("laq_block_map"), address("laq_fp4_store"), address("laq_fp4_compact"), address("laq_fp4_load"),
+                        address("laq_fp4_attention"), address("laq_fp4_attention_workspace_bytes"))
         _native = native
     _lib = lib
     return lib

@@ -37,6 +37,11 @@ def laq_block_pool(n_blocks: int, device="cuda:0") -> Tuple[torch.Tensor, torch.
     return free, torch.tensor([n_blocks, 0, 0, 0], dtype=torch.int32, device=device)
 
 
+def _here(t: torch.Tensor) -> None:
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError("the tensors live on %s, which is not the current device" % t.device)
+
+
 def _ints(t: torch.Tensor, name: str, like: torch.Tensor, numel: int) -> torch.Tensor:
     """A dense int32 tensor of at least `numel` entries on the device of `like`."""
     if t.device.type != "cuda":
@@ -50,6 +55,7 @@ def _fp4(cache: Fp4Cache) -> _Fp4Cache:
     k, k_scale, v, v_scale = cache
     if k.device.type != "cuda":
         raise ValueError("the cache must live on the GPU")
+    _here(k)
     n_blocks, Hkv, block_rows, half = k.shape
     for t, name, like in ((k, "k", k), (v, "v", k), (k_scale, "k_scale", k_scale), (v_scale, "v_scale", k_scale)):
         want = (n_blocks, Hkv, block_rows, half if like is k else half // 16)
@@ -76,12 +82,19 @@ def laq_block_map(add: torch.Tensor, rows: torch.Tensor, block_table: torch.Tens
     GPU; rows, block_table, free_blocks and state are updated in place.  Returns (start [n + 1], slots [n_slots]), made if n_slots (the
     batch's rows, padding included) is given and they are not; None where they are not wanted.  state[0]: free blocks, state[1]: requests
     refused for want of blocks or table entries (rows as before, slots -1)."""
-    lib = load_library()
+    lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.block_map(add, rows, block_table, free_blocks, state, block_rows, start, slots, n_slots)
+        if got is not None:
+            if type(got) is int:
+                raise LaqError(got, "laq_block_map")
+            return got
     n = add.numel()
     _ints(add, "add", rows, n), _ints(rows, "rows", rows, n), _ints(state, "state", rows, 4), _ints(free_blocks, "free_blocks", rows, 1)
     if block_table.dim() != 2 or block_table.shape[0] != n or rows.numel() != n:
         raise ValueError("add and rows are [n], block_table is [n, blocks per request]")
     _ints(block_table, "block_table", rows, n)
+    _here(rows)
     if slots is None and n_slots is not None:
         slots = torch.empty(n_slots, dtype=torch.int32, device=rows.device)
     if start is None and n_slots is not None:
@@ -101,7 +114,13 @@ def laq_block_map(add: torch.Tensor, rows: torch.Tensor, block_table: torch.Tens
 def laq_fp4_store(cache: Fp4Cache, k: Optional[torch.Tensor], v: Optional[torch.Tensor], slots: torch.Tensor, stream=None) -> None:
     """k, v [tokens, Hkv, d] (or one of them; views with contiguous rows, e.g. of a fused projection, are fine) into the rows slots [tokens]
     of the cache; tokens whose slot is -1 are left out."""
-    lib = load_library()
+    lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.fp4_store(cache, k, v, slots)
+        if got is not None:
+            if got is not True:
+                raise LaqError(got, "laq_fp4_store")
+            return
     c = _fp4(cache)
     like = k if k is not None else v
     if like is None:
@@ -123,7 +142,13 @@ def laq_fp4_compact(cache: Fp4Cache, k: torch.Tensor, v: Optional[torch.Tensor],
     """k, v [n, Hkv, L, d] + packed idx (as laq_select writes it) -> the rows slots of the cache: laq_compact into the 4-bit cache.
     slots: one entry per kept row of an instance, for all its KV heads, instance after instance (laq_block_map with add = min(budget, L));
     block_table / L: k, v are paged caches, as for laq_compact."""
-    lib = load_library()
+    lib = binding._lib or load_library()
+    if stream is None and block_table is None and L is None and binding._native is not None:
+        got = binding._native.fp4_compact(cache, k, v, idx, budget, slots)
+        if got is not None:
+            if got is not True:
+                raise LaqError(got, "laq_fp4_compact")
+            return
     c = _fp4(cache)
     _dev(idx, "idx")
     n, Hkv, L, d, kvs, paged = _cache(k, "k", block_table, L)
@@ -146,7 +171,13 @@ def laq_fp4_compact(cache: Fp4Cache, k: torch.Tensor, v: Optional[torch.Tensor],
 def laq_fp4_load(cache: Fp4Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, k: Optional[torch.Tensor] = None,
                  v: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows slots [tokens] of the cache as (k, v) [tokens, Hkv, d] of type dtype (made if not given); rows whose slot is -1 are 0."""
-    lib = load_library()
+    lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.fp4_load(cache, slots, dtype, k, v)
+        if got is not None:
+            if type(got) is int:
+                raise LaqError(got, "laq_fp4_load")
+            return got
     c = _fp4(cache)
     _ints(slots, "slots", cache.k, 0)
     T = slots.numel()
@@ -174,7 +205,13 @@ def laq_fp4_attention(q: torch.Tensor, cache: Fp4Cache, block_table: torch.Tenso
     lengths that the launch is planned with (None: what the table holds).  want_lse (or an lse buffer, fp32 [tokens, Hq]): returns
     (out, lse), lse the logarithm of the sum of the exponentials.  split: let the library spread long rows over several workgroups (a workspace of
     laq_fp4_attention_workspace_bytes is made if ws is None)."""
-    lib = load_library()
+    lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.fp4_attention(q, cache, block_table, rows, start, max_rows, scale, out, lse, want_lse, ws, split)
+        if got is not None:
+            if type(got) is int:
+                raise LaqError(got, "laq_fp4_attention")
+            return got
     c = _fp4(cache)
     strides = _tokens(q, "q", None, c.d)
     T, Hq, d = q.shape
@@ -194,6 +231,8 @@ def laq_fp4_attention(q: torch.Tensor, cache: Fp4Cache, block_table: torch.Tenso
     if lse is None and want_lse:
         lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device)
     code = _dtype_code(q)
+    if ws is not None and (ws.device != q.device or not ws.is_contiguous()):
+        raise ValueError("ws must be a dense tensor on %s" % q.device)
     if not split:
         ws = None
     elif ws is None:
