@@ -15,6 +15,7 @@ namespace {
 
 struct MapArgs {
   int32_t n, block_rows, n_blocks, width, per;         // per: requests of a thread
+  int32_t shift;                                        // log2 of block_rows, or -1
   const int32_t* add;
   int32_t *rows, *table, *list, *state, *start, *slots;
   int64_t n_slots;
@@ -26,16 +27,16 @@ struct Request {
   int32_t need, back;                    // blocks taken (if there are enough), given back
   bool wide;                             // more blocks than the table holds
 };
-__device__ __forceinline__ Request request(const MapArgs& a, int i) {
+__device__ __forceinline__ int blocks_of(const MapArgs& a, int rows) { return a.shift >= 0 ? rows >> a.shift : rows / a.block_rows; }
+__device__ __forceinline__ Request request(const MapArgs& a, int rows, int add) {
   Request r;
-  const long long most = (long long)a.width * a.block_rows;
-  const int add = a.add[i];
-  r.old_rows = (int)min(max((long long)a.rows[i], 0ll), most);
+  const int most = a.width * a.block_rows;
+  r.old_rows = min(max(rows, 0), most);
   const long long now = max((long long)r.old_rows + add, 0ll);
-  r.have = (r.old_rows + a.block_rows - 1) / a.block_rows;
   r.wide = now > most;
   r.new_rows = r.wide ? r.old_rows : (int)now;
-  r.want = (r.new_rows + a.block_rows - 1) / a.block_rows;
+  r.have = blocks_of(a, r.old_rows) + (r.old_rows != blocks_of(a, r.old_rows) * a.block_rows);
+  r.want = blocks_of(a, r.new_rows) + (r.new_rows != blocks_of(a, r.new_rows) * a.block_rows);
   r.more = max(add, 0);
   r.need = max(r.want - r.have, 0);
   r.back = max(r.have - r.want, 0);
@@ -69,12 +70,24 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   __shared__ long long wave_more[WAVES], wave_need[WAVES], wave_back[WAVES];
   __shared__ long long taken_of[WAVES];
   __shared__ int refused_of[WAVES], last;
+  __shared__ int2 given[THREADS];        // rows and add of all requests, where a thread has one
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i0 = (int)min((long long)tid * a.per, (long long)a.n), i1 = (int)min((long long)i0 + a.per, (long long)a.n);
 
+  const bool one = a.per == 1;
+  const int held = a.state[0];
+  int2 mine = {0, 0};
+  if (i0 < i1) mine = int2{a.rows[i0], a.add[i0]};
+  given[tid] = mine;
+  // of this thread's requests; of any (after the first barrier)
+  auto own = [&](int i) { return i == i0 ? request(a, mine.x, mine.y) : request(a, a.rows[i], a.add[i]); };
+  auto any = [&](int i) {
+    const int2 x = one ? given[i] : int2{a.rows[i], a.add[i]};
+    return request(a, x.x, x.y);
+  };
   long long more = 0, need = 0, back = 0;
   for (int i = i0; i < i1; ++i) {
-    const Request r = request(a, i);
+    const Request r = own(i);
     more += r.more;
     need += r.need;
     back += r.back;
@@ -104,12 +117,12 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   need_before[tid] = need0;
   back_before[tid] = back0;
 
-  const long long count = min(max(a.state[0], 0), a.n_blocks), there = count + all_back;
+  const long long count = min(max(held, 0), a.n_blocks), there = count + all_back;
   // blocks taken: up to the last request that gets its own
   long long upto = need0, taken = 0;
   int refused = 0;
   for (int i = i0; i < i1; ++i) {
-    const Request r = request(a, i);
+    const Request r = own(i);
     upto += r.need;
     if (r.need > 0 && upto <= there) taken = upto;
     if (r.wide || (r.need > 0 && upto > there)) ++refused;
@@ -137,7 +150,7 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
     const int t = holder<THREADS>(back_before, x);
     long long at = back_before[t];
     for (int i = t * a.per;; ++i) {
-      const Request q = request(a, i);
+      const Request q = any(i);
       if (x < at + q.back) return a.table[(size_t)i * a.width + q.want + (x - at)];
       at += q.back;
     }
@@ -149,31 +162,44 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   };
 
   const long long first = (long long)blockIdx.x * THREADS + tid, step = (long long)gridDim.x * THREADS;
-  for (long long s = first; s < a.n_slots; s += step) {
-    int slot = -1;
-    if (s < all_more) {
-      const int t = holder<THREADS>(more_before, s);
+  // four slots in a row each: they are mostly of one block
+  for (long long s0 = first * 4; s0 < a.n_slots; s0 += step * 4) {
+    int slot[4] = {-1, -1, -1, -1};
+    if (s0 < all_more) {
+      const int t = holder<THREADS>(more_before, s0);
       long long at = more_before[t], k = need_before[t];
-      int i = t * a.per;
-      Request r = request(a, i);
-      while (s >= at + r.more) {
-        at += r.more;
-        k += r.need;
-        r = request(a, ++i);
-      }
-      if (!r.wide && (r.need == 0 || k + r.need <= there)) {
-        const int row = r.old_rows + (int)(s - at), b = row / a.block_rows;
-        const int number = b < r.have ? a.table[(size_t)i * a.width + b] : block(k + (b - r.have));
-        if (number >= 0 && number < a.n_blocks) slot = number * a.block_rows + (row - b * a.block_rows);
+      int i = t * a.per, known = -1, number = -1;
+      Request r = any(i);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const long long s = s0 + x;
+        if (s >= all_more) break;
+        while (s >= at + r.more) {
+          at += r.more;
+          k += r.need;
+          r = any(++i);
+          known = -1;
+        }
+        if (r.wide || (r.need > 0 && k + r.need > there)) continue;
+        const int row = r.old_rows + (int)(s - at), b = blocks_of(a, row);
+        if (b != known) {
+          known = b;
+          number = b < r.have ? a.table[(size_t)i * a.width + b] : block(k + (b - r.have));
+        }
+        if (number >= 0 && number < a.n_blocks) slot[x] = number * a.block_rows + (row - b * a.block_rows);
       }
     }
-    a.slots[s] = slot;
+    if (s0 + 4 <= a.n_slots && (reinterpret_cast<uintptr_t>(a.slots) & 15) == 0) {
+      *reinterpret_cast<int4*>(a.slots + s0) = int4{slot[0], slot[1], slot[2], slot[3]};
+    } else {
+      for (int x = 0; x < 4 && s0 + x < a.n_slots; ++x) a.slots[s0 + x] = slot[x];
+    }
   }
   for (long long k = first; k < taken; k += step) {
     const int t = holder<THREADS>(need_before, k);
     long long at = need_before[t];
     for (int i = t * a.per;; ++i) {
-      const Request r = request(a, i);
+      const Request r = any(i);
       if (k < at + r.need) {
         a.table[(size_t)i * a.width + r.have + (k - at)] = block(k);
         break;
@@ -186,7 +212,7 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
     long long at = more0;
     for (int i = i0; i < i1; ++i) {
       a.start[i] = (int)min(at, 0x7fffffffll);
-      at += max(a.add[i], 0);
+      at += own(i).more;
     }
     if (tid == 0) a.start[a.n] = (int)min(all_more, 0x7fffffffll);
   }
@@ -199,7 +225,7 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   if (gridDim.x > 1 && !last) return;
   upto = need0;
   for (int i = i0; i < i1; ++i) {
-    const Request r = request(a, i);
+    const Request r = own(i);
     upto += r.need;
     if (!r.wide && (r.need == 0 || upto <= there)) a.rows[i] = r.new_rows;
   }
@@ -210,14 +236,16 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   }
 }
 
-constexpr int MAP_MOST_WORKGROUPS = 64;
+// A thread has four slots, or as many blocks of a batch that is admitted or released, up to a workgroup per compute unit.
+constexpr int MAP_MOST_WORKGROUPS = 256;
 
 }  // namespace
 
 hipError_t launch_block_map(int n, int block_rows, int n_blocks, int width, const int32_t* add, int32_t* rows, int32_t* table, int32_t* list,
                             int32_t* state, int32_t* start, int32_t* slots, int64_t n_slots, hipStream_t st) {
   const int threads = n <= 1024 ? 256 : 1024;
-  const MapArgs a{n, block_rows, n_blocks, width, (n + threads - 1) / threads, add, rows, table, list, state, start, slots, n_slots};
+  const int shift = (block_rows & (block_rows - 1)) == 0 ? __builtin_ctz(block_rows) : -1;
+  const MapArgs a{n, block_rows, n_blocks, width, (n + threads - 1) / threads, shift, add, rows, table, list, state, start, slots, n_slots};
   const int64_t work = n_slots > n_blocks / 4 ? n_slots : n_blocks / 4, wanted = (work + 1023) / 1024;
   const dim3 grid((unsigned)(wanted < 1 ? 1 : wanted > MAP_MOST_WORKGROUPS ? MAP_MOST_WORKGROUPS : wanted));
   if (threads == 256) hipLaunchKernelGGL(block_map_kernel<256>, grid, dim3(256), 0, st, a);

@@ -7,11 +7,12 @@ namespace laq {
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 constexpr int64_t MOST_ROWS = 0x7fffffff;
+constexpr int32_t MOST_HEADS = 32768;
 
 int fp4_view(const laq_fp4_cache* cache, bool need_k, bool need_v, Fp4View* view) {
   if (!cache) return LAQ_ERR_INVALID;
   const laq_fp4_cache& c = *cache;
-  if (c.n_blocks < 1 || c.Hkv < 1 || c.block_rows < 16 || c.block_rows % 16 || c.d < 32 || c.d > 256 || c.d % 32) return LAQ_ERR_INVALID;
+  if (c.n_blocks < 1 || c.Hkv < 1 || c.block_rows < 16 || c.block_rows % 16 || c.d < 32 || c.d > 256 || c.d % 32 || c.Hkv > MOST_HEADS) return LAQ_ERR_INVALID;
   if ((int64_t)c.n_blocks * c.block_rows > MOST_ROWS) return LAQ_ERR_INVALID;
   if ((need_k && (!c.k || !c.k_scale)) || (need_v && (!c.v || !c.v_scale))) return LAQ_ERR_INVALID;
   if ((need_k && !aligned16(c.k)) || (need_v && !aligned16(c.v))) return LAQ_ERR_INVALID;

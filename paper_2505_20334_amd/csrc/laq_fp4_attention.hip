@@ -2,8 +2,8 @@
 //
 // A workgroup has one KV head of a request, a tile of its score rows (row r = query head r % G of the group of the request's token r / G) and a
 // part of the cache.  Its four waves take steps of 16 * KT keys in turn, every wave for all rows of the tile, each with its own running
-// maximum m, sum z and sums O (one pass, exponentials of s - m); they are folded at the end through LDS, parts of a cache by a second
-// launch, in a fixed order.
+// reference m, sum z and sums O (one pass, exponentials of s - m); they are folded at the end through LDS, the parts of a cache by
+// the workgroup that finds all of them finished, in a fixed order.
 //
 // Products are 16 x 16 x 32 bf16 with the keys as the first operand's rows, so that a lane has four keys of one score row (column n = lane % 16) and all that
 // belongs to a row lies in lanes n, n + 16, n + 32, n + 48:
@@ -16,6 +16,9 @@
 //
 // A V that stands for NaN must not reach rows that do not see it (0 * NaN): only in steps whose keys not every row sees, where such
 // a block is, V has 0 there and a second product of ones tells which sums it belongs to.
+#include <atomic>
+#include <chrono>
+
 #include "laq_fp4_codes.h"
 #include "laq_products.h"
 
@@ -74,13 +77,21 @@ struct KeyPiece {
 #pragma unroll
     for (int i = 0; i < NS; ++i) s[i] = scales[scale_at + i];
   }
-  __device__ __forceinline__ uint32_t scale(int t) const { return s[!PIECES<D32> ? t : D32 == 8 ? t / 4 : 0]; }
-  __device__ __forceinline__ u32x4 group(int t) const { return __builtin_bit_cast(u32x4, fp4_to_bf16(c[t], fp4_scale_value(scale(t)))); }
-  __device__ __forceinline__ bool any_nan() const {
-    bool x = false;
+  __device__ __forceinline__ u32x4 group(int t) const { return __builtin_bit_cast(u32x4, fp4_to_bf16(c[t], fp4_scale_value(s[scale_of(t)]))); }
+  static __device__ __forceinline__ int scale_of(int t) { return !PIECES<D32> ? t : D32 == 8 ? t / 4 : 0; }
+  // which of its scales stand for NaN; those blocks are 0 then
+  __device__ __forceinline__ uint32_t take_nan() {
+    uint32_t found = 0;
 #pragma unroll
-    for (int i = 0; i < NS; ++i) x |= s[i] == 255u;
-    return x;
+    for (int i = 0; i < NS; ++i)
+      if (s[i] == 255u) {
+        found |= 1u << i;
+        s[i] = 127;
+#pragma unroll
+        for (int t = 0; t < D32; ++t)
+          if (scale_of(t) == i) c[t] = 0;
+      }
+    return found;
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -209,14 +220,81 @@ template <typename T> __device__ __forceinline__ void put8(T* p, const float (&x
   }
 }
 
-// Sums of a part of a cache: [tile][KV head][part] has ws_rows rows of d sums, and behind all of these as many pairs (maximum in
-// base-2 units, sum).
-__device__ __forceinline__ size_t part_slot(const Fp4View& c, const AttPlan& p, int tile, int kv, int part) {
-  return (((size_t)tile * c.Hkv + kv) * p.parts + part) * p.ws_rows;
+// The parts of cut caches: part s of column (tile, KV head) has sums[column][s][ws_rows][d], and per row two words
+// marks[column][s][ws_rows][2]: the launch's nonce with the reference, and with the sum of weights.
+struct AttParts {
+  unsigned long long* marks;
+  float* sums;
+  uint32_t nonce;                        // a number that no other recent launch of the process has
+};
+// Written through to the device's memory, and read from there.
+__device__ __forceinline__ void store_pair(void* p, uint32_t a, uint32_t b) {
+  __hip_atomic_store(static_cast<unsigned long long*>(p), (unsigned long long)b << 32 | a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint2 load_pair(const void* p) {
+  const unsigned long long v = __hip_atomic_load(static_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_uint2((uint32_t)v, (uint32_t)(v >> 32));
+}
+__device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+constexpr float LN2 = 0.69314718055994530942f;
+// Where score row `row` of the tile goes: its number among the rows of out and lse.
+__device__ __forceinline__ size_t out_row(const Fp4Attention& a, const AttTile& tl, int kv, int G, int row) {
+  const int global = tl.first_row + row, token = global / G;
+  return (size_t)(tl.token0 + token) * a.Hq + kv * G + (global - token * G);
+}
+
+// Folds the parts of a column, in their order, if all of them are finished (decode attention's way, laq_decode.hip): every part sets its marks
+// after its sums have been written and then looks at the marks of all.  Whoever finds all of them set clears them, so that a captured
+// launch, whose nonce is the same every time, never finds its own old ones; whatever else lies in the workspace is an unfinished part.
+template <typename T>
+__device__ void fold_parts(const Fp4View& c, const Fp4Attention& a, const AttPlan& p, const AttTile& tl, const AttParts& pa, size_t column, int kv, int G,
+                           float* sm) {
+  const int tid = threadIdx.x, S = tl.parts, R = tl.n_rows;
+  unsigned long long* const marks = pa.marks + column * p.parts * p.ws_rows * 2;
+  const float* const sums = pa.sums + column * p.parts * p.ws_rows * c.d;
+  float *sm_m = sm, *sm_z = sm + S * R;
+  bool all = true;
+  for (int i = tid; i < S * R; i += ATT_THREADS) {
+    const int s = i / R, r = i - s * R;
+    const unsigned long long* mark = marks + ((size_t)s * p.ws_rows + r) * 2;
+    const uint2 m = load_pair(mark), z = load_pair(mark + 1);
+    all = all && m.x == pa.nonce && z.x == pa.nonce;
+    sm_m[i] = __uint_as_float(m.y);
+    sm_z[i] = __uint_as_float(z.y);
+  }
+  if (!__syncthreads_and(all)) return;
+  for (int i = tid; i < S * R; i += ATT_THREADS) {
+    unsigned long long* mark = marks + ((size_t)(i / R) * p.ws_rows + i % R) * 2;
+    store_pair(mark, 0, 0);
+    store_pair(mark + 1, 0, 0);
+  }
+  const int pairs = c.d / 2;
+  for (int e = tid; e < R * pairs; e += ATT_THREADS) {
+    const int r = e / pairs, col = (e - r * pairs) * 2;
+    float M = -INFINITY;
+    for (int s = 0; s < S; ++s) M = fmaxf(M, sm_m[s * R + r]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float Z = 0.f, x = 0.f, y = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < S; ++s) {
+      const float w = __builtin_amdgcn_exp2f(sm_m[s * R + r] - ref);
+      const uint2 o = load_pair(sums + ((size_t)s * p.ws_rows + r) * c.d + col);
+      Z = fmaf(sm_z[s * R + r], w, Z);
+      x = fmaf(__uint_as_float(o.x), w, x);
+      y = fmaf(__uint_as_float(o.y), w, y);
+    }
+    x = Z == 0.f ? 0.f : x / Z;
+    y = Z == 0.f ? 0.f : y / Z;
+    const size_t to = out_row(a, tl, kv, G, r);
+    if constexpr (is_f32(T())) *reinterpret_cast<float2*>(static_cast<T*>(a.out) + to * c.d + col) = float2{x, y};
+    else *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + to * c.d + col) = pack2(x, y);
+    if (a.lse && col == 0) a.lse[to] = Z == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Z)) * LN2;
+  }
 }
 
 template <typename T, int D32, int RT, int KT>
-__global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, Fp4Attention a, AttPlan p, int n_tiles, float* ws) {
+__global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, Fp4Attention a, AttPlan p, AttParts pa) {
   constexpr int TR = 16 * RT, NP = PARTS_OF<T>;
   constexpr int CG = D32 < 4 ? D32 : 4, CHUNKS = (D32 + 3) / 4;        // groups of a chunk of V's channels (32 columns each), chunks
   constexpr int STRIDE = CG * 64 + 32;                                  // bytes of a key's row of a chunk in LDS
@@ -250,18 +328,24 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
   KeyPiece<D32> kp[KT], vp[KT];
   int64_t code_base[KT], scale_base[KT];
   uint32_t there = 0, there_v = 0;       // a bit for each tile of the step whose rows are there
-  auto locate = [&] {                    // the tiles of the step at `at`
+  auto locate = [&] {                    // the tiles of the step at `at`: one look at the table for those of a block
     int b = block, r = in_block;
+    bool good = false;
     there = 0;
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
-      int number = -1;
-      if (at + i < end) number = table[b];
-      const bool good = number >= 0 && number < c.n_blocks;
-      there |= good ? 1u << i : 0u;
-      const int64_t num = good ? number : 0, row = good ? r * 16 : 0;
-      code_base[i] = num * c.block + row * c.row;
-      scale_base[i] = num * c.scale_block + row * c.scale_row;
+      if (i == 0 || r == 0) {
+        int number = -1;
+        if (at + i < end) number = table[b];
+        good = number >= 0 && number < c.n_blocks;
+        const int64_t num = good ? number : 0, row = good ? r * 16 : 0;
+        code_base[i] = num * c.block + row * c.row;
+        scale_base[i] = num * c.scale_block + row * c.scale_row;
+      } else {
+        code_base[i] = code_base[i - 1] + (good ? 16 * c.row : 0);
+        scale_base[i] = scale_base[i - 1] + (good ? 16 * c.scale_row : 0);
+      }
+      there |= good && at + i < end ? 1u << i : 0u;
       if (++r == per_block) {
         r = 0;
         ++b;
@@ -278,11 +362,15 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
     }
   };
 
-  float m[RT], z[RT];                    // of row n of each tile: maximum of the products, this lane's share of the sum
+  // of row n of each tile: the exponents' reference, the product from which on it is moved (LEEWAY beyond it: weights of up to 2^8 cost
+  // nothing, and most steps then neither look for their rows' maxima across lanes nor touch the sums), this lane's share of the sum
+  constexpr float LEEWAY = 8.f;
+  float off[RT], limit[RT], z[RT];
   f32x4 acc[RT][CHUNKS * CG * 2];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = -INFINITY;
+    off[rt] = 0.f;
+    limit[rt] = -INFINITY;
     z[rt] = 0.f;
 #pragma unroll
     for (int i = 0; i < CHUNKS * CG * 2; ++i) acc[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -340,32 +428,36 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
       for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, s[rt][i][r]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m[rt], top), ref = m_new == -INFINITY ? 0.f : m_new, off = ref * factor[rt];
-      if (__any(m_new > m[rt])) {
-        const float w = __builtin_amdgcn_exp2f((m[rt] - ref) * factor[rt]);
-        z[rt] *= w;
+      if (__any(top > limit[rt])) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (top > limit[rt]) {
+          const float moved = top * factor[rt], w = limit[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[rt] - moved);
+          off[rt] = moved;
+          limit[rt] = (moved + LEEWAY) / factor[rt];
+          z[rt] *= w;
 #pragma unroll
-        for (int i = 0; i < CHUNKS * CG * 2; ++i)
+          for (int i = 0; i < CHUNKS * CG * 2; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[rt][i][r] *= w;
-        m[rt] = m_new;
+            for (int r = 0; r < 4; ++r) acc[rt][i][r] *= w;
+        }
       }
 #pragma unroll
       for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[rt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[rt][i][r], factor[rt], -off));
+          s[rt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[rt][i][r], factor[rt], -off[rt]));
           z[rt] += s[rt][i][r];
         }
     }
     bool nan_rows = false;               // some V stands for NaN where not every row sees it
+    uint32_t nan_at[KT];
     if (masked) {
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         if (!(there_v >> i & 1) || key0 + i * 16 + n >= tl.seen_max) vp[i].clear();
-        nan_rows |= vp[i].any_nan();
+        nan_at[i] = vp[i].take_nan();
+        nan_rows |= nan_at[i] != 0;
       }
       nan_rows = __any(nan_rows);
     }
@@ -374,19 +466,15 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
       u32x4 w[RT][NP];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) split_weights<T>(s[rt][j], s[rt][j + 1], w[rt]);
-      // chunk ch of two tiles of V to LDS; with ONES, 1 where it stands for NaN and else 0; without, 0 there if such are taken apart
+      // chunk ch of two tiles of V to LDS; with ONES, 1 where it stands for NaN and else 0
       auto stage = [&](int ch, bool ones) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int t = 0; t < CG; ++t)
             if (ch * CG + t < D32) {
-              u32x4 x = vp[j + i].group(ch * CG + t);
-              if (nan_rows) {
-                const bool bad = vp[j + i].scale(ch * CG + t) == 255u;
-                if (bad || ones) x = bad && ones ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u} : u32x4{0, 0, 0, 0};
-              }
-              *reinterpret_cast<u32x4*>(v_write + i * 16 * STRIDE + t * 64) = x;
+              const uint32_t one = ones && nan_at[j + i] >> KeyPiece<D32>::scale_of(ch * CG + t) & 1 ? 0x3f803f80u : 0u;
+              *reinterpret_cast<u32x4*>(v_write + i * 16 * STRIDE + t * 64) = ones ? u32x4{one, one, one, one} : vp[j + i].group(ch * CG + t);
             }
       };
       auto column = [&](int ct) {        // 32 keys of 16 columns
@@ -410,7 +498,7 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
 #pragma unroll
             for (int pl = 0; pl < NP; ++pl) acc[rt][ch * CG * 2 + ct] = mfma16(v8, w[rt][NP - 1 - pl], acc[rt][ch * CG * 2 + ct]);
         }
-        if (nan_rows) {
+        if (__builtin_expect(nan_rows, 0)) {
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
           stage(ch, true);
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -448,14 +536,13 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
     z[rt] += __shfl_xor(z[rt], 16);
     z[rt] += __shfl_xor(z[rt], 32);
     if (h == 0) {
-      sm_m[wave][rt * 16 + n] = m[rt] * factor[rt];
+      sm_m[wave][rt * 16 + n] = limit[rt] == -INFINITY ? -INFINITY : off[rt];
       sm_z[wave][rt * 16 + n] = z[rt];
     }
   }
   __syncthreads();
   const bool whole = tl.parts == 1;
-  const size_t slot = part_slot(c, p, tile, kv, part);
-  float* const pairs = ws + (size_t)n_tiles * c.Hkv * p.parts * p.ws_rows * c.d;
+  const size_t column = (size_t)tile * c.Hkv + kv, slot = (column * p.parts + part) * p.ws_rows;
   auto row_sum = [&](int r, float* top) {        // over the waves, of a row
     float M = sm_m[0][r];
 #pragma unroll
@@ -501,62 +588,34 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
             const float Z = row_sum(row, &top);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = Z == 0.f ? 0.f : x[i] / Z;
-            const int global = tl.first_row + row, token = global / G;
-            put8(static_cast<T*>(a.out) + ((size_t)(tl.token0 + token) * a.Hq + kv * G + (global - token * G)) * c.d + channel, x);
+            put8(static_cast<T*>(a.out) + out_row(a, tl, kv, G, row) * c.d + channel, x);
           } else {
-            put8(ws + (slot + row) * c.d + channel, x);
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) store_pair(pa.sums + (slot + row) * c.d + channel + i, __float_as_uint(x[i]), __float_as_uint(x[i + 1]));
           }
         }
       }
       __syncthreads();
     }
   }
+  if (!whole) {
+    stores_done();
+    __syncthreads();
+  }
   for (int row = threadIdx.x; row < tl.n_rows; row += ATT_THREADS) {
     float top;
     const float Z = row_sum(row, &top);
     if (!whole) {
-      *reinterpret_cast<float2*>(pairs + (slot + row) * 2) = float2{top, Z};
+      store_pair(pa.marks + (slot + row) * 2, pa.nonce, __float_as_uint(top));
+      store_pair(pa.marks + (slot + row) * 2 + 1, pa.nonce, __float_as_uint(Z));
+      stores_done();
     } else if (a.lse) {
-      const int global = tl.first_row + row, token = global / G;
-      a.lse[(size_t)(tl.token0 + token) * a.Hq + kv * G + (global - token * G)] =
-          Z == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(Z)) * 0.69314718055994530942f;
+      a.lse[out_row(a, tl, kv, G, row)] = Z == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(Z)) * LN2;
     }
   }
-}
-
-// Joins the parts of a tile, in their order.
-template <typename T, int TR>
-__global__ __launch_bounds__(ATT_THREADS) void fp4_attention_join(Fp4View c, Fp4Attention a, AttPlan p, int n_tiles, const float* ws) {
-  const int G = a.Hq / c.Hkv, kv = blockIdx.x % c.Hkv, tile = blockIdx.x / c.Hkv;
-  AttTile tl;
-  if (!find_tile<TR>(c, a, p, tile, G, &tl) || tl.parts == 1) return;
-  const float2* pairs = reinterpret_cast<const float2*>(ws + (size_t)n_tiles * c.Hkv * p.parts * p.ws_rows * c.d);
-  const size_t slot = part_slot(c, p, tile, kv, 0);
-  const int pieces = c.d / 8;
-  for (int e = threadIdx.x; e < tl.n_rows * pieces; e += ATT_THREADS) {
-    const int row = e / pieces, col = (e - row * pieces) * 8;
-    float M = -INFINITY;
-    for (int s = 0; s < tl.parts; ++s) M = fmaxf(M, pairs[slot + (size_t)s * p.ws_rows + row].x);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float Z = 0.f, x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-    for (int s = 0; s < tl.parts; ++s) {
-      const size_t at = slot + (size_t)s * p.ws_rows + row;
-      const float2 mz = pairs[at];
-      const float w = __builtin_amdgcn_exp2f(mz.x - ref);
-      Z = fmaf(mz.y, w, Z);
-      const float* o = ws + at * c.d + col;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fmaf(o[i], w, x[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = Z == 0.f ? 0.f : x[i] / Z;
-    const int global = tl.first_row + row, token = global / G;
-    const size_t to = (size_t)(tl.token0 + token) * a.Hq + kv * G + (global - token * G);
-    put8(static_cast<T*>(a.out) + to * c.d + col, x);
-    if (a.lse && col == 0) a.lse[to] = Z == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Z)) * 0.69314718055994530942f;
-  }
+  if (whole) return;
+  __syncthreads();
+  fold_parts<T>(c, a, p, tl, pa, column, kv, G, reinterpret_cast<float*>(lds));
 }
 
 constexpr int ATT_PART_STEP = 256;         // rows of a part: a multiple of what the four waves take in a turn
@@ -566,7 +625,7 @@ struct AttLaunch {
   AttPlan plan;
   int row_tiles, key_tiles;              // RT, KT
   int n_tiles;
-  size_t bytes;
+  size_t rows;                           // of all parts, in the workspace
 };
 
 AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each) {
@@ -584,47 +643,47 @@ AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_t
   long long parts = (ATT_WORKGROUPS + busy - 1) / busy;
   const long long most = (max_rows + ATT_PART_STEP - 1) / ATT_PART_STEP;
   if (parts > most) parts = most;
+  // the folding workgroup has two words for every row and part in LDS: what the kernel's other use of it leaves room for
+  const int fold_most = ATT_WAVES * 32 * ((c.d < 128 ? c.d : 128) * 2 + 32) / (8 * TR);
+  if (parts > fold_most) parts = fold_most;
   const long long steps = (most + parts - 1) / parts;
   l.plan.part_rows = (int)(steps * ATT_PART_STEP);
   l.plan.parts = (int)((most + steps - 1) / steps);
   const int per_block = c.block_rows / 16, turn = ATT_WAVES * l.key_tiles;
   l.plan.adv_blocks = turn / per_block;
   l.plan.adv_tiles = turn % per_block;
-  l.bytes = l.plan.parts == 1 ? 0 : (size_t)l.n_tiles * c.Hkv * l.plan.parts * l.plan.ws_rows * (c.d + 2) * sizeof(float);
+  l.rows = l.plan.parts == 1 ? 0 : (size_t)l.n_tiles * c.Hkv * l.plan.parts * l.plan.ws_rows;
   return l;
 }
 
 template <typename T, int D32, int RT, int KT>
-hipError_t launch_att(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, float* ws, hipStream_t st) {
-  const long long blocks = (long long)l.n_tiles * c.Hkv * l.plan.parts;
-  hipLaunchKernelGGL((fp4_attention_kernel<T, D32, RT, KT>), dim3((unsigned)blocks), dim3(ATT_THREADS), 0, st, c, a, l.plan, l.n_tiles, ws);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || l.plan.parts == 1) return e;
-  hipLaunchKernelGGL((fp4_attention_join<T, 16 * RT>), dim3((unsigned)(l.n_tiles * c.Hkv)), dim3(ATT_THREADS), 0, st, c, a, l.plan, l.n_tiles, ws);
+hipError_t launch_att(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
+  hipLaunchKernelGGL((fp4_attention_kernel<T, D32, RT, KT>), dim3((unsigned)((long long)l.n_tiles * c.Hkv * l.plan.parts)), dim3(ATT_THREADS), 0, st, c, a,
+                     l.plan, pa);
   return hipGetLastError();
 }
 
 template <typename T, int D32>
-hipError_t launch_d(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, float* ws, hipStream_t st) {
+hipError_t launch_d(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
   if constexpr (is_f32(T())) {
-    return launch_att<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, ws, st);
+    return launch_att<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, pa, st);
   } else {
-    if (l.row_tiles == 1) return launch_att<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, ws, st);
-    return launch_att<T, D32, 2, 2>(c, a, l, ws, st);
+    if (l.row_tiles == 1) return launch_att<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, pa, st);
+    return launch_att<T, D32, 2, 2>(c, a, l, pa, st);
   }
 }
 
 template <typename T>
-hipError_t launch_t(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, float* ws, hipStream_t st) {
+hipError_t launch_t(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
   switch (c.d / 32) {
-    case 1: return launch_d<T, 1>(c, a, l, ws, st);
-    case 2: return launch_d<T, 2>(c, a, l, ws, st);
-    case 3: return launch_d<T, 3>(c, a, l, ws, st);
-    case 4: return launch_d<T, 4>(c, a, l, ws, st);
-    case 5: return launch_d<T, 5>(c, a, l, ws, st);
-    case 6: return launch_d<T, 6>(c, a, l, ws, st);
-    case 7: return launch_d<T, 7>(c, a, l, ws, st);
-    default: return launch_d<T, 8>(c, a, l, ws, st);
+    case 1: return launch_d<T, 1>(c, a, l, pa, st);
+    case 2: return launch_d<T, 2>(c, a, l, pa, st);
+    case 3: return launch_d<T, 3>(c, a, l, pa, st);
+    case 4: return launch_d<T, 4>(c, a, l, pa, st);
+    case 5: return launch_d<T, 5>(c, a, l, pa, st);
+    case 6: return launch_d<T, 6>(c, a, l, pa, st);
+    case 7: return launch_d<T, 7>(c, a, l, pa, st);
+    default: return launch_d<T, 8>(c, a, l, pa, st);
   }
 }
 
@@ -632,9 +691,9 @@ hipError_t launch_t(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l,
 
 size_t fp4_attention_bytes(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows) {
   // (whether the tokens are one each is not known here: the larger of both)
-  const size_t some = plan_attention(c, Hq, dtype, n, n_tokens, max_rows, false).bytes;
-  const size_t one = n_tokens == n ? plan_attention(c, Hq, dtype, n, n_tokens, max_rows, true).bytes : 0;
-  return some > one ? some : one;
+  const size_t some = plan_attention(c, Hq, dtype, n, n_tokens, max_rows, false).rows;
+  const size_t one = n_tokens == n ? plan_attention(c, Hq, dtype, n, n_tokens, max_rows, true).rows : 0;
+  return (some > one ? some : one) * (2 * sizeof(unsigned long long) + c.d * sizeof(float));
 }
 
 bool fp4_attention_fits(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each) {
@@ -645,7 +704,13 @@ bool fp4_attention_fits(const Fp4View& c, int Hq, int dtype, int n, int64_t n_to
 hipError_t launch_fp4_attention(const Fp4View& c, int dtype, const Fp4Attention& a, void* ws, size_t, hipStream_t st) {
   AttLaunch l = plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, a.start == nullptr);
   if (!ws) l.plan.parts = 1;
-  return dtype == LAQ_BF16 ? launch_t<uint16_t>(c, a, l, static_cast<float*>(ws), st) : launch_t<float>(c, a, l, static_cast<float*>(ws), st);
+  static std::atomic<uint32_t> launches{(uint32_t)(std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull >> 32)};
+  AttParts pa{static_cast<unsigned long long*>(ws), nullptr, 0};
+  if (l.plan.parts > 1) {
+    pa.sums = reinterpret_cast<float*>(pa.marks + 2 * l.rows);
+    do pa.nonce = launches.fetch_add(1); while (pa.nonce == 0);        // 0 is the cleared mark
+  }
+  return dtype == LAQ_BF16 ? launch_t<uint16_t>(c, a, l, pa, st) : launch_t<float>(c, a, l, pa, st);
 }
 
 }  // namespace laq
