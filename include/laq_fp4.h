@@ -37,7 +37,7 @@ typedef struct laq_fp4_cache {
   uint8_t *k, *k_scale;  /* codes [n_blocks, Hkv, block_rows, d / 2] and scales [n_blocks, Hkv, block_rows, d / 32] */
   uint8_t *v, *v_scale;
   int32_t n_blocks;      /* >= 1; n_blocks * block_rows < 2^31 */
-  int32_t Hkv;
+  int32_t Hkv;           /* <= 32768 */
   int32_t block_rows;    /* a multiple of 16 */
   int32_t d;             /* head size, a multiple of 32, <= 256 */
   /*

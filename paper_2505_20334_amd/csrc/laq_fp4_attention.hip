@@ -1,9 +1,13 @@
 // Attention over the paged 4-bit cache (include/laq_fp4.h: laq_fp4_attention).
 //
-// A workgroup has one KV head of a request, a tile of its score rows (row r = query head r % G of the group of the request's token r / G) and a
-// part of the cache.  Its four waves take steps of 16 * KT keys in turn, every wave for all rows of the tile, each with its own running
-// reference m, sum z and sums O (one pass, exponentials of s - m); they are folded at the end through LDS, the parts of a cache by
-// the workgroup that finds all of them finished, in a fixed order.
+// A column is a KV head of a request and a tile of its score rows (row r = query head r % G of the group of the request's token r / G).  A workgroup has a
+// range of a column's keys, in turns of 64 * KT: its four waves take 16 * KT keys of a turn each, every wave for all rows of the tile, with its own
+// reference m, sum z and sums O (one pass, exponentials of s - m); they are folded at the end through LDS, the ranges of a column by the
+// workgroup that finds all of them finished, in a fixed order.
+//
+// How the ranges lie: where requests have a token each, all turns of all columns are shared out evenly (fp4_attention_shares), since the lengths, which the host does
+// not know, are as unequal as requests are.  Several tokens: equal parts of the longest request that the host expects, where there would be too few
+// workgroups otherwise.
 //
 // Products are 16 x 16 x 32 bf16 with the keys as the first operand's rows, so that a lane has four keys of one score row (column n = lane % 16) and all that
 // belongs to a row lies in lanes n, n + 16, n + 32, n + 48:
@@ -18,6 +22,7 @@
 // a block is, V has 0 there and a second product of ones tells which sums it belongs to.
 #include <atomic>
 #include <chrono>
+#include <type_traits>
 
 #include "laq_fp4_codes.h"
 #include "laq_products.h"
@@ -36,10 +41,10 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) { return __builtin_b
 
 // How the launch is cut, from what the host knows.
 struct AttPlan {
-  int32_t parts, part_rows;              // a request's rows in parts of part_rows, `parts` at most (the last one takes what is left)
-  int32_t tiles_per;                     // without `start`: tiles of a request
+  int32_t parts, part_rows;              // several tokens: a column in parts of part_rows, `parts` at most (the last one takes what is left)
+  int32_t tiles_per;                     // a token each: tiles of a request
   int32_t ws_rows;                       // rows of a tile that can be there
-  int32_t adv_blocks, adv_tiles;         // what a wave's step moves a position (block, key tile in it) by
+  int32_t adv_blocks, adv_tiles;         // what a turn moves a position (block, key tile in it) by
 };
 
 // Channel of number i of group t of lane quarter h: whole pieces of a row where scale blocks and pieces fit each other, else 8 of each block.
@@ -52,27 +57,27 @@ struct KeyPiece {
   static constexpr int NS = !PIECES<D32> ? D32 : D32 == 8 ? 2 : 1;
   uint32_t c[D32];
   uint32_t s[NS];
-  // codes, scales: of the tile's first row (uniform); the offsets: of this lane's
+  // codes, scales: of the tile's first row (uniform); the offsets: of this lane's.  ONCE: rows that one workgroup reads, past the caches
+  // (96 requests x 6144 rows x 8 heads, 641 MB: 112 us, 126 without; with 32 tiles of a request that read the same rows 288 against 267)
+  template <bool ONCE, typename W>
+  static __device__ __forceinline__ W word(const uint8_t* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const W*>(p));
+    else return *reinterpret_cast<const W*>(p);
+  }
+  template <bool ONCE>
   __device__ __forceinline__ void read(const uint8_t* codes, const uint8_t* scales, uint32_t code_at, uint32_t scale_at) {
-    if constexpr (PIECES<D32>) {
-      typedef uint32_t words __attribute__((ext_vector_type(D32 == 1 ? 2 : D32)));
-      if constexpr (D32 == 1) {
-        c[0] = *reinterpret_cast<const uint32_t*>(codes + code_at);
-      } else if constexpr (D32 == 8) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(codes + code_at), b = *reinterpret_cast<const u32x4*>(codes + code_at + 16);
+    if constexpr (PIECES<D32> && D32 > 1) {
+      constexpr int N = D32 < 4 ? D32 : 4;
+      typedef uint32_t words __attribute__((ext_vector_type(N)));
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          c[t] = a[t];
-          c[t + 4] = b[t];
-        }
-      } else {
-        const words w = *reinterpret_cast<const words*>(codes + code_at);
+      for (int j = 0; j < D32; j += N) {
+        const words w = word<ONCE, words>(codes + code_at + 4 * j);
 #pragma unroll
-        for (int t = 0; t < D32; ++t) c[t] = w[t];
+        for (int t = 0; t < N; ++t) c[j + t] = w[t];
       }
     } else {
 #pragma unroll
-      for (int t = 0; t < D32; ++t) c[t] = *reinterpret_cast<const uint32_t*>(codes + code_at + 16 * t);
+      for (int t = 0; t < D32; ++t) c[t] = word<ONCE, uint32_t>(codes + code_at + 16 * t);
     }
 #pragma unroll
     for (int i = 0; i < NS; ++i) s[i] = scales[scale_at + i];
@@ -110,19 +115,22 @@ struct AttTile {
   int first_row, n_rows;                 // score rows of this tile among the request's T * G
   int held;                              // rows of the cache
   int seen_min, seen_max;                // rows that the first and the last score row see
-  int parts;
 };
 // The rows that score row r of the request sees.
 __device__ __forceinline__ int rows_seen(const AttTile& t, int r, int G) { return min(max(t.held - t.T + r / G + 1, 0), t.held); }
 
+__device__ __forceinline__ int rows_held(const Fp4View& c, const Fp4Attention& a, int rows) {
+  return (int)min((long long)max(rows, 0), (long long)a.blocks_per_inst * c.block_rows);
+}
+
+// Tile `tile` of the batch.
 template <int TR>
 __device__ __forceinline__ bool find_tile(const Fp4View& c, const Fp4Attention& a, const AttPlan& p, int tile, int G, AttTile* out) {
   int tin;
   if (!a.start) {
-    out->inst = tile / p.tiles_per;
-    tin = tile - out->inst * p.tiles_per;
-    out->token0 = out->inst;
+    out->inst = out->token0 = tile / p.tiles_per;
     out->T = 1;
+    tin = tile - out->inst * p.tiles_per;
   } else {
     // request i has the tiles from start[i] * G / TR + i on: never fewer than it needs
     const auto start = [&](int i) { return min(max(a.start[i], 0), (int)a.n_tokens); };
@@ -135,15 +143,14 @@ __device__ __forceinline__ bool find_tile(const Fp4View& c, const Fp4Attention& 
     out->token0 = start(lo);
     out->T = max(start(lo + 1) - out->token0, 0);
     tin = tile - ((int)((uint32_t)(out->token0 * G) / TR) + lo);
+    if (tin < 0) return false;           // (a `start` that does not begin with 0)
   }
-  if (tin < 0) return false;             // (a `start` that does not begin with 0)
   out->first_row = tin * TR;
   out->n_rows = min(out->T * G - out->first_row, TR);
   if (out->n_rows <= 0) return false;
-  out->held = (int)min((long long)max(a.rows[out->inst], 0), (long long)a.blocks_per_inst * c.block_rows);
+  out->held = rows_held(c, a, a.rows[out->inst]);
   out->seen_min = rows_seen(*out, out->first_row, G);
   out->seen_max = rows_seen(*out, out->first_row + out->n_rows - 1, G);
-  out->parts = min(p.parts, max((out->seen_max + p.part_rows - 1) / p.part_rows, 1));
   return true;
 }
 
@@ -220,12 +227,19 @@ template <typename T> __device__ __forceinline__ void put8(T* p, const float (&x
   }
 }
 
-// The parts of cut caches: part s of column (tile, KV head) has sums[column][s][ws_rows][d], and per row two words
-// marks[column][s][ws_rows][2]: the launch's nonce with the reference, and with the sum of weights.
+// The ranges of cut columns: a slot of the workspace has sums[slot][ws_rows][d], and per row two words marks[slot][ws_rows][2]: the
+// launch's nonce with the reference, and with the sum of weights.
 struct AttParts {
   unsigned long long* marks;
   float* sums;
   uint32_t nonce;                        // a number that no other recent launch of the process has
+};
+// Range s of `count` of a column: slots first, then second, second + step, ...
+struct AttColumn {
+  int s, count;
+  size_t first, second;
+  int step;
+  __device__ __forceinline__ size_t slot(int i) const { return i == 0 ? first : second + (size_t)(i - 1) * step; }
 };
 // Written through to the device's memory, and read from there.
 __device__ __forceinline__ void store_pair(void* p, uint32_t a, uint32_t b) {
@@ -244,70 +258,112 @@ __device__ __forceinline__ size_t out_row(const Fp4Attention& a, const AttTile& 
   return (size_t)(tl.token0 + token) * a.Hq + kv * G + (global - token * G);
 }
 
-// Folds the parts of a column, in their order, if all of them are finished (decode attention's way, laq_decode.hip): every part sets its marks
+// Folds the ranges of a column, in their order, if all of them are finished (decode attention's way, laq_decode.hip): every range sets its marks
 // after its sums have been written and then looks at the marks of all.  Whoever finds all of them set clears them, so that a captured
-// launch, whose nonce is the same every time, never finds its own old ones; whatever else lies in the workspace is an unfinished part.
-template <typename T>
-__device__ void fold_parts(const Fp4View& c, const Fp4Attention& a, const AttPlan& p, const AttTile& tl, const AttParts& pa, size_t column, int kv, int G,
-                           float* sm) {
-  const int tid = threadIdx.x, S = tl.parts, R = tl.n_rows;
-  unsigned long long* const marks = pa.marks + column * p.parts * p.ws_rows * 2;
-  const float* const sums = pa.sums + column * p.parts * p.ws_rows * c.d;
-  float *sm_m = sm, *sm_z = sm + S * R;
+// launch, whose nonce is the same every time, never finds its own old ones; whatever else lies in the workspace is an unfinished range.
+// `sm`: room for FOLD marks.
+template <typename T, int FOLD>
+__device__ void fold_ranges(const Fp4View& c, const Fp4Attention& a, const AttPlan& p, const AttTile& tl, const AttParts& pa, const AttColumn& col, int kv,
+                            int G, float2* sm) {
+  const int tid = threadIdx.x, R = tl.n_rows;
   bool all = true;
-  for (int i = tid; i < S * R; i += ATT_THREADS) {
-    const int s = i / R, r = i - s * R;
-    const unsigned long long* mark = marks + ((size_t)s * p.ws_rows + r) * 2;
+  for (int i = tid; i < col.count * R; i += ATT_THREADS) {
+    const unsigned long long* mark = pa.marks + (col.slot(i / R) * p.ws_rows + i % R) * 2;
     const uint2 m = load_pair(mark), z = load_pair(mark + 1);
     all = all && m.x == pa.nonce && z.x == pa.nonce;
-    sm_m[i] = __uint_as_float(m.y);
-    sm_z[i] = __uint_as_float(z.y);
+    if (i < FOLD) sm[i] = float2{__uint_as_float(m.y), __uint_as_float(z.y)};
   }
   if (!__syncthreads_and(all)) return;
-  for (int i = tid; i < S * R; i += ATT_THREADS) {
-    unsigned long long* mark = marks + ((size_t)(i / R) * p.ws_rows + i % R) * 2;
+  const int pairs = c.d / 2, at_once = FOLD / R;           // ranges whose marks fit
+  // EU pairs of channels of a thread at a time, so that enough loads are under way: 16
+  auto fold = [&](auto EUC) {
+    constexpr int EU = decltype(EUC)::value;
+    for (int e0 = tid; e0 < (R * pairs + ATT_THREADS - 1) / ATT_THREADS * ATT_THREADS; e0 += ATT_THREADS * EU) {
+      int row[EU], ch[EU];
+      float M[EU], Z[EU], x[EU], y[EU];
+#pragma unroll
+      for (int u = 0; u < EU; ++u) {
+        const int e = min(e0 + u * ATT_THREADS, R * pairs - 1);
+        row[u] = e / pairs;
+        ch[u] = (e - row[u] * pairs) * 2;
+        M[u] = -INFINITY;
+        Z[u] = x[u] = y[u] = 0.f;
+      }
+      for (int s0 = 0; s0 < col.count; s0 += at_once) {
+        const int n = min(at_once, col.count - s0);
+        if (col.count > at_once) {
+          __syncthreads();
+          for (int i = tid; i < n * R; i += ATT_THREADS) {
+            const unsigned long long* mark = pa.marks + (col.slot(s0 + i / R) * p.ws_rows + i % R) * 2;
+            sm[i] = float2{__uint_as_float(load_pair(mark).y), __uint_as_float(load_pair(mark + 1).y)};
+          }
+          __syncthreads();
+        }
+        float ref[EU];
+#pragma unroll
+        for (int u = 0; u < EU; ++u) {
+          float top = M[u];
+          for (int s = 0; s < n; ++s) top = fmaxf(top, sm[s * R + row[u]].x);
+          ref[u] = top == -INFINITY ? 0.f : top;
+          const float w = M[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M[u] - ref[u]);
+          M[u] = top;
+          Z[u] *= w;
+          x[u] *= w;
+          y[u] *= w;
+        }
+#pragma unroll(16 / EU)
+        for (int s = 0; s < n; ++s) {
+          const float* from = pa.sums + col.slot(s0 + s) * p.ws_rows * c.d;
+#pragma unroll
+          for (int u = 0; u < EU; ++u) {
+            const float2 mz = sm[s * R + row[u]];
+            const uint2 o = load_pair(from + row[u] * c.d + ch[u]);
+            const float w = __builtin_amdgcn_exp2f(mz.x - ref[u]);
+            Z[u] = fmaf(mz.y, w, Z[u]);
+            x[u] = fmaf(__uint_as_float(o.x), w, x[u]);
+            y[u] = fmaf(__uint_as_float(o.y), w, y[u]);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < EU; ++u) {
+        if (e0 + u * ATT_THREADS >= R * pairs) break;
+        const float vx = Z[u] == 0.f ? 0.f : x[u] / Z[u], vy = Z[u] == 0.f ? 0.f : y[u] / Z[u];
+        const size_t to = out_row(a, tl, kv, G, row[u]);
+        if constexpr (is_f32(T())) *reinterpret_cast<float2*>(static_cast<T*>(a.out) + to * c.d + ch[u]) = float2{vx, vy};
+        else *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + to * c.d + ch[u]) = pack2(vx, vy);
+        if (a.lse && ch[u] == 0) a.lse[to] = Z[u] == 0.f ? -INFINITY : (M[u] + __builtin_amdgcn_logf(Z[u])) * LN2;
+      }
+    }
+  };
+  if (R * pairs <= ATT_THREADS) fold(std::integral_constant<int, 1>{});
+  else fold(std::integral_constant<int, 4>{});
+  if (col.count > at_once) __syncthreads();                // (the marks are read until here)
+  for (int i = tid; i < col.count * R; i += ATT_THREADS) {
+    unsigned long long* mark = pa.marks + (col.slot(i / R) * p.ws_rows + i % R) * 2;
     store_pair(mark, 0, 0);
     store_pair(mark + 1, 0, 0);
   }
-  const int pairs = c.d / 2;
-  for (int e = tid; e < R * pairs; e += ATT_THREADS) {
-    const int r = e / pairs, col = (e - r * pairs) * 2;
-    float M = -INFINITY;
-    for (int s = 0; s < S; ++s) M = fmaxf(M, sm_m[s * R + r]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float Z = 0.f, x = 0.f, y = 0.f;
-#pragma unroll 8
-    for (int s = 0; s < S; ++s) {
-      const float w = __builtin_amdgcn_exp2f(sm_m[s * R + r] - ref);
-      const uint2 o = load_pair(sums + ((size_t)s * p.ws_rows + r) * c.d + col);
-      Z = fmaf(sm_z[s * R + r], w, Z);
-      x = fmaf(__uint_as_float(o.x), w, x);
-      y = fmaf(__uint_as_float(o.y), w, y);
-    }
-    x = Z == 0.f ? 0.f : x / Z;
-    y = Z == 0.f ? 0.f : y / Z;
-    const size_t to = out_row(a, tl, kv, G, r);
-    if constexpr (is_f32(T())) *reinterpret_cast<float2*>(static_cast<T*>(a.out) + to * c.d + col) = float2{x, y};
-    else *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + to * c.d + col) = pack2(x, y);
-    if (a.lse && col == 0) a.lse[to] = Z == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Z)) * LN2;
-  }
 }
 
-template <typename T, int D32, int RT, int KT>
-__global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, Fp4Attention a, AttPlan p, AttParts pa) {
-  constexpr int TR = 16 * RT, NP = PARTS_OF<T>;
-  constexpr int CG = D32 < 4 ? D32 : 4, CHUNKS = (D32 + 3) / 4;        // groups of a chunk of V's channels (32 columns each), chunks
-  constexpr int STRIDE = CG * 64 + 32;                                  // bytes of a key's row of a chunk in LDS
-  constexpr int OSTRIDE = CG * 32 + 4;                                  // floats of a row's sums in LDS
-  constexpr int V_BYTES = 32 * STRIDE, O_BYTES = 16 * OSTRIDE * 4;
-  constexpr int WAVE_BYTES = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
-  __shared__ __align__(16) unsigned char lds[ATT_WAVES * WAVE_BYTES];
-  __shared__ float sm_m[ATT_WAVES][TR], sm_z[ATT_WAVES][TR];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h = lane >> 4;
-  const int G = a.Hq / c.Hkv, kv = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, part = rest % p.parts, tile = rest / p.parts;
-  AttTile tl;
-  if (!find_tile<TR>(c, a, p, tile, G, &tl) || part >= tl.parts) return;
+template <int D32, int RT>
+struct AttLds {
+  static constexpr int CG = D32 < 4 ? D32 : 4, CHUNKS = (D32 + 3) / 4;        // groups of a chunk of V's channels (32 columns each), chunks
+  static constexpr int STRIDE = CG * 64 + 32;                                  // bytes of a key's row of a chunk
+  static constexpr int OSTRIDE = CG * 32 + 4;                                  // floats of a row's sums
+  static constexpr int V_BYTES = 32 * STRIDE, O_BYTES = 16 * OSTRIDE * 4;
+  static constexpr int WAVE_BYTES = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
+  __align__(16) unsigned char wave[ATT_WAVES][WAVE_BYTES];
+  float m[ATT_WAVES][16 * RT], z[ATT_WAVES][16 * RT];
+};
 
+// The key tiles first .. end - 1 of a column.
+template <typename T, int D32, int RT, int KT, bool ONCE>
+__device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, const AttPlan& p, const AttParts& pa, const AttTile& tl, int kv, int G,
+                                       int first, int end, const AttColumn& col, AttLds<D32, RT>& sh) {
+  using Lds = AttLds<D32, RT>;
+  constexpr int NP = PARTS_OF<T>, CG = Lds::CG, CHUNKS = Lds::CHUNKS, STRIDE = Lds::STRIDE, OSTRIDE = Lds::OSTRIDE;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h = lane >> 4;
   u32x4 q[RT][D32][NP];
   float factor[RT];
   read_queries<T, D32, RT>(a, tl, kv, G, lane, q, factor);
@@ -315,9 +371,7 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) seen[rt] = rows_seen(tl, tl.first_row + min(rt * 16 + n, tl.n_rows - 1), G);
 
-  // key tiles of this part, and this wave's position: tile `at`, in block `block` of the request its tile `in_block`
-  const int first = part * p.part_rows / 16;
-  const int end = part == tl.parts - 1 ? (tl.seen_max + 15) / 16 : (part + 1) * p.part_rows / 16;
+  // this wave's position: key tile `at`, in block `block` of the request its tile `in_block`
   const int per_block = c.block_rows / 16;
   int at = first + wave * KT, block = at / per_block, in_block = at - block * per_block;
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
@@ -375,7 +429,7 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
 #pragma unroll
     for (int i = 0; i < CHUNKS * CG * 2; ++i) acc[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  unsigned char* const my_lds = lds + wave * WAVE_BYTES;
+  unsigned char* const my_lds = sh.wave[wave];
   unsigned char* const v_write = my_lds + n * STRIDE + h * 16;
   const uint32_t v_read = (uint32_t)(4 * h + n / 4) * STRIDE + (n & 3) * 8;
   typedef __attribute__((address_space(3))) s16x4* LdsQuad;
@@ -384,9 +438,9 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
     locate();
     there_v = there;
 #pragma unroll
-    for (int i = 0; i < KT; ++i) kp[i].read(kc + code_base[i], ks + scale_base[i], code_at, scale_at);
+    for (int i = 0; i < KT; ++i) kp[i].template read<ONCE>(kc + code_base[i], ks + scale_base[i], code_at, scale_at);
 #pragma unroll
-    for (int i = 0; i < KT; ++i) vp[i].read(vc + code_base[i], vs + scale_base[i], code_at, scale_at);
+    for (int i = 0; i < KT; ++i) vp[i].template read<ONCE>(vc + code_base[i], vs + scale_base[i], code_at, scale_at);
   }
 #pragma unroll 1
   while (at < end) {
@@ -410,7 +464,7 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
     if (at < end) {
       locate();
 #pragma unroll
-      for (int i = 0; i < KT; ++i) kp[i].read(kc + code_base[i], ks + scale_base[i], code_at, scale_at);
+      for (int i = 0; i < KT; ++i) kp[i].template read<ONCE>(kc + code_base[i], ks + scale_base[i], code_at, scale_at);
     }
     if (masked) {
 #pragma unroll
@@ -526,7 +580,7 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
     if (at < end) {
       there_v = there;
 #pragma unroll
-      for (int i = 0; i < KT; ++i) vp[i].read(vc + code_base[i], vs + scale_base[i], code_at, scale_at);
+      for (int i = 0; i < KT; ++i) vp[i].template read<ONCE>(vc + code_base[i], vs + scale_base[i], code_at, scale_at);
     }
   }
 
@@ -536,31 +590,31 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
     z[rt] += __shfl_xor(z[rt], 16);
     z[rt] += __shfl_xor(z[rt], 32);
     if (h == 0) {
-      sm_m[wave][rt * 16 + n] = limit[rt] == -INFINITY ? -INFINITY : off[rt];
-      sm_z[wave][rt * 16 + n] = z[rt];
+      sh.m[wave][rt * 16 + n] = limit[rt] == -INFINITY ? -INFINITY : off[rt];
+      sh.z[wave][rt * 16 + n] = z[rt];
     }
   }
   __syncthreads();
-  const bool whole = tl.parts == 1;
-  const size_t column = (size_t)tile * c.Hkv + kv, slot = (column * p.parts + part) * p.ws_rows;
+  const bool whole = col.count == 1;
+  const size_t slot = col.slot(col.s) * p.ws_rows;
   auto row_sum = [&](int r, float* top) {        // over the waves, of a row
-    float M = sm_m[0][r];
+    float M = sh.m[0][r];
 #pragma unroll
-    for (int w = 1; w < ATT_WAVES; ++w) M = fmaxf(M, sm_m[w][r]);
+    for (int w = 1; w < ATT_WAVES; ++w) M = fmaxf(M, sh.m[w][r]);
     const float ref = M == -INFINITY ? 0.f : M;
     float Z = 0.f;
 #pragma unroll
-    for (int w = 0; w < ATT_WAVES; ++w) Z = fmaf(sm_z[w][r], __builtin_amdgcn_exp2f(sm_m[w][r] - ref), Z);
+    for (int w = 0; w < ATT_WAVES; ++w) Z = fmaf(sh.z[w][r], __builtin_amdgcn_exp2f(sh.m[w][r] - ref), Z);
     *top = M;
     return Z;
   };
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     if (rt * 16 >= tl.n_rows) break;
-    float M = sm_m[0][rt * 16 + n];
+    float M = sh.m[0][rt * 16 + n];
 #pragma unroll
-    for (int w = 1; w < ATT_WAVES; ++w) M = fmaxf(M, sm_m[w][rt * 16 + n]);
-    const float mine = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_m[wave][rt * 16 + n] - M);
+    for (int w = 1; w < ATT_WAVES; ++w) M = fmaxf(M, sh.m[w][rt * 16 + n]);
+    const float mine = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh.m[wave][rt * 16 + n] - M);
 #pragma unroll
     for (int ch = 0; ch < CHUNKS; ++ch) {
 #pragma unroll
@@ -581,7 +635,7 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
 #pragma unroll
           for (int w = 0; w < ATT_WAVES; ++w)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] += reinterpret_cast<const float*>(lds + w * WAVE_BYTES)[r * OSTRIDE + t * 32 + hh * 8 + i];
+            for (int i = 0; i < 8; ++i) x[i] += reinterpret_cast<const float*>(sh.wave[w])[r * OSTRIDE + t * 32 + hh * 8 + i];
           const int channel = channel_of<D32>(ch * CG + t, hh);
           if (whole) {
             float top;
@@ -615,62 +669,189 @@ __global__ __launch_bounds__(ATT_THREADS) void fp4_attention_kernel(Fp4View c, F
   }
   if (whole) return;
   __syncthreads();
-  fold_parts<T>(c, a, p, tl, pa, column, kv, G, reinterpret_cast<float*>(lds));
+  fold_ranges<T, (int)sizeof sh.wave / 8>(c, a, p, tl, pa, col, kv, G, reinterpret_cast<float2*>(sh.wave[0]));
 }
 
-constexpr int ATT_PART_STEP = 256;         // rows of a part: a multiple of what the four waves take in a turn
-constexpr long long ATT_WORKGROUPS = 1024;
+// Several tokens of a request, and calls that are not cut: a workgroup per part of a column.
+template <typename T, int D32, int RT, int KT, bool ONCE>
+__global__ __launch_bounds__(ATT_THREADS) void fp4_attention_parts(Fp4View c, Fp4Attention a, AttPlan p, AttParts pa) {
+  __shared__ AttLds<D32, RT> sh;
+  const int G = a.Hq / c.Hkv, kv = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, part = rest % p.parts, tile = rest / p.parts;
+  AttTile tl;
+  if (!find_tile<16 * RT>(c, a, p, tile, G, &tl)) return;
+  const int parts = min(p.parts, max((tl.seen_max + p.part_rows - 1) / p.part_rows, 1));
+  if (part >= parts) return;
+  const size_t slot = ((size_t)tile * c.Hkv + kv) * p.parts;
+  attend<T, D32, RT, KT, ONCE>(c, a, p, pa, tl, kv, G, part * p.part_rows / 16, part == parts - 1 ? (tl.seen_max + 15) / 16 : (part + 1) * p.part_rows / 16,
+                               AttColumn{part, parts, slot, slot + 1, 1}, sh);
+}
+
+// One token each: the turns of all columns, request by request, are shared out evenly among the workgroups.  A share may end one column, have others whole and begin another, so a workgroup leaves at
+// most two ranges for others to fold: slot 2w what it begins with, 2w + 1 what it ends with.
+// SHARES_PER_UNIT: workgroups that a compute unit holds, four waves to each, by the registers that a variant is given.
+constexpr int SHARE_MOST_REQUESTS = 1024;
+constexpr int COLUMN_TURNS = 1;
+template <typename T, int D32>
+constexpr int SHARES_PER_UNIT = is_f32(T()) ? (D32 <= 2 ? 3 : D32 <= 5 ? 2 : 1) : D32 <= 4 ? 3 : 2;
+template <typename T, int D32, int KT, bool ONCE>
+__global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_attention_shares(Fp4View c, Fp4Attention a, AttPlan p, AttParts pa) {
+  constexpr int TURN = ATT_WAVES * KT * 16, PER = SHARE_MOST_REQUESTS / ATT_THREADS;
+  __shared__ AttLds<D32, 1> sh;
+  __shared__ int held[SHARE_MOST_REQUESTS];
+  __shared__ int wave_turns[ATT_WAVES], begin_before, begin_inst;
+  const int G = a.Hq / c.Hkv, tid = threadIdx.x, lane = tid & 63, columns = c.Hkv * p.tiles_per;
+  const auto turns_of = [](int rows) { return max((rows + TURN - 1) / TURN, 1) + COLUMN_TURNS; };
+  int mine = 0;                          // (the launch sees to it that the sum of all is one)
+  const int per = (a.n + ATT_THREADS - 1) / ATT_THREADS;
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int i = tid * per + x;
+    if (x < per && i < a.n) {
+      held[i] = rows_held(c, a, a.rows[i]);
+      mine += turns_of(held[i]) * columns;
+    }
+  }
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int y = __shfl_up(upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 63) wave_turns[tid >> 6] = upto;
+  __syncthreads();
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < ATT_WAVES; ++w) {
+    if (w < tid >> 6) upto += wave_turns[w];
+    all += wave_turns[w];
+  }
+  // shares of q + 1 turns, `more` of them, and of q
+  all = __builtin_amdgcn_readfirstlane(all);
+  const int shares = min((int)gridDim.x, all), w = blockIdx.x, q = all / shares, more = all - q * shares;
+  if (w >= shares) return;
+  int at = w * q + min(w, more);
+  const int stop = at + q + (w < more ? 1 : 0);
+  const auto share_of = [&](int turn) {
+    const int longer = more * (q + 1);
+    return turn < longer ? turn / (q + 1) : more + (turn - longer) / q;
+  };
+  if (at >= upto - mine && at < upto) {
+    int before = upto - mine, i = tid * per;
+    while (at >= before + turns_of(held[i]) * columns) before += turns_of(held[i++]) * columns;
+    begin_inst = i;
+    begin_before = before;
+  }
+  __syncthreads();
+  int inst = __builtin_amdgcn_readfirstlane(begin_inst), before = __builtin_amdgcn_readfirstlane(begin_before);
+#pragma unroll 1
+  while (at < stop) {
+    const int rows = __builtin_amdgcn_readfirstlane(held[inst]), turns = turns_of(rows);
+    const int column = __builtin_amdgcn_readfirstlane((at - before) / turns), t0 = at - before - column * turns;
+    const int t1 = min(turns, t0 + stop - at), kv = __builtin_amdgcn_readfirstlane(column / p.tiles_per), tile = column - kv * p.tiles_per;
+    AttTile tl;
+    tl.inst = tl.token0 = inst;
+    tl.T = 1;
+    tl.first_row = tile * 16;
+    tl.n_rows = min(G - tl.first_row, 16);
+    tl.held = tl.seen_min = tl.seen_max = rows;
+    if (t1 > COLUMN_TURNS) {
+      const int begin = at - t0, s0 = __builtin_amdgcn_readfirstlane(share_of(begin + COLUMN_TURNS));
+      const int s1 = __builtin_amdgcn_readfirstlane(share_of(begin + turns - 1));
+      attend<T, D32, 1, KT, ONCE>(c, a, p, pa, tl, kv, G, max(t0 - COLUMN_TURNS, 0) * (TURN / 16), min((t1 - COLUMN_TURNS) * (TURN / 16), (rows + 15) / 16),
+                                  AttColumn{w - s0, s1 - s0 + 1, (size_t)2 * s0 + 1, (size_t)2 * (s0 + 1), 2}, sh);
+      __syncthreads();
+    }
+    at += t1 - t0;
+    if (at - before >= turns * columns) {
+      before += turns * columns;
+      ++inst;
+    }
+  }
+}
 
 struct AttLaunch {
   AttPlan plan;
   int row_tiles, key_tiles;              // RT, KT
-  int n_tiles;
-  size_t rows;                           // of all parts, in the workspace
+  bool shares, once;
+  long long workgroups;
+  size_t slots;                          // of the workspace
 };
 
-AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each) {
+template <typename T>
+int shares_per_unit(int d) {
+  switch (d / 32) {
+    case 1: return SHARES_PER_UNIT<T, 1>;
+    case 2: return SHARES_PER_UNIT<T, 2>;
+    case 3: return SHARES_PER_UNIT<T, 3>;
+    case 4: return SHARES_PER_UNIT<T, 4>;
+    case 5: return SHARES_PER_UNIT<T, 5>;
+    case 6: return SHARES_PER_UNIT<T, 6>;
+    case 7: return SHARES_PER_UNIT<T, 7>;
+    default: return SHARES_PER_UNIT<T, 8>;
+  }
+}
+
+AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each, bool cut) {
   const int G = Hq / c.Hkv;
   const long long rows_each = one_each ? G : (n_tokens * G + n - 1) / n;        // score rows of a request, on average
   AttLaunch l;
-  l.row_tiles = rows_each <= 16 || dtype == LAQ_F32 ? 1 : 2;
-  l.key_tiles = l.row_tiles == 1 ? 4 : 2;
-  if (c.d > 128) l.key_tiles = 2;
-  const int TR = 16 * l.row_tiles;
-  l.plan.tiles_per = (G + TR - 1) / TR;
-  l.n_tiles = one_each ? n * l.plan.tiles_per : (int)(n_tokens * G / TR) + n;
-  l.plan.ws_rows = one_each && G < TR ? G : TR;
-  const long long busy = (one_each ? l.n_tiles : n_tokens * G / TR > n ? n_tokens * G / TR : n) * (long long)c.Hkv;
-  long long parts = (ATT_WORKGROUPS + busy - 1) / busy;
-  const long long most = (max_rows + ATT_PART_STEP - 1) / ATT_PART_STEP;
-  if (parts > most) parts = most;
-  // the folding workgroup has two words for every row and part in LDS: what the kernel's other use of it leaves room for
-  const int fold_most = ATT_WAVES * 32 * ((c.d < 128 ? c.d : 128) * 2 + 32) / (8 * TR);
-  if (parts > fold_most) parts = fold_most;
-  const long long steps = (most + parts - 1) / parts;
-  l.plan.part_rows = (int)(steps * ATT_PART_STEP);
-  l.plan.parts = (int)((most + steps - 1) / steps);
-  const int per_block = c.block_rows / 16, turn = ATT_WAVES * l.key_tiles;
-  l.plan.adv_blocks = turn / per_block;
-  l.plan.adv_tiles = turn % per_block;
-  l.rows = l.plan.parts == 1 ? 0 : (size_t)l.n_tiles * c.Hkv * l.plan.parts * l.plan.ws_rows;
+  l.row_tiles = one_each || rows_each <= 16 || dtype == LAQ_F32 ? 1 : 2;
+  l.key_tiles = l.row_tiles == 1 && c.d <= 128 ? 4 : 2;
+  l.once = rows_each <= 16;
+  const int TR = 16 * l.row_tiles, turn = ATT_WAVES * l.key_tiles * 16;
+  l.plan = AttPlan{1, 0x7fffff00, (G + TR - 1) / TR, one_each && G < TR ? G : TR, turn / c.block_rows, turn % c.block_rows / 16};
+  // Columns (as many as are surely there) and the turns of the longest.  As many ranges of a column as make the sum of what they take (a turn 2 us where few
+  // workgroups run) and what folding them takes (0.12 us each) least, as long as that makes no more than two workgroups a compute unit: that many
+  // saturate the memory, and more of them only fold more.  us, bf16, 8 heads of d = 128, with 1, 2, 4, 8, 16, 32, 64 ranges:
+  //   1 x 4096 rows 37, 24, 17, 14, 12;  1 x 65536 503, 259, 136, 76, 43, 29, 28;  4 x 16384 133, 73, 42, 28, 23, 33, 42
+  //   16 x 16384 140, 79, 53, 66, 67, 86, 121;  32 x 4096 41, 31, 40, 48, 59;  64 x 4096 53, 65, 67, 83, 109
+  const long long tiles = one_each ? (long long)n * l.plan.tiles_per : n_tokens * G / TR + n;
+  const long long columns = (one_each ? tiles : n_tokens * G / TR > n ? n_tokens * G / TR : n) * c.Hkv, turns = (max_rows + turn - 1) / turn;
+  long long ranges = 1;
+  while (ranges < turns && ranges * ranges < 16 * turns && (ranges + 1) * columns <= 512) ++ranges;
+  // Long calls of one token each and several requests are shared out evenly.  us, shared out : the best equal parts, requests of that many rows, and of
+  // an eighth of that to that many: 8 x 65536 106 : 97, 73 : 92 (of 8);  16 x 16384 59 : 53, 42 : 51;  32 x 16384 101 : 98, 67 : 89;
+  // 64 x 4096 59 : 53, 41 : 46;  128 x 4096 109 : 101, 68 : 73;  shorter: 8 x 16384 38 : 34, 30 : 32;  8 x 4096 22 : 18, 20 : 16.
+  // (A workgroup's scan of the lengths holds SHARE_MOST_REQUESTS of them; with more there are columns enough.)
+  l.shares = cut && one_each && n > 1 && n <= SHARE_MOST_REQUESTS && turns >= 16 && columns * turns >= 8192;
+  if (l.shares) {
+    l.workgroups = 256 * (dtype == LAQ_BF16 ? shares_per_unit<uint16_t>(c.d) : shares_per_unit<float>(c.d));
+    l.slots = 2 * l.workgroups;
+    return l;
+  }
+  if (cut && ranges > 1) {
+    const long long steps = (turns + ranges - 1) / ranges;
+    l.plan.part_rows = (int)(steps * turn);
+    l.plan.parts = (int)((turns + steps - 1) / steps);
+  }
+  l.workgroups = tiles * c.Hkv * l.plan.parts;
+  l.slots = l.plan.parts > 1 ? l.workgroups : 0;
   return l;
 }
 
 template <typename T, int D32, int RT, int KT>
-hipError_t launch_att(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
-  hipLaunchKernelGGL((fp4_attention_kernel<T, D32, RT, KT>), dim3((unsigned)((long long)l.n_tiles * c.Hkv * l.plan.parts)), dim3(ATT_THREADS), 0, st, c, a,
-                     l.plan, pa);
+hipError_t launch_rt(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
+  const dim3 grid((unsigned)l.workgroups), threads(ATT_THREADS);
+  if constexpr (RT == 1) {
+    if (l.shares) {
+      if (l.once) hipLaunchKernelGGL((fp4_attention_shares<T, D32, KT, true>), grid, threads, 0, st, c, a, l.plan, pa);
+      else hipLaunchKernelGGL((fp4_attention_shares<T, D32, KT, false>), grid, threads, 0, st, c, a, l.plan, pa);
+      return hipGetLastError();
+    }
+    if (l.once) {
+      hipLaunchKernelGGL((fp4_attention_parts<T, D32, RT, KT, true>), grid, threads, 0, st, c, a, l.plan, pa);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((fp4_attention_parts<T, D32, RT, KT, false>), grid, threads, 0, st, c, a, l.plan, pa);
   return hipGetLastError();
 }
 
 template <typename T, int D32>
 hipError_t launch_d(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
-  if constexpr (is_f32(T())) {
-    return launch_att<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, pa, st);
-  } else {
-    if (l.row_tiles == 1) return launch_att<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, pa, st);
-    return launch_att<T, D32, 2, 2>(c, a, l, pa, st);
-  }
+  if constexpr (!is_f32(T()))
+    if (l.row_tiles == 2) return launch_rt<T, D32, 2, 2>(c, a, l, pa, st);
+  return launch_rt<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, pa, st);
 }
 
 template <typename T>
@@ -691,23 +872,28 @@ hipError_t launch_t(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l,
 
 size_t fp4_attention_bytes(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows) {
   // (whether the tokens are one each is not known here: the larger of both)
-  const size_t some = plan_attention(c, Hq, dtype, n, n_tokens, max_rows, false).rows;
-  const size_t one = n_tokens == n ? plan_attention(c, Hq, dtype, n, n_tokens, max_rows, true).rows : 0;
-  return (some > one ? some : one) * (2 * sizeof(unsigned long long) + c.d * sizeof(float));
+  size_t most = 0;
+  for (int one = 0; one <= (n_tokens == n ? 1 : 0); ++one) {
+    const AttLaunch l = plan_attention(c, Hq, dtype, n, n_tokens, max_rows, one, true);
+    const size_t bytes = l.slots * l.plan.ws_rows * (2 * sizeof(unsigned long long) + c.d * sizeof(float));
+    if (bytes > most) most = bytes;
+  }
+  return most;
 }
 
-bool fp4_attention_fits(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each) {
-  const AttLaunch l = plan_attention(c, Hq, dtype, n, n_tokens, max_rows, one_each);
-  return (long long)l.n_tiles * c.Hkv * l.plan.parts < (1ll << 32) / ATT_THREADS;
+bool fp4_attention_fits(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each, bool cut) {
+  return plan_attention(c, Hq, dtype, n, n_tokens, max_rows, one_each, cut).workgroups < (1ll << 32) / ATT_THREADS;
 }
 
-hipError_t launch_fp4_attention(const Fp4View& c, int dtype, const Fp4Attention& a, void* ws, size_t, hipStream_t st) {
-  AttLaunch l = plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, a.start == nullptr);
-  if (!ws) l.plan.parts = 1;
+hipError_t launch_fp4_attention(const Fp4View& c, int dtype, const Fp4Attention& a, void* ws, hipStream_t st) {
   static std::atomic<uint32_t> launches{(uint32_t)(std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull >> 32)};
+  AttLaunch l = plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, a.start == nullptr, ws != nullptr);
+  // (a batch whose turns are more than an int holds is not shared out)
+  if (l.shares && ((int64_t)a.blocks_per_inst * c.block_rows / 128 + 1) * a.n * c.Hkv * l.plan.tiles_per > 0x7fffffff)
+    l = plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, true, false);
   AttParts pa{static_cast<unsigned long long*>(ws), nullptr, 0};
-  if (l.plan.parts > 1) {
-    pa.sums = reinterpret_cast<float*>(pa.marks + 2 * l.rows);
+  if (l.slots) {
+    pa.sums = reinterpret_cast<float*>(pa.marks + 2 * l.slots * l.plan.ws_rows);
     do pa.nonce = launches.fetch_add(1); while (pa.nonce == 0);        // 0 is the cleared mark
   }
   return dtype == LAQ_BF16 ? launch_t<uint16_t>(c, a, l, pa, st) : launch_t<float>(c, a, l, pa, st);
