@@ -43,7 +43,8 @@ typedef struct laq_fp4_cache {
   /*
    * Distances in bytes between blocks, KV heads and rows, of the codes and of the scales; K and V alike.  All six zero: dense as
    * above.  Token-major blocks [block_rows, Hkv, ...]: {block, d / 2, Hkv * d / 2} and {block, d / 32, Hkv * d / 32}.  Those of
-   * the codes are multiples of 16 (as are the codes' addresses), and rows must not overlap (not checked).
+   * the codes are multiples of 16 (as are the codes' addresses); blocks are less than 2^32 apart, rows at most 2^27; rows must not
+   * overlap (not checked).
    */
   int64_t stride_block, stride_head, stride_row;
   int64_t scale_stride_block, scale_stride_head, scale_stride_row;
@@ -67,7 +68,8 @@ typedef struct laq_fp4_cache {
  * take what they need from the top, in their order: dropping what was just appended restores the list.  A request is refused, its rows
  * left as they were, if it would need more than blocks_per_inst blocks, or if it needs blocks and those that it and the requests
  * before it need are more than there are.  Lengths outside of the table count as its nearest end, and state[0] as 0 .. n_blocks.
- * block_rows a multiple of 16, n_blocks * block_rows and blocks_per_inst * block_rows below 2^31.
+ * block_rows a multiple of 16, n_blocks * block_rows and blocks_per_inst * block_rows below 2^31; n * blocks_per_inst too
+ * (LAQ_ERR_UNSUPPORTED).
  */
 int laq_block_map(int32_t n, int32_t block_rows, int32_t n_blocks, int32_t blocks_per_inst, const int32_t *add, int32_t *rows,
                   int32_t *block_table, int32_t *free_blocks, int32_t *state, int32_t *start, int32_t *slots, int64_t n_slots,

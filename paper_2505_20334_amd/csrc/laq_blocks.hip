@@ -43,19 +43,22 @@ __device__ __forceinline__ Request request(const MapArgs& a, int rows, int add) 
   return r;
 }
 
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ long long wave_sums(long long x, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const long long y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
+// Sums that stay at the largest number.
+__device__ __forceinline__ uint32_t add_most(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
+// Inclusive sum over the lanes of a wave: within 16 lanes by shifts of 1, 2, 4, 8, then from the last lane of 16 and of 32 to the lanes behind (by
+// lane exchanges through the LDS three of these took 2 us).
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
+  x = add_most(x, __builtin_amdgcn_update_dpp(0u, x, 0x111, 0xf, 0xf, false));
+  x = add_most(x, __builtin_amdgcn_update_dpp(0u, x, 0x112, 0xf, 0xf, false));
+  x = add_most(x, __builtin_amdgcn_update_dpp(0u, x, 0x114, 0xf, 0xf, false));
+  x = add_most(x, __builtin_amdgcn_update_dpp(0u, x, 0x118, 0xf, 0xf, false));
+  x = add_most(x, __builtin_amdgcn_update_dpp(0u, x, 0x142, 0xa, 0xf, false));
+  return add_most(x, __builtin_amdgcn_update_dpp(0u, x, 0x143, 0xc, 0xf, false));
 }
 
 // The thread whose requests hold number x of a running sum.
 template <int THREADS>
-__device__ __forceinline__ int holder(const long long* before, long long x) {
+__device__ __forceinline__ int holder(const uint32_t* before, uint32_t x) {
   int lo = 0;
 #pragma unroll
   for (int step = THREADS / 2; step > 0; step /= 2)
@@ -66,10 +69,10 @@ __device__ __forceinline__ int holder(const long long* before, long long x) {
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   constexpr int WAVES = THREADS / 64;
-  __shared__ long long more_before[THREADS + 1], need_before[THREADS + 1], back_before[THREADS + 1];
-  __shared__ long long wave_more[WAVES], wave_need[WAVES], wave_back[WAVES];
-  __shared__ long long taken_of[WAVES];
-  __shared__ int refused_of[WAVES], last;
+  __shared__ uint32_t more_before[THREADS], need_before[THREADS], back_before[THREADS];
+  __shared__ uint32_t wave_more[WAVES], wave_need[WAVES], wave_back[WAVES];
+  __shared__ uint32_t taken_most;
+  __shared__ int refused_all, last;
   __shared__ int2 given[THREADS];        // rows and add of all requests, where a thread has one
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i0 = (int)min((long long)tid * a.per, (long long)a.n), i1 = (int)min((long long)i0 + a.per, (long long)a.n);
@@ -85,41 +88,48 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
     const int2 x = one ? given[i] : int2{a.rows[i], a.add[i]};
     return request(a, x.x, x.y);
   };
-  long long more = 0, need = 0, back = 0;
+  // (blocks are entries of the table: their sums are ints; rows appended beyond 2^32 - 1 have no slots and no start of their own)
+  uint32_t more = 0, need = 0, back = 0;
   for (int i = i0; i < i1; ++i) {
     const Request r = own(i);
-    more += r.more;
+    more = add_most(more, r.more);
     need += r.need;
     back += r.back;
   }
-  const long long more_in = wave_sums(more, lane), need_in = wave_sums(need, lane), back_in = wave_sums(back, lane);
+  uint32_t more0 = wave_sums(more), need0 = wave_sums(need), back0 = wave_sums(back);
   if (lane == 63) {
-    wave_more[wave] = more_in;
-    wave_need[wave] = need_in;
-    wave_back[wave] = back_in;
+    wave_more[wave] = more0;
+    wave_need[wave] = need0;
+    wave_back[wave] = back0;
+  }
+  if (tid == 0) {
+    taken_most = 0;
+    refused_all = 0;
   }
   __syncthreads();
-  long long more0 = 0, need0 = 0, back0 = 0, all_back = 0, all_more = 0;
+  // of the threads before this one
+  more0 = __builtin_amdgcn_update_dpp(0u, more0, 0x138, 0xf, 0xf, false);     // (from the lane before: a sum that stays at its most has no difference)
+  need0 -= need;
+  back0 -= back;
+  uint32_t all_back = 0, all_more = 0;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) {
     if (w < wave) {
-      more0 += wave_more[w];
+      more0 = add_most(more0, wave_more[w]);
       need0 += wave_need[w];
       back0 += wave_back[w];
     }
     all_back += wave_back[w];
-    all_more += wave_more[w];
+    all_more = add_most(all_more, wave_more[w]);
   }
-  more0 += more_in - more;               // of the threads before this one
-  need0 += need_in - need;
-  back0 += back_in - back;
   more_before[tid] = more0;
   need_before[tid] = need0;
   back_before[tid] = back0;
 
-  const long long count = min(max(held, 0), a.n_blocks), there = count + all_back;
+  const uint32_t count = (uint32_t)min(max(held, 0), a.n_blocks);
+  const long long there = (long long)count + all_back;
   // blocks taken: up to the last request that gets its own
-  long long upto = need0, taken = 0;
+  uint32_t upto = need0, taken = 0;
   int refused = 0;
   for (int i = i0; i < i1; ++i) {
     const Request r = own(i);
@@ -127,28 +137,17 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
     if (r.need > 0 && upto <= there) taken = upto;
     if (r.wide || (r.need > 0 && upto > there)) ++refused;
   }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    taken = max(taken, __shfl_xor(taken, o));
-    refused += __shfl_xor(refused, o);
-  }
-  if (lane == 0) {
-    taken_of[wave] = taken;
-    refused_of[wave] = refused;
-  }
+  if (taken) atomicMax(&taken_most, taken);
+  if (refused) atomicAdd(&refused_all, refused);
   __syncthreads();
-  refused = 0;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    taken = max(taken, taken_of[w]);
-    refused += refused_of[w];
-  }
+  taken = taken_most;
+  refused = refused_all;
 
   // the block that comes back as number r (the last request's last one is number 0)
-  auto given_back = [&](long long r) {
-    const long long x = all_back - 1 - r;
+  auto given_back = [&](uint32_t r) {
+    const uint32_t x = all_back - 1 - r;
     const int t = holder<THREADS>(back_before, x);
-    long long at = back_before[t];
+    uint32_t at = back_before[t];
     for (int i = t * a.per;; ++i) {
       const Request q = any(i);
       if (x < at + q.back) return a.table[(size_t)i * a.width + q.want + (x - at)];
@@ -156,9 +155,9 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
     }
   };
   // the block that is taken as number k
-  auto block = [&](long long k) {
+  auto block = [&](uint32_t k) {
     const long long p = there - 1 - k;
-    return p < count ? a.list[p] : given_back(p - count);
+    return p < count ? a.list[p] : given_back((uint32_t)(p - count));
   };
 
   const long long first = (long long)blockIdx.x * THREADS + tid, step = (long long)gridDim.x * THREADS;
@@ -166,8 +165,9 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   for (long long s0 = first * 4; s0 < a.n_slots; s0 += step * 4) {
     int slot[4] = {-1, -1, -1, -1};
     if (s0 < all_more) {
-      const int t = holder<THREADS>(more_before, s0);
-      long long at = more_before[t], k = need_before[t];
+      const int t = holder<THREADS>(more_before, (uint32_t)s0);
+      long long at = more_before[t];
+      uint32_t k = need_before[t];
       int i = t * a.per, known = -1, number = -1;
       Request r = any(i);
 #pragma unroll
@@ -195,9 +195,10 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
       for (int x = 0; x < 4 && s0 + x < a.n_slots; ++x) a.slots[s0 + x] = slot[x];
     }
   }
-  for (long long k = first; k < taken; k += step) {
+  for (long long x = first; x < taken; x += step) {
+    const uint32_t k = (uint32_t)x;
     const int t = holder<THREADS>(need_before, k);
-    long long at = need_before[t];
+    uint32_t at = need_before[t];
     for (int i = t * a.per;; ++i) {
       const Request r = any(i);
       if (k < at + r.need) {
@@ -207,14 +208,14 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
       at += r.need;
     }
   }
-  for (long long r = first; r < all_back - taken && count + r < a.n_blocks; r += step) a.list[count + r] = given_back(r);
+  for (long long r = first; r < (long long)all_back - taken && count + r < a.n_blocks; r += step) a.list[count + r] = given_back((uint32_t)r);
   if (a.start && blockIdx.x == 0) {
-    long long at = more0;
+    uint32_t at = more0;
     for (int i = i0; i < i1; ++i) {
-      a.start[i] = (int)min(at, 0x7fffffffll);
-      at += own(i).more;
+      a.start[i] = (int)min(at, 0x7fffffffu);
+      at = add_most(at, own(i).more);
     }
-    if (tid == 0) a.start[a.n] = (int)min(all_more, 0x7fffffffll);
+    if (tid == 0) a.start[a.n] = (int)min(all_more, 0x7fffffffu);
   }
 
   if (gridDim.x > 1) {
@@ -236,18 +237,22 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   }
 }
 
-// A thread has four slots, or as many blocks of a batch that is admitted or released, up to a workgroup per compute unit.
-constexpr int MAP_MOST_WORKGROUPS = 256;
+// Workgroups: a thread has two times four slots, or, where there are no slots (rows are dropped), may have two blocks of a pool of more than 4096.  They cost
+// a count in memory at the end, 0.7 us for two of them, 1.5 for 128.  294000 slots of 256 requests, 9200 blocks, appended and dropped, with 1, 8, 32, 64, 128
+// and 256 workgroups: 512, 80, 29, 21.6, 19.2, 22 us; 32 requests of 8 slots each 11.5, 12.9, 12.9, 12.7, 14.4, 18.3.
+constexpr int MAP_MOST_WORKGROUPS = 128;
 
 }  // namespace
 
 hipError_t launch_block_map(int n, int block_rows, int n_blocks, int width, const int32_t* add, int32_t* rows, int32_t* table, int32_t* list,
                             int32_t* state, int32_t* start, int32_t* slots, int64_t n_slots, hipStream_t st) {
-  const int threads = n <= 1024 ? 256 : 1024;
+  const int64_t work = n_slots ? n_slots / 4 : n_blocks > 4096 ? n_blocks : 1, wanted = (work + 511) / 512;
+  // (many workgroups are a quarter as many of 1024 threads: the count at the end takes less)
+  const int threads = n <= 256 && wanted < 16 ? 256 : 1024;
   const int shift = (block_rows & (block_rows - 1)) == 0 ? __builtin_ctz(block_rows) : -1;
   const MapArgs a{n, block_rows, n_blocks, width, (n + threads - 1) / threads, shift, add, rows, table, list, state, start, slots, n_slots};
-  const int64_t work = n_slots > n_blocks / 4 ? n_slots : n_blocks / 4, wanted = (work + 1023) / 1024;
-  const dim3 grid((unsigned)(wanted < 1 ? 1 : wanted > MAP_MOST_WORKGROUPS ? MAP_MOST_WORKGROUPS : wanted));
+  const int64_t groups = threads == 256 ? wanted : (wanted + 3) / 4;
+  const dim3 grid((unsigned)(groups < 1 ? 1 : groups > MAP_MOST_WORKGROUPS ? MAP_MOST_WORKGROUPS : groups));
   if (threads == 256) hipLaunchKernelGGL(block_map_kernel<256>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(block_map_kernel<1024>, grid, dim3(1024), 0, st, a);
   return hipGetLastError();

@@ -33,6 +33,7 @@ int fp4_view(const laq_fp4_cache* cache, bool need_k, bool need_v, Fp4View* view
   } else if (zeros) {
     return LAQ_ERR_INVALID;
   }
+  if (view->block > 0xffffffffLL || view->scale_block > 0xffffffffLL) return LAQ_ERR_INVALID;
   if (view->row > (1 << 27) || view->scale_row > (1 << 27)) return LAQ_ERR_INVALID;      // (16 rows are addressed with 32 bits)
   if (view->row < c.d / 2 || view->scale_row < c.d / 32 || (view->block | view->head | view->row) % 16) return LAQ_ERR_INVALID;
   return LAQ_OK;
@@ -58,6 +59,7 @@ static int block_map_impl(int32_t n, int32_t block_rows, int32_t n_blocks, int32
                           int32_t* list, int32_t* state, int32_t* start, int32_t* slots, int64_t n_slots, hipStream_t st) {
   if (n < 1 || block_rows < 16 || block_rows % 16 || n_blocks < 1 || width < 1 || n_slots < 0) return LAQ_ERR_INVALID;
   if ((int64_t)n_blocks * block_rows > MOST_ROWS || (int64_t)width * block_rows > MOST_ROWS || n_slots > MOST_ROWS) return LAQ_ERR_INVALID;
+  if ((int64_t)n * width > MOST_ROWS) return LAQ_ERR_UNSUPPORTED;
   if (!add || !rows || !table || !list || !state || (!slots && n_slots)) return LAQ_ERR_INVALID;
   return done(launch_block_map(n, block_rows, n_blocks, width, add, rows, table, list, state, start, slots, n_slots, st));
 }

@@ -159,7 +159,7 @@ template <typename T> constexpr int PARTS_OF = is_f32(T()) ? 3 : 1;
 
 template <typename T, int D32, int RT>
 __device__ __forceinline__ void read_queries(const Fp4Attention& a, const AttTile& tl, int kv, int G, int lane, u32x4 (&q)[RT][D32][PARTS_OF<T>],
-                                             float (&factor)[RT]) {
+                                             float (&factor)[is_f32(T()) ? RT : 1]) {
   const int n = lane & 15, h = lane >> 4;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -167,7 +167,6 @@ __device__ __forceinline__ void read_queries(const Fp4Attention& a, const AttTil
     const bool there = r < tl.n_rows;
     const int t = row / G, g = row - t * G;
     const T* src = static_cast<const T*>(a.q) + (int64_t)(tl.token0 + (there ? t : 0)) * a.stride_token + (int64_t)(kv * G + (there ? g : 0)) * a.stride_head;
-    factor[rt] = fmaxf(a.scale2, 0x1p-126f);           // (not 0: a masked product is -infinity)
     if constexpr (is_f32(T())) {
       u32x4 x[D32][2];
       uint32_t most = 0;
@@ -185,7 +184,7 @@ __device__ __forceinline__ void read_queries(const Fp4Attention& a, const AttTil
       // the largest of the row to 2^-20 .. 2^-19 (from 2^40 on: times 2^-60, so that the factor stays a number): no part is too small for bf16, no sum of
       // products overflows before the logit does
       const int e = (int)(most >> 23), shift = most >= 0x7f800000u || most == 0 ? 0 : max(107 - e, -60);
-      factor[rt] = fmaxf(ldexpf(a.scale2, -shift), 0x1p-126f);
+      factor[rt] = fmaxf(ldexpf(a.scale2, -shift), 0x1p-126f);           // (not 0, as below)
 #pragma unroll
       for (int g8 = 0; g8 < D32; ++g8) {
 #pragma unroll
@@ -328,7 +327,7 @@ __device__ void fold_ranges(const Fp4View& c, const Fp4Attention& a, const AttPl
 #pragma unroll
       for (int u = 0; u < EU; ++u) {
         if (e0 + u * ATT_THREADS >= R * pairs) break;
-        const float vx = Z[u] == 0.f ? 0.f : x[u] / Z[u], vy = Z[u] == 0.f ? 0.f : y[u] / Z[u];
+        const float part_of = Z[u] == 0.f ? 0.f : 1.f / Z[u], vx = x[u] * part_of, vy = y[u] * part_of;
         const size_t to = out_row(a, tl, kv, G, row[u]);
         if constexpr (is_f32(T())) *reinterpret_cast<float2*>(static_cast<T*>(a.out) + to * c.d + ch[u]) = float2{vx, vy};
         else *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + to * c.d + ch[u]) = pack2(vx, vy);
@@ -346,6 +345,22 @@ __device__ void fold_ranges(const Fp4View& c, const Fp4Attention& a, const AttPl
   }
 }
 
+// A call's arguments.  Kernels read them where they are needed, from the launch's own argument memory through the scalar cache: kept in registers from their first
+// use to their last, they and what a step computes are more than the 102 scalar registers hold, and a step then fetches spilled ones back one instruction each.
+struct AttCall {
+  Fp4View c;
+  Fp4Attention a;
+  AttPlan p;
+  AttParts pa;
+};
+typedef __attribute__((address_space(4))) const AttCall* AttCallPtr;
+__device__ __forceinline__ AttCallPtr att_call() { return (AttCallPtr)__builtin_amdgcn_kernarg_segment_ptr(); }
+// The same, to be read anew.
+__device__ __forceinline__ const AttCall& anew(AttCallPtr call) {
+  asm volatile("" : "+s"(call));
+  return *(const AttCall*)call;
+}
+
 template <int D32, int RT>
 struct AttLds {
   static constexpr int CG = D32 < 4 ? D32 : 4, CHUNKS = (D32 + 3) / 4;        // groups of a chunk of V's channels (32 columns each), chunks
@@ -357,19 +372,29 @@ struct AttLds {
   float m[ATT_WAVES][16 * RT], z[ATT_WAVES][16 * RT];
 };
 
-// The key tiles first .. end - 1 of a column.
-template <typename T, int D32, int RT, int KT, bool ONCE>
-__device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, const AttPlan& p, const AttParts& pa, const AttTile& tl, int kv, int G,
-                                       int first, int end, const AttColumn& col, AttLds<D32, RT>& sh) {
+// The key tiles first .. end - 1 of a column.  EARLY_V: the next step's rows of V are asked for as soon as this step's are in LDS, not after their
+// products: 256 requests x 1024 rows 54.5 : 53.5 us, 64 of 2048 to 100 24.2 : 22.8; but where all places are taken for long 102 : 108 (96 x 6144).
+template <typename T, int D32, int RT, int KT, bool ONCE, bool EARLY_V>
+__device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int kv, int G, int first, int end, const AttColumn& col, AttLds<D32, RT>& sh) {
+  const AttCall& k = anew(call);
+  const Fp4View& c = k.c;
+  const Fp4Attention& a = k.a;
+  const AttPlan& p = k.p;
   using Lds = AttLds<D32, RT>;
   constexpr int NP = PARTS_OF<T>, CG = Lds::CG, CHUNKS = Lds::CHUNKS, STRIDE = Lds::STRIDE, OSTRIDE = Lds::OSTRIDE;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, h = lane >> 4;
   u32x4 q[RT][D32][NP];
-  float factor[RT];
-  read_queries<T, D32, RT>(a, tl, kv, G, lane, q, factor);
-  int seen[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) seen[rt] = rows_seen(tl, tl.first_row + min(rt * 16 + n, tl.n_rows - 1), G);
+  // the factor of the products: of all rows, but where rows are brought to a magnitude (fp32)
+  float row_factor[is_f32(T()) ? RT : 1];
+  read_queries<T, D32, RT>(a, tl, kv, G, lane, q, row_factor);
+  const float factor_of_all = fmaxf(a.scale2, 0x1p-126f);        // (not 0: a masked product is -infinity)
+  auto factor = [&](int rt) {
+    if constexpr (is_f32(T())) return row_factor[rt];
+    else return factor_of_all;
+  };
+
+  // rows of the cache that row n of tile rt sees (few steps ask)
+  auto row_sees = [&](int rt) { return rows_seen(tl, tl.first_row + min(rt * 16 + n, tl.n_rows - 1), G); };
 
   // this wave's position: key tile `at`, in block `block` of the request its tile `in_block`
   const int per_block = c.block_rows / 16;
@@ -382,28 +407,52 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
   KeyPiece<D32> kp[KT], vp[KT];
   int64_t code_base[KT], scale_base[KT];
   uint32_t there = 0, there_v = 0;       // a bit for each tile of the step whose rows are there
-  auto locate = [&] {                    // the tiles of the step at `at`: one look at the table for those of a block
-    int b = block, r = in_block;
-    bool good = false;
-    there = 0;
+  // Block numbers are asked for a step ahead, so that their way does not lie in front of the codes'.  (Addresses of products of 32 bits: what is scalar in a step
+  // takes a third of its instructions.)
+  int number[KT];
+  const int last_block = max((tl.held + c.block_rows - 1) / c.block_rows - 1, 0);
+  const bool straddles = per_block % KT != 0;              // a step's tiles may lie in several blocks
+  const uint32_t tile_codes = (uint32_t)c.row * 16, tile_scales = (uint32_t)c.scale_row * 16;
+  auto ask = [&](int b, int r) {
+    number[0] = table[min(b, last_block)];
+    if (straddles) {
 #pragma unroll
-    for (int i = 0; i < KT; ++i) {
-      if (i == 0 || r == 0) {
-        int number = -1;
-        if (at + i < end) number = table[b];
-        good = number >= 0 && number < c.n_blocks;
-        const int64_t num = good ? number : 0, row = good ? r * 16 : 0;
-        code_base[i] = num * c.block + row * c.row;
-        scale_base[i] = num * c.scale_block + row * c.scale_row;
-      } else {
-        code_base[i] = code_base[i - 1] + (good ? 16 * c.row : 0);
-        scale_base[i] = scale_base[i - 1] + (good ? 16 * c.scale_row : 0);
+      for (int i = 1; i < KT; ++i) {
+        if (++r == per_block) {
+          r = 0;
+          ++b;
+        }
+        number[i] = table[min(b, last_block)];
       }
-      there |= good && at + i < end ? 1u << i : 0u;
-      if (++r == per_block) {
-        r = 0;
-        ++b;
+    }
+  };
+  auto locate = [&] {                    // the tiles of the step at `at`, whose block numbers have been asked for
+    // (tiles beyond the end are those of the last block: read, and not there)
+    auto place = [&](int i, int r) {
+      const bool good = (uint32_t)number[i] < (uint32_t)c.n_blocks;
+      const uint32_t num = good ? number[i] : 0;
+      code_base[i] = (uint64_t)num * (uint32_t)c.block + (uint64_t)(uint32_t)r * tile_codes;
+      scale_base[i] = (uint64_t)num * (uint32_t)c.scale_block + (uint64_t)(uint32_t)r * tile_scales;
+      return good;
+    };
+    const int left = min(end - at, KT);  // tiles
+    const bool good = place(0, in_block);
+    if (straddles) {
+      there = good;
+      int r = in_block;
+#pragma unroll
+      for (int i = 1; i < KT; ++i) {
+        if (++r == per_block) r = 0;
+        there |= (uint32_t)place(i, r) << i;
       }
+      there &= (1u << left) - 1;
+    } else {
+#pragma unroll
+      for (int i = 1; i < KT; ++i) {
+        code_base[i] = code_base[0] + i * tile_codes;
+        scale_base[i] = scale_base[0] + i * tile_scales;
+      }
+      there = good ? (1u << left) - 1 : 0u;
     }
   };
   auto advance = [&] {
@@ -414,6 +463,14 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
       in_block -= per_block;
       ++block;
     }
+  };
+  auto ask_next = [&] {                  // for the step after that at `at`
+    int b = block + p.adv_blocks, r = in_block + p.adv_tiles;
+    if (r >= per_block) {
+      r -= per_block;
+      ++b;
+    }
+    ask(b, r);
   };
 
   // of row n of each tile: the exponents' reference, the product from which on it is moved (LEEWAY beyond it: weights of up to 2^8 cost
@@ -430,12 +487,16 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
     for (int i = 0; i < CHUNKS * CG * 2; ++i) acc[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   unsigned char* const my_lds = sh.wave[wave];
-  unsigned char* const v_write = my_lds + n * STRIDE + h * 16;
-  const uint32_t v_read = (uint32_t)(4 * h + n / 4) * STRIDE + (n & 3) * 8;
+  // Rows of V are an odd number of 32 bytes apart, and rows 4 .. 7 of 8 have the halves of every 32 bytes changed: the reads (4 rows of 32 bytes by 16 lanes,
+  // over 64 banks) and the writes (8 rows of 16 bytes at a time, over 32) then meet in no bank; without the change a write takes 16 cycles instead of 8.
+  unsigned char* const v_write = my_lds + n * STRIDE + (h ^ (n >> 2 & 1)) * 16;
+  const uint32_t v_read = (uint32_t)(4 * h + n / 4) * STRIDE + ((n & 3) * 8 ^ (h & 1) * 16);
   typedef __attribute__((address_space(3))) s16x4* LdsQuad;
 
   if (at < end) {
+    ask(block, in_block);
     locate();
+    ask_next();
     there_v = there;
 #pragma unroll
     for (int i = 0; i < KT; ++i) kp[i].template read<ONCE>(kc + code_base[i], ks + scale_base[i], code_at, scale_at);
@@ -463,17 +524,20 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
     advance();
     if (at < end) {
       locate();
+      ask_next();
 #pragma unroll
       for (int i = 0; i < KT; ++i) kp[i].template read<ONCE>(kc + code_base[i], ks + scale_base[i], code_at, scale_at);
     }
     if (masked) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < RT; ++rt) {
+        const int seen = row_sees(rt);
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (!(there_v >> i & 1) || key0 + i * 16 + 4 * h + r >= seen[rt]) s[rt][i][r] = -INFINITY;
+            if (!(there_v >> i & 1) || key0 + i * 16 + 4 * h + r >= seen) s[rt][i][r] = -INFINITY;
+      }
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -486,9 +550,9 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         if (top > limit[rt]) {
-          const float moved = top * factor[rt], w = limit[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[rt] - moved);
+          const float moved = top * factor(rt), w = limit[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[rt] - moved);
           off[rt] = moved;
-          limit[rt] = (moved + LEEWAY) / factor[rt];
+          limit[rt] = (moved + LEEWAY) / factor(rt);
           z[rt] *= w;
 #pragma unroll
           for (int i = 0; i < CHUNKS * CG * 2; ++i)
@@ -500,7 +564,7 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
       for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[rt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[rt][i][r], factor[rt], -off[rt]));
+          s[rt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[rt][i][r], factor(rt), -off[rt]));
           z[rt] += s[rt][i][r];
         }
     }
@@ -542,6 +606,10 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
         // (LDS operations of a wave are done in their order: only the compiler has to keep it)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         stage(ch, false);
+        if (EARLY_V && ch == CHUNKS - 1 && at < end) {
+#pragma unroll
+          for (int i = j; i < j + 2; ++i) vp[i].template read<ONCE>(vc + code_base[i], vs + scale_base[i], code_at, scale_at);
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int ct = 0; ct < CG * 2; ++ct) {
@@ -559,11 +627,12 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
             u32x4 sees;
+            const int seen = row_sees(rt);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int tile_of = j + x / 2, key = key0 + tile_of * 16 + 4 * h + (x & 1) * 2;
               const bool in = there_v >> tile_of & 1;
-              sees[x] = (in && key < seen[rt] ? 0x3f80u : 0u) | (in && key + 1 < seen[rt] ? 0x3f800000u : 0u);
+              sees[x] = (in && key < seen ? 0x3f80u : 0u) | (in && key + 1 < seen ? 0x3f800000u : 0u);
             }
 #pragma unroll
             for (int ct = 0; ct < CG * 2; ++ct) {
@@ -577,11 +646,11 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
         }
       }
     }
-    if (at < end) {
-      there_v = there;
+    if (!EARLY_V && at < end) {
 #pragma unroll
       for (int i = 0; i < KT; ++i) vp[i].template read<ONCE>(vc + code_base[i], vs + scale_base[i], code_at, scale_at);
     }
+    there_v = there;
   }
 
   // fold the waves, 16 rows and a chunk of channels at a time
@@ -595,8 +664,9 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
     }
   }
   __syncthreads();
+  const AttCall& e = anew(call);
   const bool whole = col.count == 1;
-  const size_t slot = col.slot(col.s) * p.ws_rows;
+  const size_t slot = col.slot(col.s) * e.p.ws_rows;
   auto row_sum = [&](int r, float* top) {        // over the waves, of a row
     float M = sh.m[0][r];
 #pragma unroll
@@ -626,8 +696,8 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
           *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(my_lds) + n * OSTRIDE + ct * 16 + 4 * h) = x;
         }
       __syncthreads();
-      for (int e = threadIdx.x; e < 16 * CG * 4; e += ATT_THREADS) {       // eight columns of a row: group t, quarter hh
-        const int r = e / (CG * 4), t = e % (CG * 4) / 4, hh = e & 3, row = rt * 16 + r;
+      for (int x8 = threadIdx.x; x8 < 16 * CG * 4; x8 += ATT_THREADS) {       // eight columns of a row: group t, quarter hh
+        const int r = x8 / (CG * 4), t = x8 % (CG * 4) / 4, hh = x8 & 3, row = rt * 16 + r;
         if (row < tl.n_rows && ch * CG + t < D32) {
           float x[8];
 #pragma unroll
@@ -639,13 +709,13 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
           const int channel = channel_of<D32>(ch * CG + t, hh);
           if (whole) {
             float top;
-            const float Z = row_sum(row, &top);
+            const float Z = row_sum(row, &top), part_of = Z == 0.f ? 0.f : 1.f / Z;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = Z == 0.f ? 0.f : x[i] / Z;
-            put8(static_cast<T*>(a.out) + out_row(a, tl, kv, G, row) * c.d + channel, x);
+            for (int i = 0; i < 8; ++i) x[i] *= part_of;
+            put8(static_cast<T*>(e.a.out) + out_row(e.a, tl, kv, G, row) * e.c.d + channel, x);
           } else {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) store_pair(pa.sums + (slot + row) * c.d + channel + i, __float_as_uint(x[i]), __float_as_uint(x[i + 1]));
+            for (int i = 0; i < 8; i += 2) store_pair(e.pa.sums + (slot + row) * e.c.d + channel + i, __float_as_uint(x[i]), __float_as_uint(x[i + 1]));
           }
         }
       }
@@ -660,29 +730,34 @@ __device__ __forceinline__ void attend(const Fp4View& c, const Fp4Attention& a, 
     float top;
     const float Z = row_sum(row, &top);
     if (!whole) {
-      store_pair(pa.marks + (slot + row) * 2, pa.nonce, __float_as_uint(top));
-      store_pair(pa.marks + (slot + row) * 2 + 1, pa.nonce, __float_as_uint(Z));
+      store_pair(e.pa.marks + (slot + row) * 2, e.pa.nonce, __float_as_uint(top));
+      store_pair(e.pa.marks + (slot + row) * 2 + 1, e.pa.nonce, __float_as_uint(Z));
       stores_done();
-    } else if (a.lse) {
-      a.lse[out_row(a, tl, kv, G, row)] = Z == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(Z)) * LN2;
+    } else if (e.a.lse) {
+      e.a.lse[out_row(e.a, tl, kv, G, row)] = Z == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(Z)) * LN2;
     }
   }
   if (whole) return;
   __syncthreads();
-  fold_ranges<T, (int)sizeof sh.wave / 8>(c, a, p, tl, pa, col, kv, G, reinterpret_cast<float2*>(sh.wave[0]));
+  fold_ranges<T, (int)sizeof sh.wave / 8>(e.c, e.a, e.p, tl, e.pa, col, kv, G, reinterpret_cast<float2*>(sh.wave[0]));
 }
 
 // Several tokens of a request, and calls that are not cut: a workgroup per part of a column.
 template <typename T, int D32, int RT, int KT, bool ONCE>
-__global__ __launch_bounds__(ATT_THREADS) void fp4_attention_parts(Fp4View c, Fp4Attention a, AttPlan p, AttParts pa) {
+__global__ __launch_bounds__(ATT_THREADS, (RT == 3 ? 2 : 1)) void fp4_attention_parts(AttCall) {
   __shared__ AttLds<D32, RT> sh;
+  const AttCallPtr call = att_call();
+  const AttCall& k = anew(call);
+  const Fp4View& c = k.c;
+  const Fp4Attention& a = k.a;
+  const AttPlan& p = k.p;
   const int G = a.Hq / c.Hkv, kv = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, part = rest % p.parts, tile = rest / p.parts;
   AttTile tl;
   if (!find_tile<16 * RT>(c, a, p, tile, G, &tl)) return;
   const int parts = min(p.parts, max((tl.seen_max + p.part_rows - 1) / p.part_rows, 1));
   if (part >= parts) return;
   const size_t slot = ((size_t)tile * c.Hkv + kv) * p.parts;
-  attend<T, D32, RT, KT, ONCE>(c, a, p, pa, tl, kv, G, part * p.part_rows / 16, part == parts - 1 ? (tl.seen_max + 15) / 16 : (part + 1) * p.part_rows / 16,
+  attend<T, D32, RT, KT, ONCE, true>(call, tl, kv, G, part * p.part_rows / 16, part == parts - 1 ? (tl.seen_max + 15) / 16 : (part + 1) * p.part_rows / 16,
                                AttColumn{part, parts, slot, slot + 1, 1}, sh);
 }
 
@@ -694,12 +769,16 @@ constexpr int COLUMN_TURNS = 1;
 template <typename T, int D32>
 constexpr int SHARES_PER_UNIT = is_f32(T()) ? (D32 <= 2 ? 3 : D32 <= 5 ? 2 : 1) : D32 <= 4 ? 3 : 2;
 template <typename T, int D32, int KT, bool ONCE>
-__global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_attention_shares(Fp4View c, Fp4Attention a, AttPlan p, AttParts pa) {
+__global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_attention_shares(AttCall) {
   constexpr int TURN = ATT_WAVES * KT * 16, PER = SHARE_MOST_REQUESTS / ATT_THREADS;
   __shared__ AttLds<D32, 1> sh;
   __shared__ int held[SHARE_MOST_REQUESTS];
   __shared__ int wave_turns[ATT_WAVES], begin_before, begin_inst;
-  const int G = a.Hq / c.Hkv, tid = threadIdx.x, lane = tid & 63, columns = c.Hkv * p.tiles_per;
+  const AttCallPtr call = att_call();
+  const AttCall& k = anew(call);
+  const Fp4View& c = k.c;
+  const Fp4Attention& a = k.a;
+  const int tiles_per = k.p.tiles_per, G = a.Hq / c.Hkv, tid = threadIdx.x, lane = tid & 63, columns = c.Hkv * tiles_per;
   const auto turns_of = [](int rows) { return max((rows + TURN - 1) / TURN, 1) + COLUMN_TURNS; };
   int mine = 0;                          // (the launch sees to it that the sum of all is one)
   const int per = (a.n + ATT_THREADS - 1) / ATT_THREADS;
@@ -747,7 +826,7 @@ __global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_at
   while (at < stop) {
     const int rows = __builtin_amdgcn_readfirstlane(held[inst]), turns = turns_of(rows);
     const int column = __builtin_amdgcn_readfirstlane((at - before) / turns), t0 = at - before - column * turns;
-    const int t1 = min(turns, t0 + stop - at), kv = __builtin_amdgcn_readfirstlane(column / p.tiles_per), tile = column - kv * p.tiles_per;
+    const int t1 = min(turns, t0 + stop - at), kv = __builtin_amdgcn_readfirstlane(column / tiles_per), tile = column - kv * tiles_per;
     AttTile tl;
     tl.inst = tl.token0 = inst;
     tl.T = 1;
@@ -757,7 +836,7 @@ __global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_at
     if (t1 > COLUMN_TURNS) {
       const int begin = at - t0, s0 = __builtin_amdgcn_readfirstlane(share_of(begin + COLUMN_TURNS));
       const int s1 = __builtin_amdgcn_readfirstlane(share_of(begin + turns - 1));
-      attend<T, D32, 1, KT, ONCE>(c, a, p, pa, tl, kv, G, max(t0 - COLUMN_TURNS, 0) * (TURN / 16), min((t1 - COLUMN_TURNS) * (TURN / 16), (rows + 15) / 16),
+      attend<T, D32, 1, KT, ONCE, false>(call, tl, kv, G, max(t0 - COLUMN_TURNS, 0) * (TURN / 16), min((t1 - COLUMN_TURNS) * (TURN / 16), (rows + 15) / 16),
                                   AttColumn{w - s0, s1 - s0 + 1, (size_t)2 * s0 + 1, (size_t)2 * (s0 + 1), 2}, sh);
       __syncthreads();
     }
@@ -795,7 +874,12 @@ AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_t
   const int G = Hq / c.Hkv;
   const long long rows_each = one_each ? G : (n_tokens * G + n - 1) / n;        // score rows of a request, on average
   AttLaunch l;
-  l.row_tiles = one_each || rows_each <= 16 || dtype == LAQ_F32 ? 1 : 2;
+  // Tiles of 16 score rows of a workgroup.  More share what a step costs that does not depend on them (a third of its instructions with two, of d = 128), but
+  // leave fewer workgroups: three from 192 rows on, with two of these a compute unit, where head sizes leave registers for it and less would not let more
+  // workgroups in.  Two : three, us, 8 KV heads: 4 x 512 tokens x 4 heads over 8704 rows 243 : 211; 2 x 2048 over 8192 576 : 498;  16 x 48 over 2048 43.4 : 33.9,
+  // x 100 69.3 : 63.5, x 24 27.3 : 34.6;  1 x 64 over 8192 33 : 44;  d = 64, 4 x 256 over 8192 117 : 136.
+  const bool three = rows_each >= 192 && c.d > 64 && c.d <= 128 && n_tokens * G / 48 * c.Hkv >= 512;
+  l.row_tiles = one_each || rows_each <= 16 || dtype == LAQ_F32 ? 1 : three ? 3 : 2;
   l.key_tiles = l.row_tiles == 1 && c.d <= 128 ? 4 : 2;
   l.once = rows_each <= 16;
   const int TR = 16 * l.row_tiles, turn = ATT_WAVES * l.key_tiles * 16;
@@ -832,25 +916,30 @@ AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_t
 template <typename T, int D32, int RT, int KT>
 hipError_t launch_rt(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
   const dim3 grid((unsigned)l.workgroups), threads(ATT_THREADS);
+  const AttCall call{c, a, l.plan, pa};
   if constexpr (RT == 1) {
     if (l.shares) {
-      if (l.once) hipLaunchKernelGGL((fp4_attention_shares<T, D32, KT, true>), grid, threads, 0, st, c, a, l.plan, pa);
-      else hipLaunchKernelGGL((fp4_attention_shares<T, D32, KT, false>), grid, threads, 0, st, c, a, l.plan, pa);
+      if (l.once) hipLaunchKernelGGL((fp4_attention_shares<T, D32, KT, true>), grid, threads, 0, st, call);
+      else hipLaunchKernelGGL((fp4_attention_shares<T, D32, KT, false>), grid, threads, 0, st, call);
       return hipGetLastError();
     }
     if (l.once) {
-      hipLaunchKernelGGL((fp4_attention_parts<T, D32, RT, KT, true>), grid, threads, 0, st, c, a, l.plan, pa);
+      hipLaunchKernelGGL((fp4_attention_parts<T, D32, RT, KT, true>), grid, threads, 0, st, call);
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((fp4_attention_parts<T, D32, RT, KT, false>), grid, threads, 0, st, c, a, l.plan, pa);
+  hipLaunchKernelGGL((fp4_attention_parts<T, D32, RT, KT, false>), grid, threads, 0, st, call);
   return hipGetLastError();
 }
 
 template <typename T, int D32>
 hipError_t launch_d(const Fp4View& c, const Fp4Attention& a, const AttLaunch& l, const AttParts& pa, hipStream_t st) {
   if constexpr (!is_f32(T()))
-    if (l.row_tiles == 2) return launch_rt<T, D32, 2, 2>(c, a, l, pa, st);
+    {
+      if constexpr (D32 == 3 || D32 == 4)
+        if (l.row_tiles == 3) return launch_rt<T, D32, 3, 2>(c, a, l, pa, st);
+      if (l.row_tiles == 2) return launch_rt<T, D32, 2, 2>(c, a, l, pa, st);
+    }
   return launch_rt<T, D32, 1, D32 <= 4 ? 4 : 2>(c, a, l, pa, st);
 }
 

@@ -316,6 +316,9 @@ ONE = [  # one token per request: (dtype, Hq, H, d, block, lengths)
     (BF16, 8, 1, 128, 256, [1000, 3]), (BF16, 16, 1, 160, 32, [95, 0, 300]), (BF16, 17, 1, 128, 16, [70]), (BF16, 40, 1, 64, 64, [200, 1]), (BF16, 71, 1, 64, 128, [333]),
     (BF16, 6, 2, 192, 16, [257, 255]), (BF16, 3, 3, 224, 80, [161]), (BF16, 8, 2, 256, 64, [63, 1000]), (BF16, 2, 1, 128, 128, [5000, 17, 1025]),
     (BF16, 8, 8, 128, 16, [300 + 13 * i for i in range(40)]),
+    # shared out: columns that end and begin within a share, one request of most rows, many shares of a column, requests of no rows in between
+    (BF16, 32, 8, 64, 64, [4100, 1, 0, 700, 4096, 33, 0, 2000] * 2), (BF16, 8, 8, 128, 16, [9000] + [5] * 130), (BF16, 16, 16, 96, 16, [6000, 5990, 257, 513] * 2),
+    (F32, 16, 8, 64, 32, [5000, 0, 300, 4999] * 4), (BF16, 40, 8, 256, 64, [4000, 70, 2900, 1] * 2),
     (F32, 4, 4, 32, 16, [3, 40]), (F32, 28, 4, 96, 16, [700, 1]), (F32, 32, 8, 128, 64, [130, 513]), (F32, 17, 1, 64, 32, [99]), (F32, 2, 2, 256, 48, [150, 31]),
     (F32, 8, 2, 192, 16, [64, 65]), (F32, 3, 1, 160, 16, [17]), (F32, 1, 1, 128, 256, [3000]), (F32, 9, 3, 224, 16, [77]),
 ]
@@ -337,6 +340,8 @@ MANY = [  # (dtype, Hq, H, d, block, lengths, tokens)
     (BF16, 5, 1, 160, 16, [100], [50]), (BF16, 16, 4, 64, 64, [1500, 5], [3, 5]), (BF16, 6, 3, 32, 16, [90, 40], [90, 40]),
     (F32, 8, 2, 128, 64, [100, 33, 8], [8, 3, 8]), (F32, 28, 4, 96, 16, [300, 64], [8, 7]), (F32, 4, 2, 256, 32, [90], [40]), (F32, 3, 3, 192, 16, [60], [33]),
     (F32, 2, 1, 64, 16, [250, 30], [100, 30]),
+    # tiles of 48 score rows (as many of them as two workgroups a compute unit), the last ones short
+    (BF16, 64, 16, 128, 16, [300, 110, 200, 97], [100, 110, 93, 97]), (BF16, 28, 14, 96, 64, [260, 400], [250, 131]), (BF16, 56, 8, 128, 48, [130, 90], [95, 90]),
 ]
 
 
@@ -390,27 +395,30 @@ def test_large_logits_scales_and_a_dominant_row(dtype):
         c.check(out, lse, scale=scale or None, what="scale %g" % scale)
 
 
-@pytest.mark.parametrize("tokens", [1, 5])
-def test_a_nan_in_the_cache_reaches_those_that_see_it(tokens):
+@pytest.mark.parametrize("tokens,Hq,H,d", [(1, 4, 2, 64), (5, 4, 2, 64), (30, 4, 2, 64), (30, 8, 2, 160), (50, 128, 32, 128), (3, 4, 2, 256)])
+def test_a_nan_in_the_cache_reaches_those_that_see_it(tokens, Hq, H, d):
     laq = _laq()
-    c = Case(BF16, 4, 2, 64, 16, [50, 60], [tokens, tokens])
-    nan_row = 59 if tokens == 1 else 57                  # of request 1: the last row, or one that the first tokens do not see
+    print("case:", tokens, Hq, H, d, flush=True)
+    c = Case(BF16, Hq, H, d, 16, [50, 60], [tokens, tokens])
+    last, G = H - 1, Hq // H                             # the head that gets it, its queries
+    nan_row = 59 if tokens == 1 else 60 - tokens // 2 - 1      # of request 1: the last row, or one that the first tokens do not see
     slot = int(c.table[1, nan_row // 16]) * 16 + nan_row % 16
-    bad = torch.zeros(1, 2, 64, device=DEV)
-    bad[0, 1, 5] = math.inf
+    bad = torch.zeros(1, H, d, device=DEV)
+    bad[0, last, 5] = math.inf
     laq.laq_fp4_store(c.cache, None, bad, torch.tensor([slot], dtype=torch.int32, device=DEV))
     out, lse = c.run()
     torch.cuda.synchronize()
-    out = out.cpu().view(2, tokens, 4, 64)
+    out = out.cpu().view(2, tokens, Hq, d)
     sees = torch.arange(tokens) + 60 - tokens >= nan_row
-    assert torch.isfinite(out[0]).all() and torch.isfinite(out[1, ~sees]).all() and torch.isfinite(out[1, sees][:, :2]).all()
-    assert torch.isnan(out[1, sees][:, 2:, :32]).all() and torch.isfinite(out[1, sees][:, 2:, 32:]).all() and torch.isfinite(lse).all()
+    assert sees.any() and (tokens == 1 or not sees.all())
+    assert torch.isfinite(out[0]).all() and torch.isfinite(out[1, ~sees]).all() and torch.isfinite(out[1, sees][:, :last * G]).all()
+    assert torch.isnan(out[1, sees][:, last * G:, :32]).all() and torch.isfinite(out[1, sees][:, last * G:, 32:]).all() and torch.isfinite(lse).all()
     # in K: the logit, and with it everything of the head
     laq.laq_fp4_store(c.cache, bad, torch.ones_like(bad), torch.tensor([slot], dtype=torch.int32, device=DEV))
     out, lse = c.run()
     torch.cuda.synchronize()
-    out = out.cpu().view(2, tokens, 4, 64)
-    assert torch.isnan(out[1, sees][:, 2:]).all() and torch.isfinite(out[1, sees][:, :2]).all() and torch.isfinite(out[1, ~sees]).all()
+    out = out.cpu().view(2, tokens, Hq, d)
+    assert torch.isnan(out[1, sees][:, last * G:]).all() and torch.isfinite(out[1, sees][:, :last * G]).all() and torch.isfinite(out[1, ~sees]).all()
 
 
 def test_infinite_and_nan_queries_stay_with_their_own_head():
