@@ -47,55 +47,80 @@ struct AttPlan {
   int32_t adv_blocks, adv_tiles;         // what a turn moves a position (block, key tile in it) by
 };
 
-// Channel of number i of group t of lane quarter h: whole pieces of a row where scale blocks and pieces fit each other, else 8 of each block.
-template <int D32> constexpr bool PIECES = D32 == 1 || D32 == 2 || D32 == 4 || D32 == 8;
-template <int D32> __device__ __forceinline__ int channel_of(int t, int h) { return PIECES<D32> ? h * 8 * D32 + 8 * t : 32 * t + 8 * h; }
+template <int FROM, int TO, typename F>
+__device__ __forceinline__ void for_groups(F&& f) {
+  if constexpr (FROM < TO) {
+    f(std::integral_constant<int, FROM>{});
+    for_groups<FROM + 1, TO>(f);
+  }
+}
 
-// A lane's codes and scales of a key row.
+// A lane of quarter h has the numbers 8 D32 h .. of a row, in D32 groups of eight: one piece of memory.
+template <int D32> __device__ __forceinline__ int channel_of(int t, int h) { return 8 * (h * D32 + t); }
+
+// A lane's codes and scales of a key row.  Group t lies in scale block (h D32 + t) / 4; a quarter touches NS of these, and reads NS from first_scale() on.
 template <int D32>
 struct KeyPiece {
-  static constexpr int NS = !PIECES<D32> ? D32 : D32 == 8 ? 2 : 1;
+  static constexpr int NS = D32 == 7 ? 3 : D32 == 3 || D32 >= 5 ? 2 : 1;
   uint32_t c[D32];
   uint32_t s[NS];
+  static constexpr __host__ __device__ int first_scale(int h) { return h * D32 / 4 < D32 - NS ? h * D32 / 4 : D32 - NS; }
+  static constexpr __host__ __device__ int scale_of(int t, int h) { return (h * D32 + t) / 4 - first_scale(h); }
+  // the quarters, a bit each, whose group t has the lane's scale i or a later one: none or all where head sizes fit the pieces
+  static constexpr __host__ __device__ int quarters(int t, int i) {
+    int q = 0;
+    for (int h = 0; h < 4; ++h) q |= scale_of(t, h) >= i ? 1 << h : 0;
+    return q;
+  }
+  template <int T>
+  __device__ __forceinline__ uint32_t scale(int h) const {
+    uint32_t x = s[0];
+    if constexpr (NS > 1) {
+      constexpr int Q = quarters(T, 1);
+      x = Q == 15 ? s[1] : Q == 0 ? x : Q >> h & 1 ? s[1] : x;
+    }
+    if constexpr (NS > 2) {
+      constexpr int Q = quarters(T, 2);
+      x = Q == 15 ? s[2] : Q == 0 ? x : Q >> h & 1 ? s[2] : x;
+    }
+    return x;
+  }
   // codes, scales: of the tile's first row (uniform); the offsets: of this lane's.  ONCE: rows that one workgroup reads, past the caches
   // (96 requests x 6144 rows x 8 heads, 641 MB: 112 us, 126 without; with 32 tiles of a request that read the same rows 288 against 267)
-  template <bool ONCE, typename W>
-  static __device__ __forceinline__ W word(const uint8_t* p) {
-    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const W*>(p));
-    else return *reinterpret_cast<const W*>(p);
+  template <bool ONCE, int N>
+  static __device__ __forceinline__ void words(const uint8_t* p, uint32_t* to) {
+    typedef uint32_t vec __attribute__((ext_vector_type(N == 1 ? 2 : N), aligned(4)));
+    if constexpr (N == 1) {
+      to[0] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p)) : *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      vec w;
+      if constexpr (ONCE) w = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p));
+      else w = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+      for (int i = 0; i < N; ++i) to[i] = w[i];
+    }
   }
   template <bool ONCE>
   __device__ __forceinline__ void read(const uint8_t* codes, const uint8_t* scales, uint32_t code_at, uint32_t scale_at) {
-    if constexpr (PIECES<D32> && D32 > 1) {
-      constexpr int N = D32 < 4 ? D32 : 4;
-      typedef uint32_t words __attribute__((ext_vector_type(N)));
-#pragma unroll
-      for (int j = 0; j < D32; j += N) {
-        const words w = word<ONCE, words>(codes + code_at + 4 * j);
-#pragma unroll
-        for (int t = 0; t < N; ++t) c[j + t] = w[t];
-      }
-    } else {
-#pragma unroll
-      for (int t = 0; t < D32; ++t) c[t] = word<ONCE, uint32_t>(codes + code_at + 16 * t);
-    }
+    words<ONCE, (D32 < 4 ? D32 : 4)>(codes + code_at, c);
+    if constexpr (D32 > 4) words<ONCE, D32 - 4>(codes + code_at + 16, c + 4);
 #pragma unroll
     for (int i = 0; i < NS; ++i) s[i] = scales[scale_at + i];
   }
-  __device__ __forceinline__ u32x4 group(int t) const { return __builtin_bit_cast(u32x4, fp4_to_bf16(c[t], fp4_scale_value(s[scale_of(t)]))); }
-  static __device__ __forceinline__ int scale_of(int t) { return !PIECES<D32> ? t : D32 == 8 ? t / 4 : 0; }
-  // which of its scales stand for NaN; those blocks are 0 then
-  __device__ __forceinline__ uint32_t take_nan() {
+  template <int T>
+  __device__ __forceinline__ u32x4 group(int h) const { return __builtin_bit_cast(u32x4, fp4_to_bf16(c[T], fp4_scale_value(scale<T>(h)))); }
+  // which groups stand for NaN; those are 0 then
+  __device__ __forceinline__ uint32_t take_nan(int h) {
     uint32_t found = 0;
+    for_groups<0, D32>([&](auto t) {
+      if (scale<t()>(h) == 255u) {
+        found |= 1u << t();
+        c[t()] = 0;
+      }
+    });
 #pragma unroll
     for (int i = 0; i < NS; ++i)
-      if (s[i] == 255u) {
-        found |= 1u << i;
-        s[i] = 127;
-#pragma unroll
-        for (int t = 0; t < D32; ++t)
-          if (scale_of(t) == i) c[t] = 0;
-      }
+      if (s[i] == 255u) s[i] = 127;
     return found;
   }
   __device__ __forceinline__ void clear() {
@@ -105,9 +130,6 @@ struct KeyPiece {
     for (int i = 0; i < NS; ++i) s[i] = 127;
   }
 };
-// offsets of a lane's piece in a row
-template <int D32> __device__ __forceinline__ uint32_t piece_codes(int h) { return PIECES<D32> ? h * 4 * D32 : 4 * h; }
-template <int D32> __device__ __forceinline__ uint32_t piece_scales(int h) { return !PIECES<D32> ? 0 : h * D32 / 4; }
 
 // A tile's request and rows.
 struct AttTile {
@@ -402,7 +424,7 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
   const ConstTable table = (ConstTable)(unsigned long long)(a.table + (size_t)tl.inst * a.blocks_per_inst);
   const uint8_t *kc = c.k.codes + kv * c.head, *ks = c.k.scales + kv * c.scale_head, *vc = c.v.codes + kv * c.head, *vs = c.v.scales + kv * c.scale_head;
-  const uint32_t code_at = n * (uint32_t)c.row + piece_codes<D32>(h), scale_at = n * (uint32_t)c.scale_row + piece_scales<D32>(h);
+  const uint32_t code_at = n * (uint32_t)c.row + h * 4 * D32, scale_at = n * (uint32_t)c.scale_row + KeyPiece<D32>::first_scale(h);
 
   KeyPiece<D32> kp[KT], vp[KT];
   int64_t code_base[KT], scale_base[KT];
@@ -510,14 +532,13 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
     for (int i = 0; i < KT; ++i) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) s[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t = 0; t < D32; ++t) {
-        const u32x4 k8 = kp[i].group(t);
+      for_groups<0, D32>([&](auto t) {
+        const u32x4 k8 = kp[i].template group<t()>(h);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int pl = 0; pl < NP; ++pl) s[rt][i] = mfma16(k8, q[rt][t][NP - 1 - pl], s[rt][i]);
-      }
+          for (int pl = 0; pl < NP; ++pl) s[rt][i] = mfma16(k8, q[rt][t()][NP - 1 - pl], s[rt][i]);
+      });
     }
     const int key0 = at * 16;
     const bool masked = key0 + KT * 16 > tl.seen_min || there_v != (1u << KT) - 1;
@@ -574,7 +595,7 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         if (!(there_v >> i & 1) || key0 + i * 16 + n >= tl.seen_max) vp[i].clear();
-        nan_at[i] = vp[i].take_nan();
+        nan_at[i] = vp[i].take_nan(h);
         nan_rows |= nan_at[i] != 0;
       }
       nan_rows = __any(nan_rows);
@@ -585,15 +606,14 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) split_weights<T>(s[rt][j], s[rt][j + 1], w[rt]);
       // chunk ch of two tiles of V to LDS; with ONES, 1 where it stands for NaN and else 0
-      auto stage = [&](int ch, bool ones) {
+      auto stage = [&](auto ch, bool ones) {
+        constexpr int first = ch() * CG, beyond = first + CG < D32 ? first + CG : D32;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int t = 0; t < CG; ++t)
-            if (ch * CG + t < D32) {
-              const uint32_t one = ones && nan_at[j + i] >> KeyPiece<D32>::scale_of(ch * CG + t) & 1 ? 0x3f803f80u : 0u;
-              *reinterpret_cast<u32x4*>(v_write + i * 16 * STRIDE + t * 64) = ones ? u32x4{one, one, one, one} : vp[j + i].group(ch * CG + t);
-            }
+          for_groups<first, beyond>([&](auto t) {
+            const uint32_t one = ones && nan_at[j + i] >> t() & 1 ? 0x3f803f80u : 0u;
+            *reinterpret_cast<u32x4*>(v_write + i * 16 * STRIDE + (t() - first) * 64) = ones ? u32x4{one, one, one, one} : vp[j + i].template group<t()>(h);
+          });
       };
       auto column = [&](int ct) {        // 32 keys of 16 columns
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(my_lds + v_read + ct * 32));
@@ -601,11 +621,11 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
         const uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
         return u32x4{x.x, x.y, y.x, y.y};
       };
-#pragma unroll
-      for (int ch = 0; ch < CHUNKS; ++ch) {
+      for_groups<0, CHUNKS>([&](auto CH) {
+        constexpr int ch = CH();
         // (LDS operations of a wave are done in their order: only the compiler has to keep it)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        stage(ch, false);
+        stage(CH, false);
         if (EARLY_V && ch == CHUNKS - 1 && at < end) {
 #pragma unroll
           for (int i = j; i < j + 2; ++i) vp[i].template read<ONCE>(vc + code_base[i], vs + scale_base[i], code_at, scale_at);
@@ -622,7 +642,7 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
         }
         if (__builtin_expect(nan_rows, 0)) {
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          stage(ch, true);
+          stage(CH, true);
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
@@ -644,7 +664,7 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
             }
           }
         }
-      }
+      });
     }
     if (!EARLY_V && at < end) {
 #pragma unroll
@@ -744,7 +764,7 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
 
 // Several tokens of a request, and calls that are not cut: a workgroup per part of a column.
 template <typename T, int D32, int RT, int KT, bool ONCE>
-__global__ __launch_bounds__(ATT_THREADS, (RT == 3 ? 2 : 1)) void fp4_attention_parts(AttCall) {
+__global__ __launch_bounds__(ATT_THREADS, (RT > 1 && D32 <= 5 ? 2 : 1)) void fp4_attention_parts(AttCall) {
   __shared__ AttLds<D32, RT> sh;
   const AttCallPtr call = att_call();
   const AttCall& k = anew(call);
@@ -763,11 +783,12 @@ __global__ __launch_bounds__(ATT_THREADS, (RT == 3 ? 2 : 1)) void fp4_attention_
 
 // One token each: the turns of all columns, request by request, are shared out evenly among the workgroups.  A share may end one column, have others whole and begin another, so a workgroup leaves at
 // most two ranges for others to fold: slot 2w what it begins with, 2w + 1 what it ends with.
-// SHARES_PER_UNIT: workgroups that a compute unit holds, four waves to each, by the registers that a variant is given.
+// SHARES_PER_UNIT: workgroups that a compute unit holds, four waves to each, by the registers that a variant is given (bf16, d = 64: four spill, 64 requests of 8192 to
+// 1000 rows 54 us, three 47).
 constexpr int SHARE_MOST_REQUESTS = 1024;
 constexpr int COLUMN_TURNS = 1;
 template <typename T, int D32>
-constexpr int SHARES_PER_UNIT = is_f32(T()) ? (D32 <= 2 ? 3 : D32 <= 5 ? 2 : 1) : D32 <= 4 ? 3 : 2;
+constexpr int SHARES_PER_UNIT = is_f32(T()) ? (D32 <= 2 ? 3 : D32 <= 6 ? 2 : 1) : D32 <= 5 ? 3 : 2;
 template <typename T, int D32, int KT, bool ONCE>
 __global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_attention_shares(AttCall) {
   constexpr int TURN = ATT_WAVES * KT * 16, PER = SHARE_MOST_REQUESTS / ATT_THREADS;
