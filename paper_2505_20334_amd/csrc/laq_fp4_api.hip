@@ -127,9 +127,9 @@ static int attention_impl(const laq_fp4_cache* cache, int32_t Hq, int32_t dtype,
   if (token_strides(Hq, c.d, dtype, &stride_token, &stride_head) != LAQ_OK) return LAQ_ERR_INVALID;
   if (ws && (ws_bytes < fp4_attention_bytes(c, Hq, dtype, n, n_tokens, max_rows) || !aligned16(ws))) return LAQ_ERR_WORKSPACE;
   if (n_tokens == 0) return LAQ_OK;
-  if (!fp4_attention_fits(c, Hq, dtype, n, n_tokens, max_rows, !start, ws)) return LAQ_ERR_UNSUPPORTED;
   const float s = scale > 0.f ? scale : 1.0f / sqrtf((float)c.d);
   const Fp4Attention a{Hq, n, width, max_rows, s * 1.44269504088896340736f, n_tokens, stride_token, stride_head, start, table, rows, q, out, lse};
+  if (!fp4_attention_fits(c, dtype, a, ws)) return LAQ_ERR_UNSUPPORTED;
   return done(launch_fp4_attention(c, dtype, a, ws, st));
 }
 

@@ -1,16 +1,21 @@
 // Attention over the paged 4-bit cache (include/laq_fp4.h: laq_fp4_attention).
 //
-// A column is a KV head of a request and a tile of its score rows (row r = query head r % G of the group of the request's token r / G).  A workgroup has a
-// range of a column's keys, in turns of 64 * KT: its four waves take 16 * KT keys of a turn each, every wave for all rows of the tile, with its own
-// reference m, sum z and sums O (one pass, exponentials of s - m); they are folded at the end through LDS, the ranges of a column by the
-// workgroup that finds all of them finished, in a fixed order.
+// A column is a KV head of a request and a tile of its score rows (row r = query head r % G of the group of the request's token r / G).  A
+// workgroup has a range of a column's keys, in turns of 64 * KT: its four waves take 16 * KT keys of a turn each, every wave for all rows of the
+// tile, with its own reference m, sum z and sums O (one pass, exponentials of s - m; m moves only when a score is more than 8 above it, so that
+// the usual step has no maximum over lanes); they are folded at the end through LDS, the ranges of a column by the workgroup that finds all of
+// them finished, in a fixed order.
 //
-// How the ranges lie: where requests have a token each, all turns of all columns are shared out evenly (fp4_attention_shares), since the lengths, which the host does
-// not know, are as unequal as requests are.  Several tokens: equal parts of the longest request that the host expects, where there would be too few
-// workgroups otherwise.
+// How the ranges lie: long calls of several requests with a token each are shared out evenly, all turns of all columns (fp4_attention_shares),
+// since the lengths, which the host does not know, are as unequal as requests are.  Other calls: equal parts of the longest request that the
+// host expects, where there would be too few workgroups otherwise (fp4_attention_parts).
 //
-// Products are 16 x 16 x 32 bf16 with the keys as the first operand's rows, so that a lane has four keys of one score row (column n = lane % 16) and all that
-// belongs to a row lies in lanes n, n + 16, n + 32, n + 48:
+// Bound: single tokens, the cache's bytes (68 a row of d = 128, K and V each): 96 x 8 heads x 6144 rows 6.3 TB/s, 128 x 8 heads x 2048 to 8192
+// rows 5.7 TB/s; the conversions are a quarter of what the vector units could do meanwhile.  Chunks of a prompt, the vector units beside the
+// matrix cores (exponentials, conversions, packing): 4 x 512 tokens x 32 heads over 8704 rows 213 us, 876 TFLOP/s.
+//
+// Products are 16 x 16 x 32 bf16 with the keys as the first operand's rows, so that a lane has four keys of one score row (column n = lane % 16)
+// and all that belongs to a row lies in lanes n, n + 16, n + 32, n + 48:
 //   S^T = K Q^T   codes go from memory to the operand's registers, converted eight numbers in four instructions with the scale applied: exact, no LDS.
 //                 A lane reads one contiguous piece of a key row (the sum over channels may take them in any order, Q the same)
 //   O^T = V^T P^T P^T is where S^T left it: the lane's four keys of two tiles are eight of the 32 summed over.  V^T needs eight keys of one channel in a
@@ -781,10 +786,11 @@ __global__ __launch_bounds__(ATT_THREADS, (RT > 1 && D32 <= 5 ? 2 : 1)) void fp4
                                AttColumn{part, parts, slot, slot + 1, 1}, sh);
 }
 
-// One token each: the turns of all columns, request by request, are shared out evenly among the workgroups.  A share may end one column, have others whole and begin another, so a workgroup leaves at
-// most two ranges for others to fold: slot 2w what it begins with, 2w + 1 what it ends with.
-// SHARES_PER_UNIT: workgroups that a compute unit holds, four waves to each, by the registers that a variant is given (bf16, d = 64: four spill, 64 requests of 8192 to
-// 1000 rows 54 us, three 47).
+// One token each: the turns of all columns, request by request, are shared out evenly among the workgroups.  A share may end one column, have
+// others whole and begin another, so a workgroup leaves at most two ranges for others to fold: slot 2w what it begins with, 2w + 1 what it ends with.
+// A column counts COLUMN_TURNS more than it has, for what beginning and folding it takes.
+// SHARES_PER_UNIT: workgroups that a compute unit holds, four waves to each, by the registers that a variant is given (bf16, d = 64: four
+// spill, 64 requests of 8192 to 1000 rows 54 us, three 47).
 constexpr int SHARE_MOST_REQUESTS = 1024;
 constexpr int COLUMN_TURNS = 1;
 template <typename T, int D32>
@@ -895,19 +901,19 @@ AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_t
   const int G = Hq / c.Hkv;
   const long long rows_each = one_each ? G : (n_tokens * G + n - 1) / n;        // score rows of a request, on average
   AttLaunch l;
-  // Tiles of 16 score rows of a workgroup.  More share what a step costs that does not depend on them (a third of its instructions with two, of d = 128), but
-  // leave fewer workgroups: three from 192 rows on, with two of these a compute unit, where head sizes leave registers for it and less would not let more
-  // workgroups in.  Two : three, us, 8 KV heads: 4 x 512 tokens x 4 heads over 8704 rows 243 : 211; 2 x 2048 over 8192 576 : 498;  16 x 48 over 2048 43.4 : 33.9,
-  // x 100 69.3 : 63.5, x 24 27.3 : 34.6;  1 x 64 over 8192 33 : 44;  d = 64, 4 x 256 over 8192 117 : 136.
+  // Tiles of 16 score rows of a workgroup.  More share what a step costs that does not depend on them (a third of its instructions with two, of
+  // d = 128), but leave fewer workgroups: three from 192 rows on, with two of these a compute unit, where head sizes leave registers for it and
+  // less would not let more workgroups in.  Two : three, us, 8 KV heads: 4 x 512 tokens x 4 heads over 8704 rows 243 : 211; 2 x 2048 over 8192
+  // 576 : 498;  16 x 48 over 2048 43.4 : 33.9, x 100 69.3 : 63.5, x 24 27.3 : 34.6;  1 x 64 over 8192 33 : 44;  d = 64, 4 x 256 over 8192 117 : 136.
   const bool three = rows_each >= 192 && c.d > 64 && c.d <= 128 && n_tokens * G / 48 * c.Hkv >= 512;
   l.row_tiles = one_each || rows_each <= 16 || dtype == LAQ_F32 ? 1 : three ? 3 : 2;
   l.key_tiles = l.row_tiles == 1 && c.d <= 128 ? 4 : 2;
   l.once = rows_each <= 16;
   const int TR = 16 * l.row_tiles, turn = ATT_WAVES * l.key_tiles * 16;
   l.plan = AttPlan{1, 0x7fffff00, (G + TR - 1) / TR, one_each && G < TR ? G : TR, turn / c.block_rows, turn % c.block_rows / 16};
-  // Columns (as many as are surely there) and the turns of the longest.  As many ranges of a column as make the sum of what they take (a turn 2 us where few
-  // workgroups run) and what folding them takes (0.12 us each) least, as long as that makes no more than two workgroups a compute unit: that many
-  // saturate the memory, and more of them only fold more.  us, bf16, 8 heads of d = 128, with 1, 2, 4, 8, 16, 32, 64 ranges:
+  // Columns (as many as are surely there) and the turns of the longest.  As many ranges of a column as make the sum of what they take (a turn 2 us
+  // where few workgroups run) and what folding them takes (0.12 us each) least, as long as that makes no more than two workgroups a compute unit:
+  // that many saturate the memory, and more of them only fold more.  us, bf16, 8 heads of d = 128, with 1, 2, 4, 8, 16, 32, 64 ranges:
   //   1 x 4096 rows 37, 24, 17, 14, 12;  1 x 65536 503, 259, 136, 76, 43, 29, 28;  4 x 16384 133, 73, 42, 28, 23, 33, 42
   //   16 x 16384 140, 79, 53, 66, 67, 86, 121;  32 x 4096 41, 31, 40, 48, 59;  64 x 4096 53, 65, 67, 83, 109
   const long long tiles = one_each ? (long long)n * l.plan.tiles_per : n_tokens * G / TR + n;
@@ -991,16 +997,24 @@ size_t fp4_attention_bytes(const Fp4View& c, int Hq, int dtype, int n, int64_t n
   return most;
 }
 
-bool fp4_attention_fits(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each, bool cut) {
-  return plan_attention(c, Hq, dtype, n, n_tokens, max_rows, one_each, cut).workgroups < (1ll << 32) / ATT_THREADS;
+namespace {
+// The launch of a call: not shared out where its turns are more than an int holds.
+AttLaunch plan_call(const Fp4View& c, int dtype, const Fp4Attention& a, bool cut) {
+  const AttLaunch l = plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, a.start == nullptr, cut);
+  const int turn = ATT_WAVES * l.key_tiles * 16;
+  const long long turns = (long long)a.blocks_per_inst * c.block_rows / turn + 1 + COLUMN_TURNS;      // of a column at most
+  if (!l.shares || turns * a.n * c.Hkv * l.plan.tiles_per <= 0x7fffffff) return l;
+  return plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, true, false);
+}
+}  // namespace
+
+bool fp4_attention_fits(const Fp4View& c, int dtype, const Fp4Attention& a, bool cut) {
+  return plan_call(c, dtype, a, cut).workgroups < (1ll << 32) / ATT_THREADS;
 }
 
 hipError_t launch_fp4_attention(const Fp4View& c, int dtype, const Fp4Attention& a, void* ws, hipStream_t st) {
   static std::atomic<uint32_t> launches{(uint32_t)(std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull >> 32)};
-  AttLaunch l = plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, a.start == nullptr, ws != nullptr);
-  // (a batch whose turns are more than an int holds is not shared out)
-  if (l.shares && ((int64_t)a.blocks_per_inst * c.block_rows / 128 + 1) * a.n * c.Hkv * l.plan.tiles_per > 0x7fffffff)
-    l = plan_attention(c, a.Hq, dtype, a.n, a.n_tokens, a.max_rows, true, false);
+  const AttLaunch l = plan_call(c, dtype, a, ws != nullptr);
   AttParts pa{static_cast<unsigned long long*>(ws), nullptr, 0};
   if (l.slots) {
     pa.sums = reinterpret_cast<float*>(pa.marks + 2 * l.slots * l.plan.ws_rows);

@@ -70,7 +70,7 @@ hipError_t launch_fp4_compact(const Fp4View& c, int dtype, int n, int inst0, int
                               const void* k, const void* v, const int32_t* idx, const int32_t* slots, hipStream_t st);
 hipError_t launch_fp4_load(const Fp4View& c, int dtype, int64_t n_tokens, const int32_t* slots, void* k, void* v, hipStream_t st);
 size_t fp4_attention_bytes(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows);
-bool fp4_attention_fits(const Fp4View& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows, bool one_each, bool cut);      // in a launch
+bool fp4_attention_fits(const Fp4View& c, int dtype, const Fp4Attention& a, bool cut);      // in a launch
 hipError_t launch_fp4_attention(const Fp4View& c, int dtype, const Fp4Attention& a, void* ws, hipStream_t st);
 
 }  // namespace laq

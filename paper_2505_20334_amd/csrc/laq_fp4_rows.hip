@@ -19,9 +19,13 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true));    // lane ^ 2
 }
 
+// Reads of rows that one workgroup reads once, past the caches (32 x 8 heads, 2048 to 128 rows of 8192 compacted and loaded: 81 -> 73 us).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 read_once(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4*>(p)); }
+
 struct Piece16 {
   uint4 x;
-  __device__ __forceinline__ void read(const uint16_t* p) { x = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void read(const uint16_t* p) { x = __builtin_bit_cast(uint4, read_once(p)); }
   __device__ __forceinline__ uint32_t most() const {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     uint32_t m = 0;
@@ -40,8 +44,8 @@ struct Piece16 {
 struct Piece32 {
   float4 a, b;
   __device__ __forceinline__ void read(const float* p) {
-    a = *reinterpret_cast<const float4*>(p);
-    b = *reinterpret_cast<const float4*>(p + 4);
+    a = __builtin_bit_cast(float4, read_once(p));
+    b = __builtin_bit_cast(float4, read_once(p + 4));
   }
   __device__ __forceinline__ uint32_t most() const {
     const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -61,7 +65,7 @@ struct Piece32 {
 template <typename T> struct PieceOfRow { using type = Piece16; };
 template <> struct PieceOfRow<float> { using type = Piece32; };
 
-// A workgroup's lanes over rows of d / 8 pieces: as many rows as fit, PASSES times.
+// A workgroup's lanes over rows of d / 8 pieces: as many rows as fit, a number of times.
 template <int D32>
 struct RowLanes {
   static constexpr int PIECES = 4 * D32, ROWS = ROWS_THREADS / PIECES;
@@ -69,8 +73,10 @@ struct RowLanes {
   bool on;
   __device__ __forceinline__ RowLanes() : row(threadIdx.x / PIECES), col(threadIdx.x % PIECES), on((int)threadIdx.x < ROWS * PIECES) {}
 };
-// Rows that a lane has in flight, K and V of each: one made 16381 tokens x 8 heads of d = 128 wait 25.4 us for their memory.
-constexpr int PASSES = 2;
+// Rows that a lane has in flight, K and V of each.  Rows that lie in order: two (16381 tokens x 8 heads of d = 128 stored in 33.2 us, with one
+// 33.8).  Rows that are looked up in a list first: one, since more workgroups hide the wait better than longer ones (32 x 8 heads, 2048 to
+// 128 rows of 8192 compacted and loaded, one 72.5 us, two 76.5, four 76.9).
+constexpr int PASSES_ORDERED = 2, PASSES_LISTED = 1;
 
 __device__ __forceinline__ int64_t code_at(const Fp4View& c, int block, int head, int row) { return block * c.block + head * c.head + row * c.row; }
 __device__ __forceinline__ int64_t scale_at(const Fp4View& c, int block, int head, int row) { return block * c.scale_block + head * c.scale_head + row * c.scale_row; }
@@ -101,6 +107,7 @@ template <typename T, int D32>
 __global__ __launch_bounds__(ROWS_THREADS) void fp4_store_kernel(Fp4View c, TokenRows t, const T* __restrict__ k, const T* __restrict__ v,
                                                                  const int32_t* __restrict__ slots) {
   const RowLanes<D32> l;
+  constexpr int PASSES = PASSES_ORDERED;
   const int64_t first = (int64_t)blockIdx.x * (l.ROWS * PASSES);
   typename PieceOfRow<T>::type kp[PASSES], vp[PASSES];
   int slot[PASSES], head[PASSES];
@@ -130,6 +137,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void fp4_compact_kernel(Fp4View c, in
                                                                    const T* __restrict__ v, const int32_t* __restrict__ idx,
                                                                    const int32_t* __restrict__ slots) {
   const RowLanes<D32> l;
+  constexpr int PASSES = PASSES_LISTED;
   const int li = blockIdx.z, head = blockIdx.y, bk = tab.rows(li), r0 = blockIdx.x * (l.ROWS * PASSES);
   if (r0 >= bk) return;
   const int64_t first = tab.first(li), from_head = (int64_t)(inst0 + li) * lay.inst + head * lay.head + l.col * 8;
@@ -185,6 +193,7 @@ template <typename T, int D32>
 __global__ __launch_bounds__(ROWS_THREADS) void fp4_load_kernel(Fp4View c, TokenRows t, const int32_t* __restrict__ slots, T* __restrict__ k,
                                                                 T* __restrict__ v) {
   const RowLanes<D32> l;
+  constexpr int PASSES = PASSES_ORDERED;
   const int64_t first = (int64_t)blockIdx.x * (l.ROWS * PASSES);
   int slot[PASSES], head[PASSES];
 #pragma unroll
@@ -233,12 +242,15 @@ hipError_t by_size(int d, const F& f) {
     default: return f(std::integral_constant<int, 8>{});
   }
 }
-template <int D32> unsigned workgroups(int64_t rows) { return (unsigned)((rows + RowLanes<D32>::ROWS * PASSES - 1) / (RowLanes<D32>::ROWS * PASSES)); }
+template <int D32, int PASSES>
+unsigned workgroups(int64_t rows) {
+  return (unsigned)((rows + RowLanes<D32>::ROWS * PASSES - 1) / (RowLanes<D32>::ROWS * PASSES));
+}
 
 template <typename T>
 hipError_t store(const Fp4View& c, const TokenRows& t, const void* k, const void* v, const int32_t* slots, hipStream_t st) {
   return by_size(c.d, [&](auto d32) {
-    hipLaunchKernelGGL((fp4_store_kernel<T, d32()>), dim3(workgroups<d32()>(t.n_rows)), dim3(ROWS_THREADS), 0, st, c, t, static_cast<const T*>(k),
+    hipLaunchKernelGGL((fp4_store_kernel<T, d32()>), dim3(workgroups<d32(), PASSES_ORDERED>(t.n_rows)), dim3(ROWS_THREADS), 0, st, c, t, static_cast<const T*>(k),
                        static_cast<const T*>(v), slots);
     return hipGetLastError();
   });
@@ -248,7 +260,7 @@ template <typename T>
 hipError_t compact(const Fp4View& c, int n, int inst0, int most, int L, const KvLayout& lay, const InstTable& tab, const void* k, const void* v,
                    const int32_t* idx, const int32_t* slots, hipStream_t st) {
   return by_size(c.d, [&](auto d32) {
-    hipLaunchKernelGGL((fp4_compact_kernel<T, d32()>), dim3(workgroups<d32()>(most), c.Hkv, n), dim3(ROWS_THREADS), 0, st, c, L, lay, tab, inst0,
+    hipLaunchKernelGGL((fp4_compact_kernel<T, d32()>), dim3(workgroups<d32(), PASSES_LISTED>(most), c.Hkv, n), dim3(ROWS_THREADS), 0, st, c, L, lay, tab, inst0,
                        static_cast<const T*>(k), static_cast<const T*>(v), idx, slots);
     return hipGetLastError();
   });
@@ -257,7 +269,7 @@ hipError_t compact(const Fp4View& c, int n, int inst0, int most, int L, const Kv
 template <typename T>
 hipError_t load(const Fp4View& c, const TokenRows& t, const int32_t* slots, void* k, void* v, hipStream_t st) {
   return by_size(c.d, [&](auto d32) {
-    hipLaunchKernelGGL((fp4_load_kernel<T, d32()>), dim3(workgroups<d32()>(t.n_rows)), dim3(ROWS_THREADS), 0, st, c, t, slots, static_cast<T*>(k),
+    hipLaunchKernelGGL((fp4_load_kernel<T, d32()>), dim3(workgroups<d32(), PASSES_ORDERED>(t.n_rows)), dim3(ROWS_THREADS), 0, st, c, t, slots, static_cast<T*>(k),
                        static_cast<T*>(v));
     return hipGetLastError();
   });
