@@ -14,7 +14,9 @@
  * The conventions of laq.h hold: device pointers, work enqueued on `stream`, arguments checked before
  * anything is enqueued, no allocation, results a pure function of the inputs.  `budget` is a HOST array; lengths,
  * tables and slots are DEVICE arrays whose values the host cannot see: the kernels check every block number and slot
- * against the cache and touch nothing outside of it, whatever they hold.
+ * against the cache and touch nothing outside of it, whatever they hold.  Outputs do not overlap inputs.  Calls that use one cache,
+ * one pool (rows, block_table, free_blocks, state) or one workspace run one after another: on one stream, or on streams that wait
+ * for each other; several captured graphs may hold the same ones on that condition.  A batch of no tokens is LAQ_OK and does nothing.
  *
  * Numbers: a row of d numbers is d / 32 blocks of 32 in the microscaling format with 4-bit elements (e2m1): a scale byte s stands for
  * 2^(s - 127), a code for a sign (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; number 2j of the row is in the low half of byte j,
@@ -82,6 +84,7 @@ int laq_block_map(int32_t n, int32_t block_rows, int32_t n_blocks, int32_t block
  *                 of 16 bytes, as are the addresses.  Both or one of them (the other NULL and left alone)
  *   slots         int32 [n_tokens] as laq_block_map writes them; a token whose slot is not one of the cache is left out.  Two
  *                 tokens of one call must not have the same slot (which of them each block of 32 numbers comes from is not defined)
+ * n_tokens * Hkv * d / 8 up to 2^32 - 256 (LAQ_ERR_UNSUPPORTED), for laq_fp4_load too; a KV head's rows * 32 * Hkv for laq_fp4_compact.
  */
 int laq_fp4_store(const laq_fp4_cache *cache, int32_t dtype, int64_t n_tokens, const void *k, const void *v, int64_t stride_token,
                   int64_t stride_head, const int32_t *slots, void *stream);
@@ -106,8 +109,8 @@ int laq_fp4_load(const laq_fp4_cache *cache, int32_t dtype, int64_t n_tokens, co
 /*
  * Attention over the cache: tokens of n requests attend to the rows that their request holds, the tokens' own rows (the last ones)
  * among them, each to those up to its own.
- *   Hq, dtype, scale  query heads (a multiple of the cache's Hkv), laq_dtype of q and out, logit scale (<= 0: 1/sqrt(d))
- *   n_tokens      tokens of the batch
+ *   Hq, dtype, scale  query heads (a multiple of the cache's Hkv, <= 65535), laq_dtype of q and out, logit scale (<= 0: 1/sqrt(d))
+ *   n_tokens      tokens of the batch; n_tokens * Hq < 2^31
  *   start         int32 [n + 1]: tokens start[i] .. start[i+1]-1 are those of request i, in order; ascending, start[0] = 0.
  *                 Tokens from start[n] on (padding) are left alone.  NULL: one token per request (n_tokens = n)
  *   q             [n_tokens, Hq, d], rows contiguous, stride_token and stride_head elements apart (both zero: dense); multiples of
@@ -123,6 +126,7 @@ int laq_fp4_load(const laq_fp4_cache *cache, int32_t dtype, int64_t n_tokens, co
  *   ws / ws_bytes optional device scratch.  With at least laq_fp4_attention_workspace_bytes() bytes (same arguments), long rows of
  *                 small calls are spread over several workgroups; LAQ_ERR_WORKSPACE if given but smaller or not 16-byte aligned.
  *                 With and without it the last bits of `out` may differ
+ * A call that needs more than 2^24 workgroups (about n * Hkv of them, or n_tokens * Hq / 16) is LAQ_ERR_UNSUPPORTED.
  * bf16: the products of q and K are exact, sums, maxima and weights are fp32, weights are rounded to bf16 for the product with V, out
  * is rounded once.  fp32: q and weights as three bf16 parts each (2^-24), V exact, sums fp32.
  */

@@ -12,7 +12,8 @@ constexpr int32_t MOST_HEADS = 32768;
 int fp4_view(const laq_fp4_cache* cache, bool need_k, bool need_v, Fp4View* view) {
   if (!cache) return LAQ_ERR_INVALID;
   const laq_fp4_cache& c = *cache;
-  if (c.n_blocks < 1 || c.Hkv < 1 || c.block_rows < 16 || c.block_rows % 16 || c.d < 32 || c.d > 256 || c.d % 32 || c.Hkv > MOST_HEADS) return LAQ_ERR_INVALID;
+  if (c.n_blocks < 1 || c.Hkv < 1 || c.Hkv > MOST_HEADS || c.block_rows < 16 || c.block_rows % 16) return LAQ_ERR_INVALID;
+  if (c.d < 32 || c.d > 256 || c.d % 32) return LAQ_ERR_INVALID;
   if ((int64_t)c.n_blocks * c.block_rows > MOST_ROWS) return LAQ_ERR_INVALID;
   if ((need_k && (!c.k || !c.k_scale)) || (need_v && (!c.v || !c.v_scale))) return LAQ_ERR_INVALID;
   if ((need_k && !aligned16(c.k)) || (need_v && !aligned16(c.v))) return LAQ_ERR_INVALID;
@@ -22,7 +23,8 @@ int fp4_view(const laq_fp4_cache* cache, bool need_k, bool need_v, Fp4View* view
     if (s < 0) return LAQ_ERR_INVALID;
     zeros += s == 0;
   }
-  *view = Fp4View{{c.k, c.k_scale}, {c.v, c.v_scale}, c.n_blocks, c.block_rows, c.Hkv, c.d, given[0], given[1], given[2], given[3], given[4], given[5]};
+  *view = Fp4View{{c.k, c.k_scale}, {c.v, c.v_scale}, c.n_blocks, c.block_rows, c.Hkv, c.d,
+                  given[0], given[1], given[2], given[3], given[4], given[5]};
   if (zeros == 6) {
     view->row = c.d / 2;
     view->head = view->row * c.block_rows;
@@ -68,9 +70,9 @@ static int store_impl(const laq_fp4_cache* cache, int32_t dtype, int64_t n_token
                       int64_t stride_head, const int32_t* slots, hipStream_t st) {
   Fp4View c;
   if (fp4_view(cache, k != nullptr, v != nullptr, &c) != LAQ_OK) return LAQ_ERR_INVALID;
-  if (n_tokens < 0 || (!k && !v) || !aligned16(k) || !aligned16(v) || !slots) return LAQ_ERR_INVALID;
-  if (token_strides(c.Hkv, c.d, dtype, &stride_token, &stride_head) != LAQ_OK) return LAQ_ERR_INVALID;
-  if (n_tokens == 0) return LAQ_OK;
+  if (n_tokens < 0 || token_strides(c.Hkv, c.d, dtype, &stride_token, &stride_head) != LAQ_OK) return LAQ_ERR_INVALID;
+  if (n_tokens == 0) return LAQ_OK;      // (the addresses of tensors without elements are NULL)
+  if ((!k && !v) || !aligned16(k) || !aligned16(v) || !slots) return LAQ_ERR_INVALID;
   if (n_tokens > MOST_PIECES / c.Hkv / (c.d / 8)) return LAQ_ERR_UNSUPPORTED;
   return done(launch_fp4_store(c, dtype, n_tokens, k, v, stride_token, stride_head, slots, st));
 }
@@ -78,8 +80,9 @@ static int store_impl(const laq_fp4_cache* cache, int32_t dtype, int64_t n_token
 static int load_impl(const laq_fp4_cache* cache, int32_t dtype, int64_t n_tokens, const int32_t* slots, void* k, void* v, hipStream_t st) {
   Fp4View c;
   if (fp4_view(cache, k != nullptr, v != nullptr, &c) != LAQ_OK) return LAQ_ERR_INVALID;
-  if (n_tokens < 0 || (!k && !v) || !aligned16(k) || !aligned16(v) || !slots || (dtype != LAQ_F32 && dtype != LAQ_BF16)) return LAQ_ERR_INVALID;
+  if (n_tokens < 0 || (dtype != LAQ_F32 && dtype != LAQ_BF16)) return LAQ_ERR_INVALID;
   if (n_tokens == 0) return LAQ_OK;
+  if ((!k && !v) || !aligned16(k) || !aligned16(v) || !slots) return LAQ_ERR_INVALID;
   if (n_tokens > MOST_PIECES / c.Hkv / (c.d / 8)) return LAQ_ERR_UNSUPPORTED;
   return done(launch_fp4_load(c, dtype, n_tokens, slots, k, v, st));
 }
@@ -112,8 +115,8 @@ static int fp4_compact_impl(const laq_shape* shape, const void* k, const void* v
 }
 
 static bool attention_sizes_ok(const Fp4View& c, int32_t Hq, int32_t dtype, int32_t n, int64_t n_tokens, int32_t max_rows) {
-  return Hq >= 1 && Hq % c.Hkv == 0 && Hq <= 65535 && (dtype == LAQ_F32 || dtype == LAQ_BF16) && n >= 1 && n_tokens >= 0 && n_tokens <= MOST_ROWS / Hq &&
-         max_rows >= 1;
+  return Hq >= 1 && Hq % c.Hkv == 0 && Hq <= 65535 && (dtype == LAQ_F32 || dtype == LAQ_BF16) && n >= 1 && n_tokens >= 0 &&
+         n_tokens <= MOST_ROWS / Hq && max_rows >= 1;
 }
 
 static int attention_impl(const laq_fp4_cache* cache, int32_t Hq, int32_t dtype, float scale, int32_t n, int64_t n_tokens, const int32_t* start,
@@ -122,11 +125,11 @@ static int attention_impl(const laq_fp4_cache* cache, int32_t Hq, int32_t dtype,
   Fp4View c;
   if (fp4_view(cache, true, true, &c) != LAQ_OK || !attention_sizes_ok(c, Hq, dtype, n, n_tokens, max_rows)) return LAQ_ERR_INVALID;
   if (width < 1 || (int64_t)width * c.block_rows > MOST_ROWS || max_rows > width * c.block_rows) return LAQ_ERR_INVALID;
-  if (!q || !table || !rows || !out || !aligned16(q) || !aligned16(out) || (!start && n_tokens != n)) return LAQ_ERR_INVALID;
-  if (!(scale == scale) || isinf(scale)) return LAQ_ERR_INVALID;
+  if (!(scale == scale) || isinf(scale) || (!start && n_tokens != n)) return LAQ_ERR_INVALID;
   if (token_strides(Hq, c.d, dtype, &stride_token, &stride_head) != LAQ_OK) return LAQ_ERR_INVALID;
-  if (ws && (ws_bytes < fp4_attention_bytes(c, Hq, dtype, n, n_tokens, max_rows) || !aligned16(ws))) return LAQ_ERR_WORKSPACE;
   if (n_tokens == 0) return LAQ_OK;
+  if (!q || !table || !rows || !out || !aligned16(q) || !aligned16(out)) return LAQ_ERR_INVALID;
+  if (ws && (ws_bytes < fp4_attention_bytes(c, Hq, dtype, n, n_tokens, max_rows) || !aligned16(ws))) return LAQ_ERR_WORKSPACE;
   const float s = scale > 0.f ? scale : 1.0f / sqrtf((float)c.d);
   const Fp4Attention a{Hq, n, width, max_rows, s * 1.44269504088896340736f, n_tokens, stride_token, stride_head, start, table, rows, q, out, lse};
   if (!fp4_attention_fits(c, dtype, a, ws)) return LAQ_ERR_UNSUPPORTED;

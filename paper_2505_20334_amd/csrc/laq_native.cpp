@@ -369,6 +369,7 @@ bool fp4_cache(PyObject* o, laq_fp4_cache* c, const at::Tensor** first) {
   c->Hkv = (int32_t)t[0]->size(1);
   c->block_rows = (int32_t)t[0]->size(2);
   c->d = (int32_t)(2 * t[0]->size(3));
+  if (c->block_rows < 1) return false;
   if (!t[0]->is_contiguous() || !t[1]->is_contiguous()) {
     c->stride_block = t[0]->stride(0);
     c->stride_head = t[0]->stride(1);

@@ -42,6 +42,13 @@ def _here(t: torch.Tensor) -> None:
         raise ValueError("the tensors live on %s, which is not the current device" % t.device)
 
 
+def _int32(x, name: str) -> int:
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError("%s is a number of 32 bits" % name)
+    return x
+
+
 def _ints(t: torch.Tensor, name: str, like: torch.Tensor, numel: int) -> torch.Tensor:
     """A dense int32 tensor of at least `numel` entries on the device of `like`."""
     if t.device.type != "cuda":
@@ -103,7 +110,7 @@ def laq_block_map(add: torch.Tensor, rows: torch.Tensor, block_table: torch.Tens
         _ints(slots, "slots", rows, n_slots or 0)
     if start is not None:
         _ints(start, "start", rows, n + 1)
-    rc = lib.laq_block_map(n, int(block_rows), free_blocks.numel(), block_table.shape[1], add.data_ptr(), rows.data_ptr(), block_table.data_ptr(),
+    rc = lib.laq_block_map(n, _int32(block_rows, "block_rows"), free_blocks.numel(), block_table.shape[1], add.data_ptr(), rows.data_ptr(), block_table.data_ptr(),
                            free_blocks.data_ptr(), state.data_ptr(), start.data_ptr() if start is not None else None,
                            slots.data_ptr() if slots is not None else None, slots.numel() if slots is not None else 0, _stream(stream))
     if rc != 0:
@@ -193,7 +200,8 @@ def laq_fp4_load(cache: Fp4Cache, slots: torch.Tensor, dtype: torch.dtype = torc
 
 def laq_fp4_attention_workspace_bytes(cache: Fp4Cache, Hq: int, dtype: torch.dtype, n: int, n_tokens: int, max_rows: int) -> int:
     code = binding.LAQ_F32 if dtype == torch.float32 else binding.LAQ_BF16
-    return int(load_library().laq_fp4_attention_workspace_bytes(ctypes.byref(_fp4(cache)), int(Hq), code, int(n), int(n_tokens), int(max_rows)))
+    return int(load_library().laq_fp4_attention_workspace_bytes(ctypes.byref(_fp4(cache)), _int32(Hq, "Hq"), code, _int32(n, "n"), int(n_tokens),
+                                                               _int32(max_rows, "max_rows")))
 
 
 def laq_fp4_attention(q: torch.Tensor, cache: Fp4Cache, block_table: torch.Tensor, rows: torch.Tensor, start: Optional[torch.Tensor] = None,
@@ -223,7 +231,7 @@ def laq_fp4_attention(q: torch.Tensor, cache: Fp4Cache, block_table: torch.Tenso
         _ints(start, "start", q, n + 1)
     elif T != n:
         raise ValueError("without start there is one token per request")
-    most = width * c.block_rows if max_rows is None else max(1, int(max_rows))
+    most = max(1, _int32(width * c.block_rows if max_rows is None else max_rows, "max_rows"))
     _out(out, "out", q.dtype, T * Hq * d, q)
     _out(lse, "lse", torch.float32, T * Hq, q)
     if out is None:

@@ -144,3 +144,38 @@ def test_the_library_exports_what_its_second_header_declares(repo_root):
     assert names == ["laq_block_map", "laq_fp4_attention", "laq_fp4_attention_workspace_bytes", "laq_fp4_compact", "laq_fp4_load", "laq_fp4_store"]
     for name in names:
         assert getattr(laq.load_library(), name) is not None and name in laq.__all__
+
+
+WIDE = dict(stride_head=1024, stride_row=64, scale_stride_block=128, scale_stride_head=64, scale_stride_row=4)
+
+
+@pytest.mark.parametrize("bad", [dict(Hkv=32769), dict(stride_block=1 << 32, **WIDE), dict(stride_block=2048, **{**WIDE, "scale_stride_block": 1 << 32}),
+                                 dict(stride_block=2048, **{**WIDE, "stride_row": (1 << 27) + 16}),
+                                 dict(stride_block=2048, **{**WIDE, "scale_stride_row": (1 << 27) + 1})])
+def test_caches_whose_offsets_do_not_fit(bad):
+    test_caches_that_are_refused(bad)
+
+
+def test_calls_that_are_too_large():
+    lib = laq.load_library()
+    assert lib.laq_block_map(1 << 16, 16, 8, 1 << 15, FAKE, FAKE, FAKE, FAKE, FAKE, None, None, 0, None) == UNSUPPORTED
+    c = ctypes.byref(_cache())
+    assert lib.laq_fp4_load(c, 1, 1 << 32, FAKE, FAKE, FAKE, None) == UNSUPPORTED
+    n = 1 << 23                                          # x 2 KV heads
+    assert lib.laq_fp4_attention(c, 2, 1, 0.0, n, n, None, FAKE, 0, 0, FAKE, 4, FAKE, 64, FAKE, None, None, 0, None) == UNSUPPORTED
+    # shared out among few workgroups, but for turns that may be more than an int holds
+    many = ctypes.byref(_cache(Hkv=32768))
+    args = (many, 32768, 1, 0.0, 1024, 1024, None, FAKE, 0, 0, FAKE, (1 << 27) - 1, FAKE, 8192, FAKE, None)
+    assert lib.laq_fp4_attention(*args, FAKE, 1 << 62, None) == UNSUPPORTED
+
+
+def test_batches_without_tokens_need_no_addresses():
+    lib = laq.load_library()
+    c = ctypes.byref(_cache())
+    assert lib.laq_fp4_store(c, 1, 0, None, None, 0, 0, None, None) == 0
+    assert lib.laq_fp4_load(c, 1, 0, None, None, None, None) == 0
+    assert lib.laq_fp4_attention(c, 8, 1, 0.0, 2, 0, FAKE, None, 0, 0, FAKE, 4, FAKE, 64, None, None, None, 0, None) == 0
+    # but sizes that are right
+    assert lib.laq_fp4_store(c, 3, 0, None, None, 0, 0, None, None) == INVALID
+    assert lib.laq_fp4_load(c, 3, 0, None, None, None, None) == INVALID
+    assert lib.laq_fp4_attention(c, 7, 1, 0.0, 2, 0, FAKE, None, 0, 0, FAKE, 4, FAKE, 64, None, None, None, 0, None) == INVALID

@@ -568,3 +568,139 @@ def test_evict_into_the_cache_and_decode_on_it():
     want = laq.laq_evict(q[:1], kv[0].contiguous(), kv[1].contiguous(), [50], 7)
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+# ---- calls that the documentation allows ---------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_more_requests_than_are_shared_out(dtype):
+    rows = [(i * 37) % 50 for i in range(1100)]
+    c = Case(dtype, 2, 1, 32, 16, rows, [1] * 1100)
+    for most in (50, 65536):                          # (as long as a bound may make it: spread over workgroups, if that is worth it)
+        c.table = torch.nn.functional.pad(c.table, (0, 4096 - c.table.shape[1]), value=-1)
+        out, lse = c.run(max_rows=most)
+        torch.cuda.synchronize()
+        c.check(out, lse, what="max_rows %d" % most)
+
+
+def test_turns_that_may_be_more_than_an_int_holds():
+    # a table of 2^31 rows, nearly, a request, three requests of 128 heads: 2^23 turns of 256 rows for each of 384 columns
+    c = Case(BF16, 128, 128, 32, 65536, [300, 40, 0], [1, 1, 1], spare=32766)
+    out, lse = c.run(max_rows=8192)
+    torch.cuda.synchronize()
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_start_that_makes_no_sense_stays_in_bounds(dtype):
+    c = Case(dtype, 8, 2, 64, 16, [100, 50, 70], [20, 5, 30])
+    T, big = 55, (1 << 31) - 1
+    for start in ([7, 20, 25, 55], [0, 40, 10, 55], [-5, 20, 25, 1000], [big, big, big, big], [0, 0, 0, 0], [-big, big, -big, big]):
+        bounds = torch.full((T + 60, 8, 64), 5.0, dtype=dtype, device=DEV)
+        lse = torch.full((T + 60, 8), 5.0, device=DEV)
+        c.start_d = torch.tensor(start, dtype=torch.int32, device=DEV)
+        for split in (True, False):
+            c.run(out=bounds[30:30 + T], lse=lse[30:30 + T], split=split)
+            torch.cuda.synchronize()
+            for x in (bounds, lse):
+                assert (x[:30] == 5.0).all() and (x[30 + T:] == 5.0).all(), start
+    assert (bounds[30:30 + T] != 5.0).any()           # (the last one: request 0 has all tokens, or what is left of it)
+
+
+def test_graphs_that_share_a_workspace():
+    # calls of both kinds, captured with one workspace, replayed in any order among eager calls
+    cases = [Case(BF16, 8, 2, 128, 64, [3000, 17, 900], [1, 1, 1]), Case(BF16, 8, 8, 64, 16, [5000, 4100] * 8, [1] * 16, seed=3), Case(F32, 8, 2, 64, 32, [2000, 50], [2, 9], seed=5)]
+    laq = _laq()
+    need = [laq.laq_fp4_attention_workspace_bytes(c.cache, 8, c.dtype, len(c.rows), c.qd.shape[0], max(c.rows)) for c in cases]
+    assert all(need)
+    ws = torch.zeros(max(need), dtype=torch.uint8, device=DEV)
+    graphs, outs = [], []
+    for c in cases:
+        c.run(ws=ws)
+        outs.append((torch.empty_like(c.qd), torch.empty(c.qd.shape[0], 8, device=DEV)))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.run(out=outs[-1][0], lse=outs[-1][1], ws=ws)
+        graphs.append(graph)
+    for round_, order in enumerate(((0, 1, 2), (2, 2, 1, 0, 1), (1, 0, 0, 2), (0, 2, 1))):
+        for c in cases:
+            c.qd.normal_()
+        want = [c.run() for c in cases]
+        for i in order:
+            outs[i][0].fill_(3.0)
+            graphs[i].replay()
+            if round_ % 2:
+                cases[(i + 1) % 3].run(ws=ws)
+        torch.cuda.synchronize()
+        for i, (w, o) in enumerate(zip(want, outs)):
+            assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1]), (round_, i)
+
+
+def test_two_streams_with_a_workspace_each():
+    # calls that are cut, under way at the same time on the same cache
+    cases = [Case(BF16, 8, 2, 128, 64, [30000], [1]), Case(BF16, 8, 8, 64, 16, [5000, 4100] * 8, [1] * 16, seed=3)]
+    want = [c.run() for c in cases]
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream() for _ in cases]
+    got = [[], []]
+    for _ in range(6):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(sides[i]):
+                got[i].append(c.run())
+    torch.cuda.synchronize()
+    for i, w in enumerate(want):
+        for g in got[i]:
+            assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+def test_batches_without_tokens():
+    laq = _laq()
+    c = Case(BF16, 8, 2, 64, 16, [20, 5], [0, 0], pad=1)
+    nothing = torch.empty(0, 2, 64, dtype=BF16, device=DEV)
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    before = [t.clone() for t in c.cache]
+    laq.laq_fp4_store(c.cache, nothing, nothing, none)
+    assert [t.shape for t in laq.laq_fp4_load(c.cache, none)] == [(0, 2, 64)] * 2
+    out, lse = laq.laq_fp4_attention(c.qd[:0], c.cache, c.table, c.rows_d, start=c.start_d, want_lse=True)
+    assert out.shape == (0, 8, 64) and lse.shape == (0, 8)
+    out = torch.full((1, 8, 64), 7.0, dtype=BF16, device=DEV)           # padding alone
+    c.run(out=out)
+    torch.cuda.synchronize()
+    assert (out == 7.0).all() and all(torch.equal(x, y) for x, y in zip(before, c.cache))
+
+
+def test_the_calls_without_the_compiled_binding(monkeypatch):
+    from paper_2505_20334_amd import binding
+    laq = _laq()
+    c = Case(BF16, 8, 2, 64, 16, [600, 50], [2, 3], fused=True)
+    idx = torch.arange(2 * 30, dtype=torch.int32, device=DEV) % 30
+    n_slots = torch.tensor([20, 5], dtype=torch.int32, device=DEV)
+
+    def calls():
+        cache, (free, state) = laq.laq_fp4_cache(40, 2, 16, 64, DEV), laq.laq_block_pool(40, DEV)
+        rows, table = torch.zeros(2, dtype=torch.int32, device=DEV), torch.full((2, 20), -1, dtype=torch.int32, device=DEV)
+        start, slots = laq.laq_block_map(n_slots, rows, table, free, state, 16, n_slots=30)
+        x = torch.linspace(-3, 3, 30 * 2 * 64, device=DEV).view(30, 2, 64)
+        laq.laq_fp4_store(cache, x, x.neg(), slots)
+        other = laq.laq_fp4_cache(40, 2, 16, 64, DEV)
+        laq.laq_fp4_compact(other, x.transpose(0, 1)[None], None, idx, [30], slots)
+        return [*cache, *other, *laq.laq_fp4_load(cache, slots, F32), rows, table[0, :2], table[1, :1], free[:37], state, start, slots, *c.run()]
+
+    with_it = calls()
+    binding.load_library()
+    monkeypatch.setattr(binding, "_native", None)
+    without = calls()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(with_it, without))
+
+
+def test_one_table_row_of_a_request_shared_by_two():
+    # two requests on the same blocks (a common prompt): both read them
+    c = Case(BF16, 8, 2, 128, 16, [200, 200], [1, 1])
+    c.table[1] = c.table[0]
+    q = c.qd.clone()
+    q[1] = q[0]
+    c.qd = q
+    out, lse = c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[1]) and torch.equal(lse[0], lse[1])
