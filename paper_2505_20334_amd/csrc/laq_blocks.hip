@@ -237,9 +237,10 @@ __global__ __launch_bounds__(THREADS) void block_map_kernel(MapArgs a) {
   }
 }
 
-// Workgroups: a thread has two times four slots, or, where there are no slots (rows are dropped), may have two blocks of a pool of more than 4096.  They cost
-// a count in memory at the end, 0.7 us for two of them, 1.5 for 128.  294000 slots of 256 requests, 9200 blocks, appended and dropped, with 1, 8, 32, 64, 128
-// and 256 workgroups: 512, 80, 29, 21.6, 19.2, 22 us; 32 requests of 8 slots each 11.5, 12.9, 12.9, 12.7, 14.4, 18.3.
+// Workgroups of 1024 threads with four slots each, or, in small calls, of 256 with two times four; where there are no slots (rows are dropped) and
+// the pool has more than 4096 blocks, two blocks a thread.  They cost a count in memory at the end, 0.7 us for two of them, 1.5 for 128.
+// 294000 slots of 256 requests, 9200 blocks, appended and dropped: two times four a thread 18.2 us, four 16.5, two 16.5, workgroups of 256 19.2;
+// 160000 of 1000 requests 22.2, 18.8, 18.7.  19000 slots of 64 requests in five workgroups of 1024 14.2, in ten of 256 15.4.
 constexpr int MAP_MOST_WORKGROUPS = 128;
 
 }  // namespace
@@ -247,11 +248,10 @@ constexpr int MAP_MOST_WORKGROUPS = 128;
 hipError_t launch_block_map(int n, int block_rows, int n_blocks, int width, const int32_t* add, int32_t* rows, int32_t* table, int32_t* list,
                             int32_t* state, int32_t* start, int32_t* slots, int64_t n_slots, hipStream_t st) {
   const int64_t work = n_slots ? n_slots / 4 : n_blocks > 4096 ? n_blocks : 1, wanted = (work + 511) / 512;
-  // (many workgroups are a quarter as many of 1024 threads: the count at the end takes less)
-  const int threads = n <= 256 && wanted < 16 ? 256 : 1024;
+  const int threads = n <= 256 && wanted < 4 ? 256 : 1024;
   const int shift = (block_rows & (block_rows - 1)) == 0 ? __builtin_ctz(block_rows) : -1;
   const MapArgs a{n, block_rows, n_blocks, width, (n + threads - 1) / threads, shift, add, rows, table, list, state, start, slots, n_slots};
-  const int64_t groups = threads == 256 ? wanted : (wanted + 3) / 4;
+  const int64_t groups = threads == 256 ? wanted : (wanted + 1) / 2;
   const dim3 grid((unsigned)(groups < 1 ? 1 : groups > MAP_MOST_WORKGROUPS ? MAP_MOST_WORKGROUPS : groups));
   if (threads == 256) hipLaunchKernelGGL(block_map_kernel<256>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(block_map_kernel<1024>, grid, dim3(1024), 0, st, a);
