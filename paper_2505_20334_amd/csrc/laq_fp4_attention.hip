@@ -402,7 +402,8 @@ struct AttLds {
 };
 
 // The key tiles first .. end - 1 of a column.  EARLY_V: the next step's rows of V are asked for as soon as this step's are in LDS, not after their
-// products: 256 requests x 1024 rows 54.5 : 53.5 us, 64 of 2048 to 100 24.2 : 22.8; but where all places are taken for long 102 : 108 (96 x 6144).
+// products: 256 requests x 1024 rows 54.5 : 53.5 us, 64 of 2048 to 100 24.2 : 22.8; but where all places are taken for long 102 : 108 (96 x 6144),
+// unless registers leave few places: 64 of 8192 to 1000, d = 160 105 : 98, fp32 and 32 of d = 256 121 : 112, bf16 of d = 192 to 256 the same.
 template <typename T, int D32, int RT, int KT, bool ONCE, bool EARLY_V>
 __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int kv, int G, int first, int end, const AttColumn& col, AttLds<D32, RT>& sh) {
   const AttCall& k = anew(call);
@@ -865,7 +866,7 @@ __global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_at
     if (t1 > COLUMN_TURNS) {
       const int begin = at - t0, s0 = __builtin_amdgcn_readfirstlane(share_of(begin + COLUMN_TURNS));
       const int s1 = __builtin_amdgcn_readfirstlane(share_of(begin + turns - 1));
-      attend<T, D32, 1, KT, ONCE, false>(call, tl, kv, G, max(t0 - COLUMN_TURNS, 0) * (TURN / 16), min((t1 - COLUMN_TURNS) * (TURN / 16), (rows + 15) / 16),
+      attend<T, D32, 1, KT, ONCE, (D32 > 4)>(call, tl, kv, G, max(t0 - COLUMN_TURNS, 0) * (TURN / 16), min((t1 - COLUMN_TURNS) * (TURN / 16), (rows + 15) / 16),
                                   AttColumn{w - s0, s1 - s0 + 1, (size_t)2 * s0 + 1, (size_t)2 * (s0 + 1), 2}, sh);
       __syncthreads();
     }
