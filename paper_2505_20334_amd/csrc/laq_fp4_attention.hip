@@ -164,9 +164,13 @@ __device__ __forceinline__ bool find_tile(const Fp4View& c, const Fp4Attention& 
     // request i has the tiles from start[i] * G / TR + i on: never fewer than it needs
     const auto start = [&](int i) { return min(max(a.start[i], 0), (int)a.n_tokens); };
     int lo = 0, hi = a.n;
+    // 64 requests at a time: a trip to memory instead of six
     while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if ((int)((uint32_t)(start(mid) * G) / TR) + mid <= tile) lo = mid; else hi = mid;
+      const int step = (hi - lo + 63) / 64, i = lo + (int)(threadIdx.x & 63) * step;
+      const bool before = i < hi && (int)((uint32_t)(start(i) * G) / TR) + i <= tile;
+      const unsigned long long found = __ballot(before) | 1;
+      lo += (63 - __builtin_clzll(found)) * step;
+      hi = min(lo + step, hi);
     }
     out->inst = lo;
     out->token0 = start(lo);
@@ -915,14 +919,17 @@ AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_t
   const int TR = 16 * l.row_tiles, turn = ATT_WAVES * l.key_tiles * 16;
   l.plan = AttPlan{1, 0x7fffff00, (G + TR - 1) / TR, one_each && G < TR ? G : TR, turn / c.block_rows, turn % c.block_rows / 16};
   // Columns (as many as are surely there) and the turns of the longest.  As many ranges of a column as make the sum of what they take (a turn 2 us
-  // where few workgroups run) and what folding them takes (0.12 us each) least, as long as that makes no more than two workgroups a compute unit:
-  // that many saturate the memory, and more of them only fold more.  us, bf16, 8 heads of d = 128, with 1, 2, 4, 8, 16, 32, 64 ranges:
+  // where few workgroups run) and what folding them takes (0.12 us each for sums of 512 numbers, more in proportion: one workgroup reads them all)
+  // least, as long as that makes no more than two workgroups a compute unit: that many saturate the memory, and more of them only fold more.
+  // (8 heads on one, 2 x 14 tokens over 21836 and 7278 rows, d = 256 93 : 57 us with the sums' size counted, d = 128 48 : 34.)
+  // us, bf16, 8 heads of d = 128, with 1, 2, 4, 8, 16, 32, 64 ranges:
   //   1 x 4096 rows 37, 24, 17, 14, 12;  1 x 65536 503, 259, 136, 76, 43, 29, 28;  4 x 16384 133, 73, 42, 28, 23, 33, 42
   //   16 x 16384 140, 79, 53, 66, 67, 86, 121;  32 x 4096 41, 31, 40, 48, 59;  64 x 4096 53, 65, 67, 83, 109
   const long long tiles = one_each ? (long long)n * l.plan.tiles_per : n_tokens * G / TR + n;
   const long long columns = (one_each ? tiles : n_tokens * G / TR > n ? n_tokens * G / TR : n) * c.Hkv, turns = (max_rows + turn - 1) / turn;
   long long ranges = 1;
-  while (ranges < turns && ranges * ranges < 16 * turns && (ranges + 1) * columns <= 512) ++ranges;
+  const long long folded = l.plan.ws_rows * c.d > 512 ? l.plan.ws_rows * c.d : 512;
+  while (ranges < turns && ranges * (ranges + 1) * folded < 16 * 512 * turns && (ranges + 1) * columns <= 512) ++ranges;
   // Long calls of one token each and several requests are shared out evenly.  us, shared out : the best equal parts, requests of that many rows, and of
   // an eighth of that to that many: 8 x 65536 106 : 97, 73 : 92 (of 8);  16 x 16384 59 : 53, 42 : 51;  32 x 16384 101 : 98, 67 : 89;
   // 64 x 4096 59 : 53, 41 : 46;  128 x 4096 109 : 101, 68 : 73;  shorter: 8 x 16384 38 : 34, 30 : 32;  8 x 4096 22 : 18, 20 : 16.
