@@ -293,7 +293,8 @@ __device__ __forceinline__ size_t out_row(const Fp4Attention& a, const AttTile& 
 // Folds the ranges of a column, in their order, if all of them are finished (decode attention's way, laq_decode.hip): every range sets its marks
 // after its sums have been written and then looks at the marks of all.  Whoever finds all of them set clears them, so that a captured
 // launch, whose nonce is the same every time, never finds its own old ones; whatever else lies in the workspace is an unfinished range.
-// `sm`: room for FOLD marks.
+// `sm`: room for FOLD marks.  Several workgroups may find all of them set.  Where the marks fit, each has its copy from before anybody clears, and all write
+// the same values.  Where they do not, the fold reads them again, and one alone folds: the one that takes the column's first mark away.
 template <typename T, int FOLD>
 __device__ void fold_ranges(const Fp4View& c, const Fp4Attention& a, const AttPlan& p, const AttTile& tl, const AttParts& pa, const AttColumn& col, int kv,
                             int G, float2* sm) {
@@ -307,6 +308,17 @@ __device__ void fold_ranges(const Fp4View& c, const Fp4Attention& a, const AttPl
   }
   if (!__syncthreads_and(all)) return;
   const int pairs = c.d / 2, at_once = FOLD / R;           // ranges whose marks fit
+  const bool again = col.count > at_once;
+  uint32_t taken_ref = 0;                                  // thread 0: what the mark that it took away held
+  if (again) {
+    bool taken = false;
+    if (tid == 0) {
+      const unsigned long long was = __hip_atomic_exchange(pa.marks + col.slot(0) * p.ws_rows * 2, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      taken = (uint32_t)was == pa.nonce;
+      taken_ref = (uint32_t)(was >> 32);
+    }
+    if (!__syncthreads_or(taken)) return;
+  }
   // EU pairs of channels of a thread at a time, so that enough loads are under way: 16
   auto fold = [&](auto EUC) {
     constexpr int EU = decltype(EUC)::value;
@@ -323,11 +335,11 @@ __device__ void fold_ranges(const Fp4View& c, const Fp4Attention& a, const AttPl
       }
       for (int s0 = 0; s0 < col.count; s0 += at_once) {
         const int n = min(at_once, col.count - s0);
-        if (col.count > at_once) {
+        if (again) {
           __syncthreads();
           for (int i = tid; i < n * R; i += ATT_THREADS) {
             const unsigned long long* mark = pa.marks + (col.slot(s0 + i / R) * p.ws_rows + i % R) * 2;
-            sm[i] = float2{__uint_as_float(load_pair(mark).y), __uint_as_float(load_pair(mark + 1).y)};
+            sm[i] = float2{__uint_as_float(s0 + i == 0 ? taken_ref : load_pair(mark).y), __uint_as_float(load_pair(mark + 1).y)};
           }
           __syncthreads();
         }
@@ -370,7 +382,7 @@ __device__ void fold_ranges(const Fp4View& c, const Fp4Attention& a, const AttPl
   };
   if (R * pairs <= ATT_THREADS) fold(std::integral_constant<int, 1>{});
   else fold(std::integral_constant<int, 4>{});
-  if (col.count > at_once) __syncthreads();                // (the marks are read until here)
+  if (again) __syncthreads();                              // (this workgroup, the only one to fold, reads the marks until here)
   for (int i = tid; i < col.count * R; i += ATT_THREADS) {
     unsigned long long* mark = pa.marks + (col.slot(i / R) * p.ws_rows + i % R) * 2;
     store_pair(mark, 0, 0);

@@ -704,3 +704,40 @@ def test_one_table_row_of_a_request_shared_by_two():
     out, lse = c.run()
     torch.cuda.synchronize()
     assert torch.equal(out[0], out[1]) and torch.equal(lse[0], lse[1])
+
+
+# More ranges of a column than the fold has room for the marks of (288 of 16 rows with d >= 128, 160 with d = 64, 96 with d = 32): (dtype, Hq, H, d, lengths,
+# tokens).  Shared out: a turn of 256 rows (128 with d > 128) each, 768 shares.  Parts: the last two.
+MANY_RANGES = [(BF16, 16, 1, 64, [100000] + [100] * 40, 1), (BF16, 16, 1, 128, [100] * 9 + [131072] + [100] * 9, 1), (BF16, 16, 1, 256, [70000] + [1] * 31, 1),
+               (F32, 16, 1, 64, [100000] + [100] * 40, 1), (BF16, 16, 1, 32, [200000], 1), (BF16, 32, 4, 64, [262144], 4)]
+
+
+@pytest.mark.parametrize("dtype,Hq,H,d,rows,tokens", MANY_RANGES)
+def test_more_ranges_than_are_folded_at_once(dtype, Hq, H, d, rows, tokens):
+    print("case:", dtype, Hq, H, d, len(rows), max(rows), tokens, flush=True)
+    laq = _laq()
+    n = len(rows)
+    c = Case(dtype, Hq, H, d, 64, rows, [tokens] * n)
+    need = laq.laq_fp4_attention_workspace_bytes(c.cache, Hq, dtype, n, n * tokens, max(rows))
+    ws = torch.zeros(need, dtype=torch.uint8, device=DEV)
+    first = c.run(ws=ws)
+    torch.cuda.synchronize()
+    c.check(*first, what="eager")
+    for again in range(3):                            # same bits every time, whatever lies in the workspace
+        ws.random_(0, 256)
+        got = c.run(ws=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], first[0]) and torch.equal(got[1], first[1]), again
+    out, lse = torch.empty_like(c.qd), torch.empty(c.qd.shape[0], Hq, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run(out=out, lse=lse, ws=ws)
+    longest = rows.index(max(rows))
+    for replay in range(4):
+        c.qd.normal_()
+        c.rows_d[longest] = max(rows) - 9000 * replay
+        want = c.run()
+        out.fill_(3.0)
+        graph.replay()                                # on what the one before left in the workspace
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]), "replay %d" % replay
