@@ -495,8 +495,8 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
     } else {
 #pragma unroll
       for (int i = 1; i < KT; ++i) {
-        code_base[i] = code_base[0] + i * tile_codes;
-        scale_base[i] = scale_base[0] + i * tile_scales;
+        code_base[i] = code_base[i - 1] + tile_codes;      // (one at a time: three tiles' distance is more than 32 bits hold)
+        scale_base[i] = scale_base[i - 1] + tile_scales;
       }
       there = good ? (1u << left) - 1 : 0u;
     }

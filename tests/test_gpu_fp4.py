@@ -741,3 +741,27 @@ def test_more_ranges_than_are_folded_at_once(dtype, Hq, H, d, rows, tokens):
         graph.replay()                                # on what the one before left in the workspace
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1]), "replay %d" % replay
+
+
+@pytest.mark.parametrize("row", [100_000_000, 1 << 27])
+@pytest.mark.parametrize("dtype,d,tokens", [(BF16, 128, 1), (F32, 64, 1), (BF16, 96, 20), (BF16, 160, 1)])
+def test_rows_far_apart(row, dtype, d, tokens):
+    # a row-major pool [block_rows, blocks, heads, ..]: the tiles of a step (16 rows each, four of a block) begin up to 48 rows of 2^27 bytes apart
+    laq = _laq()
+    print("case:", row, dtype, d, tokens, flush=True)
+    H, br = 2, 64
+    c = Case(dtype, 8, H, d, br, [150, 70, 64], [tokens] * 3)
+    blocks = c.cache.k.shape[0]
+    buffer = torch.empty(br * row, dtype=torch.uint8, device=DEV)
+    planes, at = [], 0
+    for plane in c.cache:
+        w = plane.shape[3]
+        planes.append(buffer.as_strided(plane.shape, (H * w, w, row, 1), at))
+        planes[-1].copy_(plane)
+        at += -(-blocks * H * w // 16) * 16
+    near = c.run()
+    c.cache = laq.Fp4Cache(*planes)
+    out, lse = c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(out, near[0]) and torch.equal(lse, near[1])
+    c.check(out, lse)
