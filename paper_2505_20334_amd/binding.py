@@ -259,6 +259,20 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(stream, *sizes: int, dtype: torch.dtype, device) -> torch.Tensor:
+    """Memory for work on `stream` (None: the current one).  It is taken under that stream, so that no work of the current one on an earlier tensor
+    is still under way in it, and goes back to be reused when both have done what they had been given by then."""
+    if stream is None:
+        return torch.empty(*sizes, dtype=dtype, device=device)
+    here = torch.cuda.current_stream()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream)) if _stream(stream) else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        t = torch.empty(*sizes, dtype=dtype, device=device)
+    t.record_stream(here)
+    return t
+
+
 def _shape(n: int, Hq: int, Hkv: int, d: int, L: int, W: int, dtype: int, scale: float,
            q_pos: Optional[Sequence[int]] = None, keep: Optional[int] = None, pool_mode: str = "max",
            kv_strides: Tuple[int, int, int] = (0, 0, 0), paged=None, choose: str = "auto") -> _Shape:

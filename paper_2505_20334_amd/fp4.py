@@ -11,7 +11,7 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 import torch
 
 from . import binding
-from .binding import LaqError, _aligned, _budget_array, _cache, _dev, _dtype_code, _Fp4Cache, _out, _shape, _stream, load_library
+from .binding import LaqError, _aligned, _budget_array, _cache, _dev, _dtype_code, _empty, _Fp4Cache, _out, _shape, _stream, load_library
 
 
 class Fp4Cache(NamedTuple):
@@ -103,9 +103,9 @@ def laq_block_map(add: torch.Tensor, rows: torch.Tensor, block_table: torch.Tens
     _ints(block_table, "block_table", rows, n)
     _here(rows)
     if slots is None and n_slots is not None:
-        slots = torch.empty(n_slots, dtype=torch.int32, device=rows.device)
+        slots = _empty(stream, n_slots, dtype=torch.int32, device=rows.device)
     if start is None and n_slots is not None:
-        start = torch.empty(n + 1, dtype=torch.int32, device=rows.device)
+        start = _empty(stream, n + 1, dtype=torch.int32, device=rows.device)
     if slots is not None:
         _ints(slots, "slots", rows, n_slots or 0)
     if start is not None:
@@ -191,7 +191,7 @@ def laq_fp4_load(cache: Fp4Cache, slots: torch.Tensor, dtype: torch.dtype = torc
     out = []
     for t, name in ((k, "k"), (v, "v")):
         _out(t, name, dtype, T * c.Hkv * c.d, cache.k)
-        out.append(t if t is not None else torch.empty(T, c.Hkv, c.d, dtype=dtype, device=cache.k.device))
+        out.append(t if t is not None else _empty(stream, T, c.Hkv, c.d, dtype=dtype, device=cache.k.device))
     rc = lib.laq_fp4_load(ctypes.byref(c), _dtype_code(out[0]), T, slots.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), _stream(stream))
     if rc != 0:
         raise LaqError(rc, "laq_fp4_load")
@@ -235,9 +235,9 @@ def laq_fp4_attention(q: torch.Tensor, cache: Fp4Cache, block_table: torch.Tenso
     _out(out, "out", q.dtype, T * Hq * d, q)
     _out(lse, "lse", torch.float32, T * Hq, q)
     if out is None:
-        out = torch.empty(T, Hq, d, dtype=q.dtype, device=q.device)
+        out = _empty(stream, T, Hq, d, dtype=q.dtype, device=q.device)
     if lse is None and want_lse:
-        lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device)
+        lse = _empty(stream, T, Hq, dtype=torch.float32, device=q.device)
     code = _dtype_code(q)
     if ws is not None and (ws.device != q.device or not ws.is_contiguous()):
         raise ValueError("ws must be a dense tensor on %s" % q.device)
@@ -246,7 +246,7 @@ def laq_fp4_attention(q: torch.Tensor, cache: Fp4Cache, block_table: torch.Tenso
     elif ws is None:
         need = int(lib.laq_fp4_attention_workspace_bytes(ctypes.byref(c), Hq, code, n, T, most))
         if need:
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            ws = _empty(stream, need, dtype=torch.uint8, device=q.device)
     rc = lib.laq_fp4_attention(ctypes.byref(c), Hq, code, float(scale), n, T, start.data_ptr() if start is not None else None, q.data_ptr(), *strides,
                                block_table.data_ptr(), width, rows.data_ptr(), most, out.data_ptr(), lse.data_ptr() if lse is not None else None,
                                ws.data_ptr() if ws is not None else None, ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream))

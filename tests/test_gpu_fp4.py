@@ -765,3 +765,22 @@ def test_rows_far_apart(row, dtype, d, tokens):
     torch.cuda.synchronize()
     assert torch.equal(out, near[0]) and torch.equal(lse, near[1])
     c.check(out, lse)
+
+
+def test_a_workspace_outlives_the_call_on_another_stream():
+    # the stream is busy, the call returns, and the caller's stream takes memory of the workspace's size and fills it
+    laq = _laq()
+    c = Case(BF16, 8, 2, 128, 64, [30000], [1])
+    need = laq.laq_fp4_attention_workspace_bytes(c.cache, 8, BF16, 1, 1, 30000)
+    want = c.run()
+    side, busy = torch.cuda.Stream(), torch.randn(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    for handle in (side, side.cuda_stream):
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                busy = (busy @ busy).clamp(-1, 1)
+        got = c.run(stream=handle)
+        others = [torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        del others
