@@ -320,13 +320,13 @@ def laq_workspace_bytes(n_inst: int, Hq: int, Hkv: int, d: int, L: int, W: int, 
     return int(load_library().laq_workspace_bytes(ctypes.byref(sh)))
 
 
-def _workspace(q_win, k, ws, q_pos=None, keep=None, Hkv=None, L=None):
+def _workspace(q_win, k, ws, q_pos=None, keep=None, Hkv=None, L=None, stream=None):
     n, Hq, W, d = q_win.shape
     if Hkv is None:
         _, Hkv, L, _ = k.shape
     need = laq_workspace_bytes(n, Hq, Hkv, d, L, W, k.dtype, q_pos, keep)
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=k.device)
+        ws = _empty(stream, need, dtype=torch.uint8, device=k.device)
     elif ws.device != k.device or not ws.is_contiguous() or ws.data_ptr() % 256:
         raise ValueError("ws must be a dense, 256-byte aligned tensor on %s" % k.device)
     return ws, ws.numel() * ws.element_size()
@@ -350,8 +350,8 @@ def laq_score(q_win: torch.Tensor, k: torch.Tensor, pool_kernel: int = 1, scale:
     _aligned(q_win, "q_win"), _aligned(k, "k")
     _out(scores, "scores", torch.float32, n * Hkv * L, k)
     if scores is None:
-        scores = torch.empty(n, Hkv, L, dtype=torch.float32, device=k.device)
-    ws, ws_bytes = _workspace(q_win, k, ws, q_pos, keep, Hkv, L)
+        scores = _empty(stream, n, Hkv, L, dtype=torch.float32, device=k.device)
+    ws, ws_bytes = _workspace(q_win, k, ws, q_pos, keep, Hkv, L, stream)
     sh = _shape(n, Hq, Hkv, d, L, W, _dtype_code(k), scale, q_pos, keep, pool_mode, kvs, paged, choose)
     rc = lib.laq_score(ctypes.byref(sh), q_win.data_ptr(), k.data_ptr(), int(pool_kernel), scores.data_ptr(),
                        ws.data_ptr(), ws_bytes, _stream(stream))
@@ -372,7 +372,7 @@ def laq_select(scores: torch.Tensor, budget: Sequence[int], pool_kernel: int, ke
     total, _ = packed_rows(budget, Hkv, L)
     _out(idx, "idx", torch.int32, total, scores)
     if idx is None:
-        idx = torch.empty(total, dtype=torch.int32, device=scores.device)
+        idx = _empty(stream, total, dtype=torch.int32, device=scores.device)
     sh = _shape(n, Hkv, Hkv, 8, L, 1, LAQ_F32, 0.0, None, keep, pool_mode)
     rc = lib.laq_select(ctypes.byref(sh), scores.data_ptr(), _budget_array(budget, n), int(pool_kernel),
                         idx.data_ptr(), _stream(stream))
@@ -388,7 +388,7 @@ def laq_select_sink_recent(n_inst: int, Hkv: int, L: int, budget: Sequence[int],
     lib = load_library()
     total, _ = packed_rows(budget, Hkv, L)
     if idx is None:
-        idx = torch.empty(total, dtype=torch.int32, device=device if device is not None else "cuda:0")
+        idx = _empty(stream, total, dtype=torch.int32, device=device if device is not None else "cuda:0")
     _dev(idx, "idx")
     if idx.dtype != torch.int32 or idx.numel() < total:
         raise ValueError("idx must be int32 with at least %d entries" % total)
@@ -412,8 +412,8 @@ def laq_recall(idx_pred: torch.Tensor, budget_pred: Sequence[int], idx_gold: tor
         raise TypeError("index lists are int32")
     if idx_pred.numel() < packed_rows(budget_pred, Hkv, L)[0] or idx_gold.numel() < packed_rows(budget_gold, Hkv, L)[0]:
         raise ValueError("an index list is shorter than its budgets say")
-    overlap = torch.empty(n, Hkv, dtype=torch.int32, device=idx_pred.device)
-    recall = torch.empty(n, Hkv, dtype=torch.float32, device=idx_pred.device)
+    overlap = _empty(stream, n, Hkv, dtype=torch.int32, device=idx_pred.device)
+    recall = _empty(stream, n, Hkv, dtype=torch.float32, device=idx_pred.device)
     rc = lib.laq_recall(n, int(Hkv), int(L), idx_pred.data_ptr(), _budget_array(budget_pred, n),
                         idx_gold.data_ptr(), _budget_array(budget_gold, n), overlap.data_ptr(), recall.data_ptr(),
                         _stream(stream))
@@ -462,13 +462,13 @@ def laq_decode_attention(q: torch.Tensor, k_c: torch.Tensor, v_c: torch.Tensor, 
         raise ValueError("k_c / v_c must be the packed [rows, d] tensors of these budgets, in q's dtype")
     _out(out, "out", torch.float32, n * Hq * d, q)
     if out is None:
-        out = torch.empty(n, Hq, d, dtype=torch.float32, device=q.device)
+        out = _empty(stream, n, Hq, d, dtype=torch.float32, device=q.device)
     sh = _shape(n, Hq, Hkv, d, L, 1, _dtype_code(q), scale, None, 0)
     bud = _budget_array(budget, n)
     if split and ws is None:
         need = int(lib.laq_decode_workspace_bytes(ctypes.byref(sh), bud))
         if need:
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            ws = _empty(stream, need, dtype=torch.uint8, device=q.device)
     if not split:
         ws = None
     rc = lib.laq_decode_attention(ctypes.byref(sh), q.data_ptr(), k_c.data_ptr(), v_c.data_ptr(), bud, out.data_ptr(),
@@ -500,14 +500,14 @@ def laq_compact(k: torch.Tensor, v: Optional[torch.Tensor], idx: torch.Tensor, b
     _aligned(k, "k")
     _out(k_out, "k_out", k.dtype, total * d, k)
     if k_out is None:
-        k_out = torch.empty(total, d, dtype=k.dtype, device=k.device)
+        k_out = _empty(stream, total, d, dtype=k.dtype, device=k.device)
     if v is not None:
         if v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
             raise ValueError("k / v mismatch (shape, dtype or strides)")
         _aligned(v, "v")
         _out(v_out, "v_out", k.dtype, total * d, k)
         if v_out is None:
-            v_out = torch.empty(total, d, dtype=k.dtype, device=k.device)
+            v_out = _empty(stream, total, d, dtype=k.dtype, device=k.device)
     elif v_out is not None:
         raise ValueError("v_out without v")
     sh = _shape(n, Hkv, Hkv, d, L, 1, _dtype_code(k), 0.0, None, keep, "max", kvs, paged)
@@ -547,18 +547,18 @@ def laq_evict(q_win: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], b
     _out(idx, "idx", torch.int32, total, k)
     _out(k_out, "k_out", k.dtype, total * d, k)
     if scores is None and want_scores:
-        scores = torch.empty(n, Hkv, L, dtype=torch.float32, device=k.device)
+        scores = _empty(stream, n, Hkv, L, dtype=torch.float32, device=k.device)
     if idx is None:
-        idx = torch.empty(total, dtype=torch.int32, device=k.device)
+        idx = _empty(stream, total, dtype=torch.int32, device=k.device)
     if k_out is None:
-        k_out = torch.empty(total, d, dtype=k.dtype, device=k.device)
+        k_out = _empty(stream, total, d, dtype=k.dtype, device=k.device)
     if v is not None:
         if v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
             raise ValueError("k / v mismatch (shape, dtype or strides)")
         _aligned(v, "v")
         _out(v_out, "v_out", k.dtype, total * d, k)
         if v_out is None:
-            v_out = torch.empty(total, d, dtype=k.dtype, device=k.device)
+            v_out = _empty(stream, total, d, dtype=k.dtype, device=k.device)
     elif v_out is not None:
         raise ValueError("v_out without v")
     sh = _shape(n, Hq, Hkv, d, L, W, _dtype_code(k), scale, q_pos, keep, pool_mode, kvs, paged, choose)
@@ -570,7 +570,7 @@ def laq_evict(q_win: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], b
         if rc != 0:
             raise LaqError(rc, "laq_evict_static")
         return scores, idx, k_out, v_out
-    ws, ws_bytes = _workspace(q_win, k, ws, q_pos, keep, Hkv, L)
+    ws, ws_bytes = _workspace(q_win, k, ws, q_pos, keep, Hkv, L, stream)
     rc = lib.laq_evict(ctypes.byref(sh), q_win.data_ptr(), k.data_ptr(), v.data_ptr() if v is not None else None,
                        _budget_array(budget, n), int(pool_kernel),
                        scores.data_ptr() if scores is not None else None, idx.data_ptr(),
