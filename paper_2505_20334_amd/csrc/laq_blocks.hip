@@ -250,7 +250,7 @@ hipError_t launch_block_map(int n, int block_rows, int n_blocks, int width, cons
   const int64_t work = n_slots ? n_slots / 4 : n_blocks > 4096 ? n_blocks : 1, wanted = (work + 511) / 512;
   const int threads = n <= 256 && wanted < 4 ? 256 : 1024;
   const int shift = (block_rows & (block_rows - 1)) == 0 ? __builtin_ctz(block_rows) : -1;
-  const MapArgs a{n, block_rows, n_blocks, width, (n + threads - 1) / threads, shift, add, rows, table, list, state, start, slots, n_slots};
+  const MapArgs a{n, block_rows, n_blocks, width, (int)(((int64_t)n + threads - 1) / threads), shift, add, rows, table, list, state, start, slots, n_slots};
   const int64_t groups = threads == 256 ? wanted : (wanted + 1) / 2;
   const dim3 grid((unsigned)(groups < 1 ? 1 : groups > MAP_MOST_WORKGROUPS ? MAP_MOST_WORKGROUPS : groups));
   if (threads == 256) hipLaunchKernelGGL(block_map_kernel<256>, grid, dim3(256), 0, st, a);

@@ -456,7 +456,7 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
   // Block numbers are asked for a step ahead, so that their way does not lie in front of the codes'.  (Addresses of products of 32 bits: what is scalar in a step
   // takes a third of its instructions.)
   int number[KT];
-  const int last_block = max((tl.held + c.block_rows - 1) / c.block_rows - 1, 0);
+  const int last_block = max(tl.held - 1, 0) / c.block_rows;
   const bool straddles = per_block % KT != 0;              // a step's tiles may lie in several blocks
   const uint32_t tile_codes = (uint32_t)c.row * 16, tile_scales = (uint32_t)c.scale_row * 16;
   auto ask = [&](int b, int r) {
@@ -565,7 +565,7 @@ __device__ __forceinline__ void attend(AttCallPtr call, const AttTile& tl, int k
       });
     }
     const int key0 = at * 16;
-    const bool masked = key0 + KT * 16 > tl.seen_min || there_v != (1u << KT) - 1;
+    const bool masked = key0 > tl.seen_min - KT * 16 || there_v != (1u << KT) - 1;
     advance();
     if (at < end) {
       locate();
@@ -798,7 +798,8 @@ __global__ __launch_bounds__(ATT_THREADS, (RT > 1 && D32 <= 5 ? 2 : 1)) void fp4
   const int G = a.Hq / c.Hkv, kv = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, part = rest % p.parts, tile = rest / p.parts;
   AttTile tl;
   if (!find_tile<16 * RT>(c, a, p, tile, G, &tl)) return;
-  const int parts = min(p.parts, max((tl.seen_max + p.part_rows - 1) / p.part_rows, 1));
+  // (lengths come up to 2^31 - 16, and a part of all of them is as long: their sum is none of an int)
+  const int parts = min(p.parts, max((int)(((uint32_t)tl.seen_max + (uint32_t)p.part_rows - 1) / (uint32_t)p.part_rows), 1));
   if (part >= parts) return;
   const size_t slot = ((size_t)tile * c.Hkv + kv) * p.parts;
   attend<T, D32, RT, KT, ONCE, true>(call, tl, kv, G, part * p.part_rows / 16, part == parts - 1 ? (tl.seen_max + 15) / 16 : (part + 1) * p.part_rows / 16,
@@ -825,7 +826,7 @@ __global__ __launch_bounds__(ATT_THREADS, (SHARES_PER_UNIT<T, D32>)) void fp4_at
   const Fp4View& c = k.c;
   const Fp4Attention& a = k.a;
   const int tiles_per = k.p.tiles_per, G = a.Hq / c.Hkv, tid = threadIdx.x, lane = tid & 63, columns = c.Hkv * tiles_per;
-  const auto turns_of = [](int rows) { return max((rows + TURN - 1) / TURN, 1) + COLUMN_TURNS; };
+  const auto turns_of = [](int rows) { return max(rows - 1, 0) / TURN + 1 + COLUMN_TURNS; };
   int mine = 0;                          // (the launch sees to it that the sum of all is one)
   const int per = (a.n + ATT_THREADS - 1) / ATT_THREADS;
 #pragma unroll
@@ -938,7 +939,7 @@ AttLaunch plan_attention(const Fp4View& c, int Hq, int dtype, int n, int64_t n_t
   //   1 x 4096 rows 37, 24, 17, 14, 12;  1 x 65536 503, 259, 136, 76, 43, 29, 28;  4 x 16384 133, 73, 42, 28, 23, 33, 42
   //   16 x 16384 140, 79, 53, 66, 67, 86, 121;  32 x 4096 41, 31, 40, 48, 59;  64 x 4096 53, 65, 67, 83, 109
   const long long tiles = one_each ? (long long)n * l.plan.tiles_per : n_tokens * G / TR + n;
-  const long long columns = (one_each ? tiles : n_tokens * G / TR > n ? n_tokens * G / TR : n) * c.Hkv, turns = (max_rows + turn - 1) / turn;
+  const long long columns = (one_each ? tiles : n_tokens * G / TR > n ? n_tokens * G / TR : n) * c.Hkv, turns = ((long long)max_rows + turn - 1) / turn;
   long long ranges = 1;
   const long long folded = l.plan.ws_rows * c.d > 512 ? l.plan.ws_rows * c.d : 512;
   while (ranges < turns && ranges * (ranges + 1) * folded < 16 * 512 * turns && (ranges + 1) * columns <= 512) ++ranges;

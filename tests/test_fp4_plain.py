@@ -179,3 +179,12 @@ def test_batches_without_tokens_need_no_addresses():
     assert lib.laq_fp4_store(c, 3, 0, None, None, 0, 0, None, None) == INVALID
     assert lib.laq_fp4_load(c, 3, 0, None, None, None, None) == INVALID
     assert lib.laq_fp4_attention(c, 7, 1, 0.0, 2, 0, FAKE, None, 0, 0, FAKE, 4, FAKE, 64, None, None, None, 0, None) == INVALID
+
+
+def test_the_longest_bounds_are_planned_like_long_ones():
+    lib = laq.load_library()
+    c = ctypes.byref(_cache(n_blocks=4))
+    for Hq, n, T in ((2, 1, 1), (8, 1, 3), (8, 3, 3), (2, 40, 40)):
+        long = lib.laq_fp4_attention_workspace_bytes(c, Hq, 1, n, T, 1 << 30)
+        for most in ((1 << 31) - 4096, (1 << 31) - 255, (1 << 31) - 16):
+            assert lib.laq_fp4_attention_workspace_bytes(c, Hq, 1, n, T, most) >= long > 0

@@ -784,3 +784,37 @@ def test_a_workspace_outlives_the_call_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         del others
+
+
+@pytest.mark.parametrize("rows,tokens", [([(1 << 31) - 16], [1]), ([(1 << 31) - 16, 100, (1 << 31) - 20], [1, 1, 1]), ([(1 << 31) - 16, 50], [3, 2])])
+def test_as_many_rows_as_a_table_may_hold(rows, tokens):
+    """2^31 - 16 rows, 511 blocks of which the first 510 are one and the same: K = 0 and V = 1 there, V = 3 in the last one, whose last four rows have
+    logits of 51 more and V of their own.  A sum of weights is one of at most 2^17 ones a lane (exact) and of 16 lanes, 4 waves and 1024 ranges: e = 2^-13 of it and of the
+    numerator at most, twice that of out.  Logits are 36 * 0.1768 * 8 in 64 bits; the exponent's rounding of 2^-24 * 74 * 2 is 2^-16."""
+    laq = _laq()
+    print("case:", rows, tokens, flush=True)
+    br, width, d, n, tail = 16 * 262657, 511, 32, len(rows), [100.0, 200.0, 400.0, 800.0]
+    cache = laq.laq_fp4_cache(2, 1, br, d, DEV)
+    k, v = torch.zeros(2 * br, 1, d, device=DEV), torch.ones(2 * br, 1, d, device=DEV)
+    v[br:] = 3.0
+    k[-4:] = 6.0
+    v[-4:] = torch.tensor(tail, device=DEV)[:, None, None]
+    laq.laq_fp4_store(cache, k, v, torch.arange(2 * br, dtype=torch.int32, device=DEV))
+    tail = plain.values(*plain.quantise(v[-4:, 0].cpu()))[:, 0].tolist()
+    table = torch.zeros(n, width, dtype=torch.int32, device=DEV)
+    table[:, -1] = 1
+    T = sum(tokens)
+    start = None if T == n else torch.tensor([0] + tokens, dtype=torch.int32, device=DEV).cumsum(0).int()
+    out, lse = laq.laq_fp4_attention(torch.full((T, 1, d), 1.5, device=DEV), cache, table, torch.tensor(rows, dtype=torch.int32, device=DEV), start=start, want_lse=True)
+    torch.cuda.synchronize()
+    tok, logit = 0, 1.5 * 6.0 * d / math.sqrt(d)
+    for r, t in zip(rows, tokens):
+        for x in range(t):
+            seen = r - t + x + 1
+            ordinary = min(seen, br * width - 4)
+            weights = [(1.0, min(ordinary, br * 510)), (3.0, max(ordinary - br * 510, 0))] + [(value, math.exp(logit)) for value in tail[:seen - ordinary]]
+            total = sum(w for _, w in weights)
+            want = sum(value * w for value, w in weights) / total
+            assert (out[tok].cpu().double() - want).abs().max() <= 2.0 ** -12 * want, (r, x)
+            assert abs(lse[tok].item() - math.log(total)) <= 2.0 ** -12, (r, x)
+            tok += 1
