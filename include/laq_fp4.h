@@ -23,7 +23,8 @@
  * 2j + 1 in the high one.  Stored, a block's scale is 2^(floor(log2 a) - 2) for its largest magnitude a, twice that from
  * a = 1.75 * 2^floor(log2 a) on (where rounding to the nearest would reach 8), held within 2^-100 and 2^125 (a block of zeros: 2^-100);
  * every number is rounded to the nearest code, ties to the even one.  A block with an infinity or a NaN gets s = 255 and codes 0,
- * and stands for NaN.
+ * and stands for NaN.  Scales that the library never stores: 0 .. 26 are numbers like the others; of 253 and 254, laq_fp4_load gives what does not
+ * fit its type as infinities, and what laq_fp4_attention makes of requests that hold such rows is not defined.
  */
 #ifndef LAQ_FP4_H
 #define LAQ_FP4_H
@@ -128,7 +129,8 @@ int laq_fp4_load(const laq_fp4_cache *cache, int32_t dtype, int64_t n_tokens, co
  *                 With and without it the last bits of `out` may differ
  * A call that needs more than 2^24 workgroups (about n * Hkv of them, or n_tokens * Hq / 16) is LAQ_ERR_UNSUPPORTED.
  * bf16: the products of q and K are exact, sums, maxima and weights are fp32, weights are rounded to bf16 for the product with V, out
- * is rounded once.  fp32: q and weights as three bf16 parts each (2^-24), V exact, sums fp32.
+ * is rounded once.  fp32: q and weights as three bf16 parts each (2^-24), V exact, sums fp32.  Weights are up to 2^8 before they are divided by their sum: sums over
+ * numbers of V beyond 2^88 may overflow.
  */
 size_t laq_fp4_attention_workspace_bytes(const laq_fp4_cache *cache, int32_t Hq, int32_t dtype, int32_t n, int64_t n_tokens,
                                          int32_t max_rows);

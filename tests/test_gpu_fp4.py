@@ -818,3 +818,20 @@ def test_as_many_rows_as_a_table_may_hold(rows, tokens):
             assert (out[tok].cpu().double() - want).abs().max() <= 2.0 ** -12 * want, (r, x)
             assert abs(lse[tok].item() - math.log(total)) <= 2.0 ** -12, (r, x)
             tok += 1
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_every_scale_and_code_reads_as_its_number(dtype):
+    # row s: all codes with scale s; what the type does not hold is an infinity
+    laq = _laq()
+    cache = laq.laq_fp4_cache(16, 1, 16, 32, DEV)
+    codes = (torch.arange(0, 32, 2) % 16 + 16 * (torch.arange(1, 32, 2) % 16)).to(torch.uint8).expand(256, 16)
+    scales = torch.arange(256, dtype=torch.int32).to(torch.uint8)[:, None]
+    for plane, x in ((cache.k, codes), (cache.k_scale, scales), (cache.v, codes.flip(1)), (cache.v_scale, scales)):
+        plane.copy_(x.view(plane.shape).to(DEV))
+    got = laq.laq_fp4_load(cache, torch.arange(256, dtype=torch.int32, device=DEV), dtype)
+    torch.cuda.synchronize()
+    for y, x in zip(got, (codes, codes.flip(1))):
+        want = plain.values(x, scales).to(dtype).double()
+        assert torch.equal(torch.nan_to_num(y[:, 0].cpu().double(), nan=12345.0, posinf=math.inf, neginf=-math.inf),
+                           torch.nan_to_num(want, nan=12345.0, posinf=math.inf, neginf=-math.inf))
