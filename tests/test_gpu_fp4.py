@@ -835,3 +835,54 @@ def test_every_scale_and_code_reads_as_its_number(dtype):
         want = plain.values(x, scales).to(dtype).double()
         assert torch.equal(torch.nan_to_num(y[:, 0].cpu().double(), nan=12345.0, posinf=math.inf, neginf=-math.inf),
                            torch.nan_to_num(want, nan=12345.0, posinf=math.inf, neginf=-math.inf))
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("dtype,tokens,Hq,H,d,long", [(F32, 1, 4, 2, 64, 60), (F32, 5, 4, 2, 128, 60), (F32, 30, 4, 2, 64, 60), (F32, 20, 8, 2, 160, 60), (F32, 3, 4, 2, 256, 60),
+                                                      (F32, 6, 8, 2, 96, 3000), (F32, 1, 8, 2, 224, 3000), (BF16, 6, 8, 2, 128, 3000), (BF16, 40, 8, 2, 256, 3000)])
+def test_a_nan_of_any_row_reaches_those_that_see_it_alone(split, dtype, tokens, Hq, H, d, long):
+    # in V and in K; the last row, one that the first tokens do not see, and one that all see; whole columns and cut ones
+    laq = _laq()
+    print("case:", dtype, tokens, Hq, H, d, long, split, flush=True)
+    G, head, block = Hq // H, H - 1, d // 32 - 1
+    for nan_row in {long - 1, long - tokens // 2 - 1, long // 2}:
+        c = Case(dtype, Hq, H, d, 16, [50, long], [tokens, tokens])
+        clean = [x.cpu() for x in c.run(split=split)]
+        slot = torch.tensor([int(c.table[1, nan_row // 16]) * 16 + nan_row % 16], dtype=torch.int32, device=DEV)
+        bad = c.v[50 + nan_row][None].clone()
+        bad[0, head, 32 * block + 7] = math.nan
+        laq.laq_fp4_store(c.cache, None, bad.to(DEV), slot)
+        out, lse = (x.cpu() for x in c.run(split=split))
+        # (the other blocks of that head keep their bits, and so does everything else)
+        want = clean[0].clone().view(2, tokens, Hq, d)
+        sees = torch.arange(tokens) + long - tokens >= nan_row
+        assert sees.any()
+        want[1, sees, head * G:, 32 * block:32 * block + 32] = math.nan
+        assert torch.equal(torch.nan_to_num(out.double(), nan=777.0), torch.nan_to_num(want.view_as(out).double(), nan=777.0)), nan_row
+        assert torch.equal(lse, clean[1])
+        key = c.k[50 + nan_row][None].clone()
+        key[0, head, 0] = -math.inf
+        laq.laq_fp4_store(c.cache, key.to(DEV), c.v[50 + nan_row][None].to(DEV), slot)
+        out, lse = (x.cpu() for x in c.run(split=split))
+        want = clean[0].clone().view(2, tokens, Hq, d)
+        want[1, sees, head * G:] = math.nan
+        want_lse = clean[1].clone().view(2, tokens, Hq)
+        want_lse[1, sees, head * G:] = math.nan
+        assert torch.equal(torch.nan_to_num(out.double(), nan=777.0), torch.nan_to_num(want.view_as(out).double(), nan=777.0)), nan_row
+        assert torch.equal(torch.nan_to_num(lse, nan=777.0), torch.nan_to_num(want_lse.view_as(lse), nan=777.0)), nan_row
+
+
+@pytest.mark.parametrize("dtype,d", [(F32, 64), (F32, 128), (F32, 256), (BF16, 256)])
+def test_infinite_and_nan_queries_of_any_type_stay_with_their_own_head(dtype, d):
+    for rows, tokens in (([100, 40], [3, 1]), ([2500, 40], [1, 1]), ([300, 90], [30, 20])):
+        c = Case(dtype, 8, 2, d, 16, rows, tokens)
+        want = [x.cpu() for x in c.run()]
+        q, last = c.qd.clone(), sum(tokens) - 1
+        q[0, 2, 5] = math.nan
+        q[last, 7, 9] = math.inf
+        c.qd = q
+        got = [x.cpu() for x in c.run()]
+        same = torch.ones(last + 1, 8, dtype=torch.bool)
+        same[0, 2] = same[last, 7] = False
+        assert torch.equal(got[0][same], want[0][same]) and torch.equal(got[1][same], want[1][same])
+        assert torch.isnan(got[0][0, 2]).all() and torch.isnan(got[0][last, 7]).all() and torch.isnan(got[1][0, 2]) and torch.isnan(got[1][last, 7])
