@@ -11,8 +11,8 @@
 // host expects, where there would be too few workgroups otherwise (fp4_attention_parts).
 //
 // Bound: single tokens, the cache's bytes (68 a row of d = 128, K and V each): 96 x 8 heads x 6144 rows 6.3 TB/s, 128 x 8 heads x 2048 to 8192
-// rows 5.7 TB/s; the conversions are a quarter of what the vector units could do meanwhile.  Chunks of a prompt, the vector units beside the
-// matrix cores (exponentials, conversions, packing): 4 x 512 tokens x 32 heads over 8704 rows 213 us, 876 TFLOP/s.
+// rows 5.7 TB/s; the vector units are busy a third of the time.  Chunks of a prompt, the vector units beside the matrix cores (exponentials,
+// conversions, packing): 4 x 512 tokens x 32 heads over 2100 to 8704 rows 212 us, 880 TFLOP/s, vector units busy 50 % of the time, matrix cores 34 %.
 //
 // Products are 16 x 16 x 32 bf16 with the keys as the first operand's rows, so that a lane has four keys of one score row (column n = lane % 16)
 // and all that belongs to a row lies in lanes n, n + 16, n + 32, n + 48:
@@ -238,7 +238,8 @@ __device__ __forceinline__ void read_queries(const Fp4Attention& a, const AttTil
   }
 }
 
-// The sum of eight weights' parts: four of one key tile, four of the next.
+// The sum of eight weights' parts: four of one key tile, four of the next.  bf16: one part, rounded as the operand has it.  A result is then 0.0023 of its size
+// from 64 bits, 0.0017 of which its own rounding makes; a second part would double the products with V for the rest.
 template <typename T>
 __device__ __forceinline__ void split_weights(const f32x4& a, const f32x4& b, u32x4 (&p)[PARTS_OF<T>]) {
   if constexpr (is_f32(T())) {
