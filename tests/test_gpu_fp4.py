@@ -886,3 +886,36 @@ def test_infinite_and_nan_queries_of_any_type_stay_with_their_own_head(dtype, d)
         same[0, 2] = same[last, 7] = False
         assert torch.equal(got[0][same], want[0][same]) and torch.equal(got[1][same], want[1][same])
         assert torch.isnan(got[0][0, 2]).all() and torch.isnan(got[0][last, 7]).all() and torch.isnan(got[1][0, 2]) and torch.isnan(got[1][last, 7])
+
+
+def test_long_folds_of_two_streams_and_of_graphs_that_share_a_workspace():
+    laq = _laq()
+    cases = [Case(BF16, 16, 1, 64, 64, [100000] + [100] * 40, [1] * 41), Case(BF16, 16, 1, 32, 64, [200000], [1], seed=2), Case(BF16, 8, 2, 128, 64, [3000, 17], [1, 1], seed=3)]
+    want = [c.run() for c in cases]
+    torch.cuda.synchronize()
+    sides, got = [torch.cuda.Stream() for _ in cases], [[] for _ in cases]
+    for _ in range(6):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(sides[i]):
+                got[i].append(c.run())
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for w, several in zip(want, got) for g in several for x, y in zip(w, g))
+    need = [laq.laq_fp4_attention_workspace_bytes(c.cache, c.Hq, BF16, len(c.rows), c.qd.shape[0], max(c.rows)) for c in cases]
+    ws = torch.zeros(max(need), dtype=torch.uint8, device=DEV)
+    graphs, outs = [], []
+    for c in cases:
+        outs.append((torch.empty_like(c.qd), torch.empty(c.qd.shape[0], c.Hq, device=DEV)))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.run(out=outs[-1][0], lse=outs[-1][1], ws=ws)
+        graphs.append(graph)
+    for order in ((0, 1, 2), (1, 1, 0, 2, 0), (2, 0, 1)):
+        for c in cases:
+            c.qd.normal_()
+        want = [c.run() for c in cases]
+        for i in order:
+            outs[i][0].fill_(3.0)
+            graphs[i].replay()
+            cases[(i + 1) % 3].run(ws=ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for w, o in zip(want, outs) for x, y in zip(w, o)), order
