@@ -919,3 +919,47 @@ def test_long_folds_of_two_streams_and_of_graphs_that_share_a_workspace():
             cases[(i + 1) % 3].run(ws=ws)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for w, o in zip(want, outs) for x, y in zip(w, o)), order
+
+
+@pytest.mark.parametrize("dtype,Hq,H,d,rows", [(BF16, 320, 8, 64, [5700, 100] * 8), (F32, 160, 8, 32, [5700, 0, 3, 900] * 5), (BF16, 132, 4, 192, [3000, 2900, 1] * 8)])
+def test_shared_out_requests_of_several_tiles(dtype, Hq, H, d, rows):
+    # 40, 20 and 33 query heads a KV head: tiles of 16, the last ones short
+    print("case:", dtype, Hq, H, d, flush=True)
+    c = Case(dtype, Hq, H, d, 32, rows, [1] * len(rows))
+    first = c.run()
+    torch.cuda.synchronize()
+    c.check(*first)
+    again = c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_replayed_maps_of_many_workgroups():
+    # as many slots as 16 workgroups and more have, appended and dropped in a captured launch each
+    laq = _laq()
+    n, br, n_blocks, width = 300, 16, 20000, 80
+    gen = torch.Generator().manual_seed(4)
+    adds = [torch.randint(0, 500, (n,), generator=gen).int().to(DEV) for _ in range(2)]
+    state_of = lambda: (torch.zeros(n, dtype=torch.int32, device=DEV), torch.full((n, width), -1, dtype=torch.int32, device=DEV), *laq.laq_block_pool(n_blocks, DEV))  # noqa: E731
+    eager, replayed = state_of(), state_of()
+    add, back = torch.zeros_like(adds[0]), torch.zeros_like(adds[0])
+    start, slots = torch.empty(n + 1, dtype=torch.int32, device=DEV), torch.empty(160000, dtype=torch.int32, device=DEV)
+    saved = [t.clone() for t in replayed]
+    laq.laq_block_map(add, *replayed, br, start=start, slots=slots)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        laq.laq_block_map(add, *replayed, br, start=start, slots=slots)
+        laq.laq_block_map(back, *replayed, br)
+    for t, s in zip(replayed, saved):
+        t.copy_(s)
+    for replay in range(5):
+        add.copy_(adds[replay % 2])
+        back.copy_(-(adds[replay % 2] // 2))
+        graph.replay()
+        want = laq.laq_block_map(add, *eager, br, n_slots=160000)
+        laq.laq_block_map(back, *eager, br)
+        torch.cuda.synchronize()
+        assert torch.equal(start, want[0]) and torch.equal(slots, want[1]), replay
+        assert torch.equal(replayed[0], eager[0]) and torch.equal(replayed[1], eager[1]) and torch.equal(replayed[3], eager[3])
+        held = eager[3][0].item()
+        assert torch.equal(replayed[2][:held], eager[2][:held])
