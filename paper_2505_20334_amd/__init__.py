@@ -9,7 +9,11 @@ from .binding import (LaqError, laq_compact, laq_init, laq_workspace_status, laq
                       laq_select_sink_recent, laq_strerror, laq_workspace_bytes, lib_path, load_library, packed_rows)
 from .fp4 import (Fp4Cache, laq_block_map, laq_block_pool, laq_fp4_attention, laq_fp4_attention_workspace_bytes, laq_fp4_cache,  # noqa: F401
                   laq_fp4_compact, laq_fp4_load, laq_fp4_store)
+from .paged import (PagedCache, Rope, laq_cache, laq_cache_append, laq_cache_attention, laq_cache_attention_workspace_bytes, laq_cache_compact,  # noqa: F401
+                    laq_cache_load, laq_rope, laq_rope_frequencies)
 
 __all__ = ["LaqError", "laq_compact", "laq_init", "laq_workspace_status", "laq_score_kernel", "laq_decode_attention", "laq_decode_workspace_bytes", "laq_evict", "laq_qcache_store", "laq_recall", "laq_score", "laq_select", "laq_select_sink_recent", "laq_strerror",
            "laq_workspace_bytes", "lib_path", "load_library", "packed_rows", "Fp4Cache", "laq_block_map", "laq_block_pool", "laq_fp4_attention",
-           "laq_fp4_attention_workspace_bytes", "laq_fp4_cache", "laq_fp4_compact", "laq_fp4_load", "laq_fp4_store"]
+           "laq_fp4_attention_workspace_bytes", "laq_fp4_cache", "laq_fp4_compact", "laq_fp4_load", "laq_fp4_store",
+           "PagedCache", "Rope", "laq_cache", "laq_cache_append", "laq_cache_attention", "laq_cache_attention_workspace_bytes", "laq_cache_compact",
+           "laq_cache_load", "laq_rope", "laq_rope_frequencies"]

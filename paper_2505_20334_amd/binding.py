@@ -39,6 +39,20 @@ class _Fp4Cache(ctypes.Structure):
                                                        "scale_stride_head", "scale_stride_row")])
 
 
+class _PagedCache(ctypes.Structure):
+    _fields_ = ([(name, ctypes.c_void_p) for name in ("k", "v", "k_scale", "v_scale")]
+                + [(name, ctypes.c_int32) for name in ("n_blocks", "Hkv", "block_rows", "d", "type")]
+                + [(name, ctypes.c_int64) for name in ("stride_block", "stride_head", "stride_row")])
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("heads", ctypes.c_int32), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
+class _RopePlan(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot", ctypes.c_int32), ("layout", ctypes.c_int32), ("mscale", ctypes.c_float)]
+
+
 class _Shape(ctypes.Structure):
     _fields_ = [("n_inst", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("L", ctypes.c_int32), ("W", ctypes.c_int32),
@@ -116,6 +130,19 @@ def load_library() -> ctypes.CDLL:
     lib.laq_fp4_attention_workspace_bytes.restype = sz
     lib.laq_fp4_attention.argtypes = [cp, i32, i32, ctypes.c_float, i32, i64, vp, vp, i64, i64, vp, i32, vp, i32, vp, vp, vp, sz, vp]
     lib.laq_fp4_attention.restype = i32
+    pp, hp, rp = ctypes.POINTER(_PagedCache), ctypes.POINTER(_Heads), ctypes.POINTER(_RopePlan)
+    lib.laq_rope.argtypes = [rp, i32, i64, i32, hp, hp, vp, hp, hp, vp]
+    lib.laq_rope.restype = i32
+    lib.laq_cache_append.argtypes = [pp, i32, i64, hp, hp, vp, rp, vp, hp, hp, vp]
+    lib.laq_cache_append.restype = i32
+    lib.laq_cache_compact.argtypes = [sp, vp, vp, vp, bp, pp, vp, vp]
+    lib.laq_cache_compact.restype = i32
+    lib.laq_cache_load.argtypes = [pp, i32, i64, vp, vp, vp, vp]
+    lib.laq_cache_load.restype = i32
+    lib.laq_cache_attention_workspace_bytes.argtypes = [pp, i32, i32, i32, i64, i32]
+    lib.laq_cache_attention_workspace_bytes.restype = sz
+    lib.laq_cache_attention.argtypes = [pp, i32, ctypes.c_float, i32, i64, vp, hp, vp, i32, vp, i32, vp, vp, vp, sz, vp]
+    lib.laq_cache_attention.restype = i32
     try:
         from . import _native as native
     except ImportError as exc:          # not built, or built against another torch: ctypes serves every call
