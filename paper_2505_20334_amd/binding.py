@@ -1,7 +1,7 @@
 """Binding of ``liblaq.so`` -- argument marshalling only.
 
 The calls that sit in a model's loop (laq_evict, laq_decode_attention, laq_qcache_store, and those of
-``fp4``) are marshalled by the extension module ``_native`` (csrc/laq_native.cpp); ctypes serves the others, and
+``fp4`` and ``paged``) are marshalled by the extension module ``_native`` (csrc/laq_native.cpp); ctypes serves the others, and
 these where an argument is out of the ordinary or the module cannot be loaded.
 
 Function names and argument meaning follow ``include/laq.h``.  Tensors are torch
@@ -156,6 +156,8 @@ def load_library() -> ctypes.CDLL:
                     torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
         native.bind_fp4(address("laq_block_map"), address("laq_fp4_store"), address("laq_fp4_compact"), address("laq_fp4_load"),
                         address("laq_fp4_attention"), address("laq_fp4_attention_workspace_bytes"))
+        native.bind_cache(address("laq_rope"), address("laq_cache_append"), address("laq_cache_compact"), address("laq_cache_load"),
+                          address("laq_cache_attention"), address("laq_cache_attention_workspace_bytes"))
         _native = native
     _lib = lib
     return lib

@@ -1,11 +1,11 @@
-// Python binding of the calls that sit in a model's loop (laq_evict, laq_decode_attention, laq_qcache_store, and those of the
-// 4-bit cache) as a CPython extension: the marshalling of binding.py and fp4.py in C++.
+// Python binding of the calls that sit in a model's loop (laq_evict, laq_decode_attention, laq_qcache_store, those of the 4-bit cache, rotary
+// positions and the paged cache) as a CPython extension: the marshalling of binding.py, fp4.py and paged.py in C++.
 //
 // A small call is bound by the host: the kernels of one layer's step take a few microseconds, and what
 // Python spends on unpacking tensors, filling ctypes structures and making output tensors took 10 us per
 // decode call and 20 us per eviction; here it is 2 to 4.
 //
-// Every function takes exactly what its namesake in binding.py or fp4.py takes (positionally, defaults filled in
+// Every function takes exactly what its namesake in binding.py, fp4.py or paged.py takes (positionally, defaults filled in
 // there) and returns None for anything out of the ordinary -- a tensor of another type, device or layout,
 // an argument that is not a plain number, anything that throws (no memory for an output, a tensor without an
 // address) -- without having launched anything: binding.py then walks its own checks and raises what it always
@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "laq.h"
+#include "laq_cache.h"
 #include "laq_fp4.h"
 
 namespace {
@@ -36,6 +37,12 @@ decltype(&laq_fp4_compact) fn_fp4_compact;
 decltype(&laq_fp4_load) fn_fp4_load;
 decltype(&laq_fp4_attention) fn_fp4_attention;
 decltype(&laq_fp4_attention_workspace_bytes) fn_fp4_attention_workspace_bytes;
+decltype(&laq_rope) fn_rope;
+decltype(&laq_cache_append) fn_cache_append;
+decltype(&laq_cache_compact) fn_cache_compact;
+decltype(&laq_cache_load) fn_cache_load;
+decltype(&laq_cache_attention) fn_cache_attention;
+decltype(&laq_cache_attention_workspace_bytes) fn_cache_attention_workspace_bytes;
 PyObject* get_device;      // torch._C._cuda_getDevice
 PyObject* get_stream;      // torch._C._cuda_getCurrentRawStream
 
@@ -628,6 +635,306 @@ PyObject* bind_fp4(PyObject*, PyObject* args) {
   Py_RETURN_NONE;
 }
 
+// ---- rotary positions and the paged cache --------------------------------------------------
+
+// a PagedCache: its tensors, and what the library takes
+bool paged_cache(PyObject* o, laq_cache* c, const at::Tensor** first) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
+  const at::Tensor *k = gpu_tensor(PyTuple_GET_ITEM(o, 0)), *v = gpu_tensor(PyTuple_GET_ITEM(o, 2));
+  if (!k || !v || k->dim() != 4 || k->stride(3) != 1 || v->scalar_type() != k->scalar_type() || v->device() != k->device() || v->sizes() != k->sizes() ||
+      v->strides() != k->strides())
+    return false;
+  for (int x = 0; x < 4; ++x)
+    if (k->size(x) > INT32_MAX) return false;
+  memset(c, 0, sizeof *c);
+  const bool scaled = k->scalar_type() == at::kFloat8_e4m3fn;
+  c->type = scaled ? LAQ_E4M3 : dtype_code(*k);
+  if (c->type < 0) return false;
+  for (int i = 0; i < 2; ++i) {
+    PyObject* s = PyTuple_GET_ITEM(o, 2 * i + 1);
+    if (!scaled) {
+      if (!is_none(s)) return false;
+      continue;
+    }
+    const at::Tensor* t = gpu_tensor(s);
+    if (!t || t->scalar_type() != at::kByte || t->device() != k->device() || !t->is_contiguous() || t->dim() != 3) return false;
+    for (int x = 0; x < 3; ++x)
+      if (t->size(x) != k->size(x)) return false;
+    (i ? c->v_scale : c->k_scale) = static_cast<uint8_t*>(t->data_ptr());
+  }
+  c->k = k->data_ptr();
+  c->v = v->data_ptr();
+  c->n_blocks = (int32_t)k->size(0);
+  c->Hkv = (int32_t)k->size(1);
+  c->block_rows = (int32_t)k->size(2);
+  c->d = (int32_t)k->size(3);
+  if (c->block_rows < 1) return false;
+  if (!k->is_contiguous()) {
+    c->stride_block = k->stride(0);
+    c->stride_head = k->stride(1);
+    c->stride_row = k->stride(2);
+  }
+  *first = k;
+  return true;
+}
+
+// [n_tokens, heads, d] in the type and on the device of `like`; false: not that
+bool heads_of(const at::Tensor* t, const at::Tensor& like, int64_t n_tokens, int64_t d, laq_heads* h) {
+  if (!token_rows(t, like.device(), d, &h->stride_token, &h->stride_head) || t->scalar_type() != like.scalar_type() || t->size(0) != n_tokens ||
+      t->size(1) > INT32_MAX)
+    return false;
+  h->x = t->data_ptr();
+  h->heads = (int32_t)t->size(1);
+  return true;
+}
+
+// a Rope and its positions
+bool rope_of(PyObject* o, const at::Device& dev, laq_rope_plan* plan) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) return false;
+  const at::Tensor* f = gpu_tensor(PyTuple_GET_ITEM(o, 0));
+  PyObject *layout = PyTuple_GET_ITEM(o, 1), *mscale = PyTuple_GET_ITEM(o, 2);
+  if (!f || f->device() != dev || f->scalar_type() != at::kFloat || f->dim() != 1 || !f->is_contiguous() || f->numel() > 128 || !PyFloat_CheckExact(mscale)) return false;
+  const bool half = is_text(layout, "half");
+  if (!half && !is_text(layout, "interleaved")) return false;
+  plan->inv_freq = static_cast<const float*>(f->data_ptr());
+  plan->rot = (int32_t)(2 * f->numel());
+  plan->layout = half ? LAQ_ROPE_HALF : LAQ_ROPE_INTERLEAVED;
+  plan->mscale = (float)PyFloat_AS_DOUBLE(mscale);
+  return true;
+}
+
+// rope(q, k, positions, rope, q_out, k_out) -> (q_out, k_out) | error code | None
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  try {
+    if (n_args != 6) return none();
+    const at::Tensor* x[2];
+    for (int i = 0; i < 2; ++i) {
+      x[i] = is_none(a[i]) ? nullptr : gpu_tensor(a[i]);
+      if ((!x[i] && !is_none(a[i])) || (!x[i] && !is_none(a[4 + i]))) return none();
+    }
+    const at::Tensor* like = x[0] ? x[0] : x[1];
+    if (!like || like->dim() != 3) return none();
+    const int64_t T = like->size(0), d = like->size(2);
+    const at::Device dev = like->device();
+    laq_rope_plan plan;
+    laq_heads in[2] = {}, out[2] = {};
+    if (d > 256 || !rope_of(a[3], dev, &plan)) return none();
+    const at::Tensor* positions = ints(a[2], dev, T);
+    if (!positions) return none();
+    for (int i = 0; i < 2; ++i) {
+      if (x[i] && !heads_of(x[i], *like, T, d, &in[i])) return none();
+      if (is_none(a[4 + i])) continue;
+      const at::Tensor* o = gpu_tensor(a[4 + i]);
+      if (!heads_of(o, *like, T, d, &out[i]) || out[i].heads != in[i].heads) return none();
+    }
+    void* stream;
+    if (!stream_on(dev, &stream)) return PyErr_Occurred() ? nullptr : none();
+    at::Tensor made[2];
+    for (int i = 0; i < 2; ++i)
+      if (x[i] && is_none(a[4 + i])) {
+        made[i] = make(x[i]->sizes(), x[i]->scalar_type(), *x[i]);
+        out[i] = laq_heads{made[i].data_ptr(), in[i].heads, 0, 0};
+      }
+    int rc;
+    const int dt = dtype_code(*like);
+    const int32_t* pp = positions->data_ptr<int32_t>();
+    Py_BEGIN_ALLOW_THREADS;
+    rc = fn_rope(&plan, dt, T, (int32_t)d, x[0] ? &in[0] : nullptr, x[1] ? &in[1] : nullptr, pp, x[0] ? &out[0] : nullptr, x[1] ? &out[1] : nullptr, stream);
+    Py_END_ALLOW_THREADS;
+    if (rc != LAQ_OK) return PyLong_FromLong(rc);
+    return pair(own_or_made(a[4], &made[0]), own_or_made(a[5], &made[1]));
+  } catch (const std::exception&) {
+    return thrown();
+  }
+}
+
+// cache_append(cache, k, v, slots, q, positions, rope, q_out) -> (q_out or None,) | error code | None
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  try {
+    if (n_args != 8) return none();
+    laq_cache c;
+    const at::Tensor *first, *k = is_none(a[1]) ? nullptr : gpu_tensor(a[1]), *v = is_none(a[2]) ? nullptr : gpu_tensor(a[2]);
+    if (!paged_cache(a[0], &c, &first) || (!k && !is_none(a[1])) || (!v && !is_none(a[2])) || (!k && !v)) return none();
+    const at::Device dev = first->device();
+    const at::Tensor& like = k ? *k : *v;
+    if (like.device() != dev || like.dim() != 3) return none();
+    const int64_t T = like.size(0);
+    laq_heads hk = {}, hv = {}, hq = {}, ho = {};
+    if ((k && (!heads_of(k, like, T, c.d, &hk) || hk.heads != c.Hkv)) || (v && (!heads_of(v, like, T, c.d, &hv) || hv.heads != c.Hkv))) return none();
+    const at::Tensor *slots = ints(a[3], dev, T), *q = is_none(a[4]) ? nullptr : gpu_tensor(a[4]), *positions = nullptr;
+    if (!slots || (!q && !is_none(a[4]))) return none();
+    laq_rope_plan plan;
+    const bool turned = !is_none(a[6]);
+    if (turned ? !rope_of(a[6], dev, &plan) || !(positions = ints(a[5], dev, T)) : q || !is_none(a[5])) return none();
+    if ((q && !heads_of(q, like, T, c.d, &hq)) || (!q && !is_none(a[7]))) return none();
+    if (!is_none(a[7]) && (!heads_of(gpu_tensor(a[7]), like, T, c.d, &ho) || ho.heads != hq.heads)) return none();
+    void* stream;
+    if (!stream_on(dev, &stream)) return PyErr_Occurred() ? nullptr : none();
+    at::Tensor made;
+    if (q && is_none(a[7])) {
+      made = make(q->sizes(), q->scalar_type(), *q);
+      ho = laq_heads{made.data_ptr(), hq.heads, 0, 0};
+    }
+    int rc;
+    const int dt = dtype_code(like);
+    const int32_t *sp = slots->data_ptr<int32_t>(), *pp = positions ? positions->data_ptr<int32_t>() : nullptr;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = fn_cache_append(&c, dt, T, k ? &hk : nullptr, v ? &hv : nullptr, sp, turned ? &plan : nullptr, pp, q ? &hq : nullptr, q ? &ho : nullptr, stream);
+    Py_END_ALLOW_THREADS;
+    if (rc != LAQ_OK) return PyLong_FromLong(rc);
+    PyObject* o = own_or_made(a[7], &made);
+    if (!o) return nullptr;
+    PyObject* res = PyTuple_Pack(1, o);
+    Py_DECREF(o);
+    return res;
+  } catch (const std::exception&) {
+    return thrown();
+  }
+}
+
+// cache_compact(cache, k, v, idx, budget, slots) -> True | error code | None (paged sources: paged.py)
+PyObject* cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  try {
+    if (n_args != 6) return none();
+    laq_cache c;
+    const at::Tensor *first, *k = gpu_tensor(a[1]), *v = is_none(a[2]) ? nullptr : gpu_tensor(a[2]);
+    if (!paged_cache(a[0], &c, &first) || !k || (!v && !is_none(a[2])) || k->dim() != 4 || k->stride(3) != 1) return none();
+    const at::Device dev = first->device();
+    const int dt = dtype_code(*k);
+    std::vector<int32_t> budget;
+    int64_t rows = 0;
+    const int64_t n = k->size(0), L = k->size(2);
+    if (dt < 0 || k->device() != dev || k->size(1) != c.Hkv || k->size(3) != c.d || !aligned(*k) || n < 1 || n > INT32_MAX || L > INT32_MAX ||
+        !as_ints(a[4], &budget) || (int64_t)budget.size() != n || !packed_rows(budget, 1, L, &rows))
+      return none();
+    if (v && (v->scalar_type() != k->scalar_type() || v->device() != dev || v->sizes() != k->sizes() || v->strides() != k->strides() || !aligned(*v))) return none();
+    const at::Tensor *idx = ints(a[3], dev, rows * c.Hkv), *slots = ints(a[5], dev, rows);
+    if (!idx || !slots) return none();
+    laq_shape sh;
+    memset(&sh, 0, sizeof sh);
+    sh.n_inst = (int32_t)n; sh.Hq = sh.Hkv = c.Hkv; sh.d = c.d; sh.L = (int32_t)L; sh.W = 1; sh.dtype = dt;
+    if (!k->is_contiguous()) {
+      sh.kv_stride_inst = k->stride(0);
+      sh.kv_stride_head = k->stride(1);
+      sh.kv_stride_row = k->stride(2);
+    }
+    void* stream;
+    if (!stream_on(dev, &stream)) return PyErr_Occurred() ? nullptr : none();
+    int rc;
+    const void *kp = k->data_ptr(), *vp = v ? v->data_ptr() : nullptr;
+    const int32_t *ip = idx->data_ptr<int32_t>(), *sp = slots->data_ptr<int32_t>();
+    Py_BEGIN_ALLOW_THREADS;
+    rc = fn_cache_compact(&sh, kp, vp, ip, budget.data(), &c, sp, stream);
+    Py_END_ALLOW_THREADS;
+    if (rc != LAQ_OK) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+  } catch (const std::exception&) {
+    return thrown();
+  }
+}
+
+// cache_load(cache, slots, dtype, k, v) -> (k, v) | error code | None
+PyObject* cache_load(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  try {
+    if (n_args != 5) return none();
+    laq_cache c;
+    const at::Tensor* first;
+    if (!paged_cache(a[0], &c, &first) || !THPDtype_Check(a[2])) return none();
+    const at::Device dev = first->device();
+    const at::ScalarType type = reinterpret_cast<THPDtype*>(a[2])->scalar_type;
+    const at::Tensor* slots = ints(a[1], dev, 0);
+    if (!slots || (type != at::kBFloat16 && type != at::kFloat)) return none();
+    const int64_t n_tokens = slots->numel();
+    const at::Tensor* out[2] = {};
+    at::Tensor made[2];
+    for (int i = 0; i < 2; ++i)
+      if (!is_none(a[3 + i]) && !(out[i] = output(a[3 + i], type, n_tokens * c.Hkv * c.d, *first))) return none();
+    void* stream;
+    if (!stream_on(dev, &stream)) return PyErr_Occurred() ? nullptr : none();
+    for (int i = 0; i < 2; ++i)
+      if (!out[i]) out[i] = &(made[i] = make({n_tokens, c.Hkv, c.d}, type, *first));
+    int rc;
+    const int32_t* sp = slots->data_ptr<int32_t>();
+    void *kp = out[0]->data_ptr(), *vp = out[1]->data_ptr();
+    Py_BEGIN_ALLOW_THREADS;
+    rc = fn_cache_load(&c, type == at::kFloat ? LAQ_F32 : LAQ_BF16, n_tokens, sp, kp, vp, stream);
+    Py_END_ALLOW_THREADS;
+    if (rc != LAQ_OK) return PyLong_FromLong(rc);
+    return pair(own_or_made(a[3], &made[0]), own_or_made(a[4], &made[1]));
+  } catch (const std::exception&) {
+    return thrown();
+  }
+}
+
+// cache_attention(q, cache, block_table, rows, start, max_rows, scale, out, lse, want_lse, ws, split) -> out | (out, lse) | error code | None
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  try {
+    if (n_args != 12) return none();
+    laq_cache c;
+    laq_heads hq = {};
+    const at::Tensor *first, *q = gpu_tensor(a[0]);
+    if (!paged_cache(a[1], &c, &first) || !q || q->dim() != 3) return none();
+    const at::Device dev = first->device();
+    const int64_t T = q->size(0), Hq = q->size(1);
+    if (q->device() != dev || !heads_of(q, *q, T, c.d, &hq)) return none();
+    const at::Tensor* table = ints(a[2], dev, 0);
+    if (!table || table->dim() != 2 || table->size(0) < 1 || table->size(0) > INT32_MAX || table->size(1) > INT32_MAX / c.block_rows) return none();
+    const int64_t n = table->size(0), width = table->size(1);
+    const at::Tensor *rows = ints(a[3], dev, n), *start = is_none(a[4]) ? nullptr : ints(a[4], dev, n + 1);
+    long long most = width * c.block_rows;
+    if (!rows || (!start && (!is_none(a[4]) || T != n)) || (!is_none(a[5]) && !as_int(a[5], &most)) || !PyFloat_CheckExact(a[6]) || !PyBool_Check(a[9]) ||
+        !PyBool_Check(a[11]))
+      return none();
+    if (most < 1) most = 1;
+    const int dt = dtype_code(*q);
+    const at::Tensor *out = nullptr, *lse = nullptr, *ws = nullptr;
+    at::Tensor made[2], scratch;
+    if (!is_none(a[7]) && !(out = output(a[7], q->scalar_type(), T * Hq * c.d, *q))) return none();
+    if (!is_none(a[8]) && !(lse = output(a[8], at::kFloat, T * Hq, *q))) return none();
+    if (!is_none(a[10])) {
+      ws = gpu_tensor(a[10]);
+      if (!ws || ws->device() != dev || !ws->is_contiguous()) return none();
+    }
+    void* stream;
+    if (!stream_on(dev, &stream)) return PyErr_Occurred() ? nullptr : none();
+    if (a[11] == Py_False) {
+      ws = nullptr;
+    } else if (!ws) {
+      if (const size_t need = fn_cache_attention_workspace_bytes(&c, (int32_t)Hq, dt, (int32_t)n, T, (int32_t)most))
+        ws = &(scratch = make({(int64_t)need}, at::kByte, *q));
+    }
+    if (!out) out = &(made[0] = make({T, Hq, c.d}, q->scalar_type(), *q));
+    if (!lse && a[9] == Py_True) lse = &(made[1] = make({T, Hq}, at::kFloat, *q));
+    int rc;
+    const size_t ws_bytes = ws ? ws->numel() * ws->element_size() : 0;
+    const int32_t *tp = table->data_ptr<int32_t>(), *rp = rows->data_ptr<int32_t>(), *stp = start ? start->data_ptr<int32_t>() : nullptr;
+    void *op = out->data_ptr(), *wp = ws ? ws->data_ptr() : nullptr;
+    float* lp = lse ? static_cast<float*>(lse->data_ptr()) : nullptr;
+    const float scale = (float)PyFloat_AS_DOUBLE(a[6]);
+    Py_BEGIN_ALLOW_THREADS;
+    rc = fn_cache_attention(&c, dt, scale, (int32_t)n, T, stp, &hq, tp, (int32_t)width, rp, (int32_t)most, op, lp, wp, ws_bytes, stream);
+    Py_END_ALLOW_THREADS;
+    if (rc != LAQ_OK) return PyLong_FromLong(rc);
+    PyObject* o = own_or_made(a[7], &made[0]);
+    return lse ? pair(o, own_or_made(a[8], &made[1])) : o;
+  } catch (const std::exception&) {
+    return thrown();
+  }
+}
+
+// bind_cache(addresses of laq_rope, laq_cache_append, laq_cache_compact, laq_cache_load, laq_cache_attention, laq_cache_attention_workspace_bytes)
+PyObject* bind_cache(PyObject*, PyObject* args) {
+  unsigned long long f[6];
+  if (!PyArg_ParseTuple(args, "KKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5])) return nullptr;
+  fn_rope = reinterpret_cast<decltype(fn_rope)>(f[0]);
+  fn_cache_append = reinterpret_cast<decltype(fn_cache_append)>(f[1]);
+  fn_cache_compact = reinterpret_cast<decltype(fn_cache_compact)>(f[2]);
+  fn_cache_load = reinterpret_cast<decltype(fn_cache_load)>(f[3]);
+  fn_cache_attention = reinterpret_cast<decltype(fn_cache_attention)>(f[4]);
+  fn_cache_attention_workspace_bytes = reinterpret_cast<decltype(fn_cache_attention_workspace_bytes)>(f[5]);
+  Py_RETURN_NONE;
+}
+
 // bind(addresses of laq_evict, laq_workspace_bytes, laq_decode_attention, laq_decode_workspace_bytes, laq_qcache_store,
 //      torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
 PyObject* bind(PyObject*, PyObject* args) {
@@ -657,6 +964,12 @@ PyMethodDef methods[] = {
     {"fp4_compact", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp4_compact)), METH_FASTCALL, nullptr},
     {"fp4_load", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp4_load)), METH_FASTCALL, nullptr},
     {"fp4_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp4_attention)), METH_FASTCALL, nullptr},
+    {"bind_cache", bind_cache, METH_VARARGS, nullptr},
+    {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope)), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_append)), METH_FASTCALL, nullptr},
+    {"cache_compact", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_compact)), METH_FASTCALL, nullptr},
+    {"cache_load", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_load)), METH_FASTCALL, nullptr},
+    {"cache_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attention)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -138,6 +138,12 @@ def laq_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: to
     """q [tokens, Hq, d] and k [tokens, Hkv, d] (one of them may be None; views with contiguous rows, e.g. of a fused projection, are fine)
     rotated to positions [tokens] (int32).  Returns (q_out, k_out), made dense if not given; an input may be its own output."""
     lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.rope(q, k, positions, rope, q_out, k_out)
+        if got is not None:
+            if type(got) is int:
+                raise LaqError(got, "laq_rope")
+            return got
     like = q if q is not None else k
     if like is None:
         raise ValueError("q or k is needed")
@@ -170,6 +176,12 @@ def laq_cache_append(cache: PagedCache, k: Optional[torch.Tensor], v: Optional[t
     cache; tokens whose slot is -1 are left out.  With rope and positions [tokens] k is rotated on the way, and q [tokens, Hq, d], if given, into
     q_out (made if not given; q itself is fine), which is returned."""
     lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.cache_append(cache, k, v, slots, q, positions, rope, q_out)
+        if got is not None:
+            if type(got) is int:
+                raise LaqError(got, "laq_cache_append")
+            return got[0]
     c = _paged(cache)
     like = k if k is not None else v
     if like is None:
@@ -209,6 +221,12 @@ def laq_cache_compact(cache: PagedCache, k: torch.Tensor, v: Optional[torch.Tens
     slots: one entry per kept row of an instance, for all its KV heads, instance after instance (laq_block_map with add = min(budget, L));
     block_table / L: k, v are paged caches, as for laq_compact."""
     lib = binding._lib or load_library()
+    if stream is None and block_table is None and L is None and binding._native is not None:
+        got = binding._native.cache_compact(cache, k, v, idx, budget, slots)
+        if got is not None:
+            if got is not True:
+                raise LaqError(got, "laq_cache_compact")
+            return
     c = _paged(cache)
     _dev(idx, "idx")
     n, Hkv, L, d, kvs, paged = _cache(k, "k", block_table, L)
@@ -232,6 +250,12 @@ def laq_cache_load(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype = 
                    v: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows slots [tokens] of the cache as (k, v) [tokens, Hkv, d] of type dtype (made if not given); rows whose slot is -1 are 0."""
     lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.cache_load(cache, slots, dtype, k, v)
+        if got is not None:
+            if type(got) is int:
+                raise LaqError(got, "laq_cache_load")
+            return got
     c = _paged(cache)
     _ints(slots, "slots", cache.k, 0)
     T = slots.numel()
@@ -261,6 +285,12 @@ def laq_cache_attention(q: torch.Tensor, cache: PagedCache, block_table: torch.T
     returns (out, lse), lse the logarithm of the sum of the exponentials.  split: let the library spread long rows over several workgroups (a
     workspace of laq_cache_attention_workspace_bytes is made if ws is None)."""
     lib = binding._lib or load_library()
+    if stream is None and binding._native is not None:
+        got = binding._native.cache_attention(q, cache, block_table, rows, start, max_rows, scale, out, lse, want_lse, ws, split)
+        if got is not None:
+            if type(got) is int:
+                raise LaqError(got, "laq_cache_attention")
+            return got
     c = _paged(cache)
     if q.dim() != 3:
         raise ValueError("q is [tokens, Hq, d]")

@@ -214,9 +214,16 @@ from torch._subclasses.fake_tensor import FakeTensorMode
 import paper_2505_20334_amd as laq
 from paper_2505_20334_amd import binding, paged
 
-laq.load_library()
+import ctypes
+lib = laq.load_library()
+address = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
+# (no device here: a device and a stream number as a GPU would give them)
+binding._native.bind(address("laq_evict"), address("laq_workspace_bytes"), address("laq_decode_attention"),
+                     address("laq_decode_workspace_bytes"), address("laq_qcache_store"), lambda: %d, lambda device: 0)
 binding._stream = paged._stream = lambda stream: 0
 torch._C._cuda_getDevice = lambda: %d
+if not %r:
+    binding._native = None
 
 def made(*sizes, dtype=torch.bfloat16):
     return torch.empty(*sizes, dtype=dtype, device="cuda")
@@ -245,17 +252,18 @@ GOOD = ["laq.laq_cache_append(cache, kv, kv, ints(3))", "laq.laq_cache_append(wi
         "laq.laq_rope(q, kv, ints(3), rope)"]
 
 
-def outcomes(calls, device=0):
-    res = subprocess.run([sys.executable, "-c", SETUP % (device, calls)], capture_output=True, text=True, timeout=110)
+def outcomes(calls, device=0, native=True):
+    res = subprocess.run([sys.executable, "-c", SETUP % (device, device, native, calls)], capture_output=True, text=True, timeout=110)
     assert res.returncode == 0, "the process ended with %d: %s" % (res.returncode, res.stderr[-600:])
     return res.stdout.strip().splitlines()[-len(calls):]
 
 
-def test_calls_in_order_reach_the_library():
+@pytest.mark.parametrize("native", [True, False])
+def test_calls_in_order_reach_the_library(native):
     # (which refuses the addresses that tensors without memory have: NULL)
-    for got in outcomes(GOOD):
+    for got in outcomes(GOOD, native=native):
         assert got.startswith("raised LaqError laq_") and got.endswith("invalid argument (code -1)"), got
-    for got in outcomes(GOOD, device=1):
+    for got in outcomes(GOOD, device=1, native=native):
         assert got.endswith("which is not the current device"), got
 
 
@@ -290,9 +298,17 @@ BAD = [
 ]
 
 
-def test_what_is_refused():
-    for (call, words), got in zip(BAD, outcomes([call for call, _ in BAD])):
+@pytest.mark.parametrize("native", [True, False])
+def test_what_is_refused(native):
+    for (call, words), got in zip(BAD, outcomes([call for call, _ in BAD], native=native)):
         assert got.startswith("raised ") and words in got, (call, got)
+
+
+@pytest.mark.parametrize("call", ["torch.vmap(lambda x: laq.laq_cache_append(cache, x, kv, ints(3)))(kv[None])", "torch.vmap(lambda x: laq.laq_cache_load(cache, x))(ints(1, 3))",
+                                  "torch.vmap(lambda x: laq.laq_rope(x, None, ints(3), rope))(kv[None])", "torch.vmap(lambda x: laq.laq_cache_attention(x, cache, ints(3, 4), ints(3)))(q[None])",
+                                  "torch.vmap(lambda x: laq.laq_cache_compact(cache, x, None, ints(200), [10, 20, 30], ints(60)))(source[None])"])
+def test_a_tensor_without_an_address(call):
+    assert outcomes([call])[0].startswith("raised RuntimeError Cannot access data pointer")
 
 
 def test_the_library_exports_what_its_third_header_declares(repo_root):
