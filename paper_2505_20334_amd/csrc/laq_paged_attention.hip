@@ -12,6 +12,8 @@
 //                 eight keys of one channel; it reads eight channels of its eight keys, and a permutation of 8 x 8 numbers in registers, two a
 //                 instruction, makes the operands of eight products.  fp32 (16 x 16 x 4): one key a lane, so the pieces are operands as they are
 // A lane's pieces of V are VN channels: its product row m of product e of piece h is channel (16 h + m) VN + e.
+#include <atomic>
+#include <chrono>
 #include <type_traits>
 
 #include "laq_paged.h"
@@ -28,7 +30,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int ATT_WAVES = 4, ATT_THREADS = 64 * ATT_WAVES;
-constexpr int JOIN_THREADS = 256;
 constexpr float MINUS_INF = -__builtin_inff();
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
@@ -39,56 +40,76 @@ __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 acc) { return __bu
 
 // How the launch is cut, from what the host knows.
 struct AttPlan {
-  int32_t parts, part_rows;              // a column in parts of part_rows keys, `parts` at most (the last one takes what is left)
   int32_t tile;                          // score rows of a column
-  int32_t slots;                         // columns of a KV head over all requests, at most
+  int32_t columns;                       // columns of a KV head over all requests, at most
+  int32_t shares;                        // workgroups that share all keys of all columns out evenly; 0: one workgroup a column
 };
 
-// Where the columns of a request begin: a request of R score rows has ceil(R / tile) columns, and floor(R' / tile) + i, with R' score rows and i requests
-// before it, leaves at least that many between one request and the next.
+// A request of the call.
+struct Request {
+  int token0, tokens, held;              // tokens 0: none, or numbers that make no sense; held: rows of the cache
+};
+__device__ __forceinline__ Request request_of(const PagedAttention& a, int block_rows, int i) {
+  Request r{i, 1, 0};
+  if (a.start) {
+    const int64_t t0 = a.start[i], t1 = a.start[i + 1];
+    r.token0 = (int)t0;
+    r.tokens = t0 < 0 || t1 <= t0 || t1 > a.n_tokens ? 0 : (int)(t1 - t0);
+  }
+  r.held = max(0, min(a.rows[i], a.blocks_per_inst * block_rows));
+  return r;
+}
+__device__ __forceinline__ int tiles_of(const Request& r, int G, int tile) { return (int)(((int64_t)r.tokens * G + tile - 1) / tile); }
+
+// Where the columns of a request begin if every column has a workgroup: a request of R score rows has ceil(R / tile) columns, and floor(R' / tile) + i, with R'
+// score rows and i requests before it, leaves at least that many between one request and the next.
 __device__ __forceinline__ int64_t first_column(const PagedAttention& a, int G, int tile, int i) {
   return a.start ? (int64_t)a.start[i] * G / tile + i : (int64_t)i * ((G + tile - 1) / tile);
 }
-
-// What a column is.
-struct Column {
-  int request, row0, rows;               // its first score row in the request, and their number (0: no such column)
-  int token0, tokens;                    // of the request
-  int held;                              // rows of the cache
-  __device__ int last(int row, int G) const { return held - tokens + (row0 + row) / G; }      // the last key that a score row sees
-  __device__ int keys(int G) const { return rows ? max(0, last(rows - 1, G) + 1) : 0; }
-};
-__device__ __forceinline__ Column find_column(const PagedAttention& a, int block_rows, int G, int tile, int slot) {
-  Column c{0, 0, 0, 0, 1, 0};
-  if (a.start) {
-    // the last request that begins at `slot` or before it: 64 looked at at a time
-    int lo = 0, n = a.n;
-    const int lane = threadIdx.x & 63;
-    while (n > 1) {
-      const int step = (n + 63) / 64, i = lo + lane * step;
-      const bool before = lane * step < n && first_column(a, G, tile, i) <= slot;
-      const int k = __popcll(__ballot(before)) - 1;
-      const int at = max(k, 0) * step;
-      lo += at;
-      n = min(step, n - at);
-      if (n < 1) n = 1;
-    }
-    c.request = __builtin_amdgcn_readfirstlane(min(lo, a.n - 1));
-    const int64_t t0 = a.start[c.request], t1 = a.start[c.request + 1];
-    if (t0 < 0 || t1 <= t0 || t1 > a.n_tokens) return c;
-    c.token0 = (int)t0;
-    c.tokens = (int)(t1 - t0);
-  } else {
-    c.request = slot / ((G + tile - 1) / tile);
-    if (c.request >= a.n) return c;
-    c.token0 = c.request;
+// The last request that begins at column `slot` or before it: 64 looked at at a time.
+__device__ __forceinline__ int find_request(const PagedAttention& a, int G, int tile, int slot) {
+  if (!a.start) return min(slot / ((G + tile - 1) / tile), a.n - 1);
+  int lo = 0, n = a.n;
+  const int lane = threadIdx.x & 63;
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lo + lane * step;
+    const bool before = lane * step < n && first_column(a, G, tile, i) <= slot;
+    const int at = max(__popcll(__ballot(before)) - 1, 0) * step;
+    lo += at;
+    n = max(min(step, n - at), 1);
   }
-  const int64_t row0 = (slot - first_column(a, G, tile, c.request)) * tile, all = (int64_t)c.tokens * G;
-  if (row0 < 0 || row0 >= all) return c;
-  c.row0 = (int)row0;
-  c.rows = (int)min((int64_t)tile, all - row0);
-  c.held = max(0, min(a.rows[c.request], a.blocks_per_inst * block_rows));
-  return c;
+  return __builtin_amdgcn_readfirstlane(min(lo, a.n - 1));
+}
+
+// What a column is: a tile of score rows of a request.
+struct Column {
+  int row0, rows;                        // its first score row in the request, and their number (0: no such column)
+  int token0, tokens, held;              // of the request
+  __device__ int last(int row, int G) const { return held - tokens + (row0 + row) / G; }      // the last key that a score row sees
+  __device__ int keys(int G) const { return max(0, last(rows - 1, G) + 1); }
+};
+__device__ __forceinline__ Column column_of(const Request& r, int G, int tile, int64_t t) {
+  const int64_t row0 = t * tile, all = (int64_t)r.tokens * G;
+  if (t < 0 || row0 >= all) return Column{0, 0, 0, 1, 0};
+  return Column{(int)row0, (int)min((int64_t)tile, all - row0), r.token0, r.tokens, r.held};
+}
+
+// Partial sums m (a score, not scaled), z and y of score rows, joined.
+__device__ __forceinline__ void join(float& m, float& z, f32x4& y, float m2, float z2, f32x4 y2, float scale2) {
+  const float top = fmaxf(m, m2);
+  const float by = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale2), by2 = m2 == top ? 1.f : __builtin_amdgcn_exp2f((m2 - top) * scale2);
+  m = top;
+  z = z * by + z2 * by2;
+  y = y * by + y2 * by2;
+}
+
+// Written through to the device's memory, and read from there.
+__device__ __forceinline__ void store_pair(void* p, float a, float b) {
+  __hip_atomic_store(static_cast<unsigned long long*>(p), (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 load_pair(const void* p) {
+  const unsigned long long v = __hip_atomic_load(static_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
 
 // N numbers of the cache in a row, as they lie.
@@ -176,8 +197,9 @@ __device__ __forceinline__ void drop_odd(Raw<E, N>& r) {
 template <typename Q, typename E, int D, int NT>
 struct Kinds {
   static constexpr bool F32 = std::is_same<Q, float>::value, SCALED = std::is_same<E, E4m3>::value;
-  static constexpr int KT = F32 ? 1 : 2;                     // tiles of 16 keys a step
+  static constexpr int KT = F32 ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
   static constexpr int KN = F32 ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
+  static constexpr bool ONCE = NT == 1;                      // one workgroup reads a row: past the caches
   static constexpr int VN = F32 || D == 64 ? 4 : 8, VP = D / (16 * VN);
   static constexpr int OT = D / 16;                          // output tiles
   static constexpr int PAD = D + 4;
@@ -191,24 +213,145 @@ struct StepKeys {
   uint32_t ks[K::KT], vs[K::KT];                             // SCALED: of this lane's key row; of its four keys of V
   bool there[K::KT];
 };
+// A tile's rows, read through a buffer descriptor: reads behind its end give zeros without memory traffic, and nothing at all is read of a tile that is not
+// there.  So the reads of a step are issued whatever the step has, and the wait for a step's keys can leave those of the next one on their way (with
+// branches around them it waited for both: 96 requests x 8 heads x 6144 rows 428 us).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_of(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
+}
+template <bool ONCE, typename R>
+__device__ __forceinline__ void fetch(R& r, __amdgpu_buffer_rsrc_t tile, int at) {
+  constexpr int PAST = ONCE ? 2 : 0;                         // nt
+  if constexpr (sizeof(r.x) == 16) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b128(tile, at, 0, PAST));
+  else if constexpr (sizeof(r.x) == 8) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b64(tile, at, 0, PAST));
+  else r.x = __builtin_amdgcn_raw_buffer_load_b32(tile, at, 0, PAST);
+}
 
-// Partial results of the ranges of a column: [slot][head][part][tile rows] of m (as a score, not scaled) and z, and as many rows of d sums.
+// The ranges of columns that several workgroups share.  A workgroup has two places: 2w for a column that began in another workgroup's share, 2w + 1 for one
+// that begins in its own and goes on; a place has mz[tile] (m and z) and sums[tile][d].  A workgroup that is done with a range counts itself in at
+// counts[the workgroup that the column begins in]; the last one to do so joins the ranges, in their order, and sets the count back.  A count is the
+// launch's nonce and a number: whatever else lies in the workspace is no count, and a replayed launch, whose nonce is the same, finds none of its own.
 struct Partials {
+  unsigned long long* counts;
   float2* mz;
   float* sums;
+  uint32_t nonce;
 };
+// True for the last one of `count` workgroups.
+__device__ __forceinline__ bool count_in(unsigned long long* at, uint32_t nonce, int count) {
+  unsigned long long was = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), is;
+  do is = (uint32_t)(was >> 32) == nonce ? was + 1 : (unsigned long long)nonce << 32 | 1;
+  while (!__hip_atomic_compare_exchange_strong(at, &was, is, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+  if ((int)(uint32_t)is != count) return false;
+  __hip_atomic_store(at, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
+// Four numbers of the output from sums and the sum of weights, and the logarithm.
+template <typename Q>
+__device__ __forceinline__ void put_out(const PagedView& c, const PagedAttention& a, const Column& col, int head, int G, int r, int at, float m, float z, f32x4 y) {
+  const int row = col.row0 + r;
+  const int64_t to = (int64_t)(col.token0 + row / G) * a.Hq + head * G + row % G;
+  const float inv = z == 0.f ? 0.f : 1.f / z;
+  if (at == 0 && a.lse) a.lse[to] = z == 0.f ? MINUS_INF : (__builtin_amdgcn_logf(z) + m * a.scale2) * 0.69314718055994530942f;
+  if constexpr (std::is_same<Q, float>::value)
+    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to * c.d + at) = y * inv;
+  else
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to * c.d + at) = u32x2{pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv)};
+}
 
 template <typename Q, typename E, int D, int NT>
-__global__ __launch_bounds__(ATT_THREADS) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
+__global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
   using K = Kinds<Q, E, D, NT>;
+  constexpr int STEP = 16 * K::KT, TURN = STEP * ATT_WAVES;
+  __shared__ float sums[ATT_WAVES][16][K::PAD];
+  __shared__ float2 marks[ATT_WAVES][16];
+  __shared__ bool odds[ATT_WAVES];
+  __shared__ int64_t found[4];
   const int H = c.Hkv, G = a.Hq / H;
-  const int head = blockIdx.x % H, pi = blockIdx.x / H % p.parts, slot = blockIdx.x / H / p.parts;
-  const Column col = find_column(a, c.block_rows, G, p.tile, slot);
-  const int keys = col.keys(G), from = pi * p.part_rows;
-  const bool cut = p.parts > 1 && keys > p.part_rows;        // this column is in parts
-  if (col.rows == 0 || (pi > 0 && from >= keys)) return;
-  const int to = pi == p.parts - 1 ? keys : min(keys, from + p.part_rows);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+
+  // Where this workgroup begins.  All keys of all columns are a line of turns, request after request, of each its heads, of each its tiles, of each the turns
+  // of the request's rows (a column of a request's earlier tokens has turns in which it sees nothing); a share is as many turns of it as any other.
+  int request, head;
+  int64_t tile_at, turn = 0, left = 1, total = 0, begin = 0;                 // turn in the column; turns of the share; of all; where the column begins on the line
+  int shares = p.shares;
+  if (shares) {
+    const int each = (a.n + ATT_THREADS - 1) / ATT_THREADS, i0 = min(a.n, (int)threadIdx.x * each), i1 = min(a.n, i0 + each);
+    int64_t mine = 0, tiles = 0;
+    for (int i = i0; i < i1; ++i) {
+      const Request r = request_of(a, c.block_rows, i);
+      const int64_t t = tiles_of(r, G, p.tile);
+      tiles += t;
+      mine += t * H * ((r.held + TURN - 1) / TURN + (r.held == 0));
+    }
+    // sums over the lanes before this one, then over the waves
+    int64_t upto = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+      const int64_t below = __shfl_up(upto, m);
+      if (lane >= m) upto += below;
+      tiles += __shfl_xor(tiles, m);
+    }
+    __shared__ int64_t waves[ATT_WAVES][2];
+    if (lane == 63) {
+      waves[wave][0] = upto;
+      waves[wave][1] = tiles;
+    }
+    if (threadIdx.x == 0) found[0] = -1;
+    __syncthreads();
+    int64_t before = upto - mine, all_tiles = 0;
+#pragma unroll
+    for (int w = 0; w < ATT_WAVES; ++w) {
+      if (w < wave) before += waves[w][0];
+      total += waves[w][0];
+      all_tiles += waves[w][1];
+    }
+    if (all_tiles > p.columns || total <= 0) return;                         // (a start that makes no sense)
+    if (shares > total) shares = (int)total;
+    const int w = blockIdx.x;
+    if (w >= shares) return;
+    const int64_t x0 = total * w / shares;
+    left = total * (w + 1) / shares - x0;
+    if (x0 >= before && x0 < before + mine) {
+      int64_t at = before;
+      for (int i = i0; i < i1; ++i) {
+        const Request r = request_of(a, c.block_rows, i);
+        const int64_t turns = (r.held + TURN - 1) / TURN + (r.held == 0), all = turns * H * tiles_of(r, G, p.tile);
+        if (x0 < at + all) {
+          found[0] = i;
+          found[1] = (x0 - at) / turns;
+          found[2] = (x0 - at) % turns;
+          break;
+        }
+        at += all;
+      }
+    }
+    __syncthreads();
+    if (found[0] < 0) return;
+    request = __builtin_amdgcn_readfirstlane((int)found[0]);
+    const int tiles_here = tiles_of(request_of(a, c.block_rows, request), G, p.tile);
+    const int64_t column = found[1];
+    head = __builtin_amdgcn_readfirstlane((int)(column / tiles_here));
+    tile_at = __builtin_amdgcn_readfirstlane((int)(column % tiles_here));
+    turn = __builtin_amdgcn_readfirstlane((int)found[2]);
+    begin = x0 - turn;
+  } else {
+    head = blockIdx.x % H;
+    const int slot = blockIdx.x / H;
+    request = find_request(a, G, p.tile, slot);
+    tile_at = slot - first_column(a, G, p.tile, request);
+  }
+
+  for (;;) {
+  const Request req = request_of(a, c.block_rows, request);
+  const Column col = column_of(req, G, p.tile, tile_at);
+  const int turns = shares ? (req.held + TURN - 1) / TURN + (req.held == 0) : 1;
+  const int turns_here = (int)min((int64_t)turns - turn, left);
+  if (col.rows == 0 && !shares) return;
+  const bool cut = shares && turns_here < turns;
+  const int keys = col.keys(G), from = (int)min((int64_t)keys, turn * TURN);
+  const int to = shares ? (int)min((int64_t)keys, (turn + turns_here) * TURN) : keys;
 
   // the score rows of this lane's columns
   int last[NT];
@@ -241,56 +384,63 @@ __global__ __launch_bounds__(ATT_THREADS) void paged_attention_kernel(PagedView 
 
   bool odd = false;                                          // an infinity or a NaN in V that not every row sees
 
-  // where the lane's pieces lie behind a tile's first row (channels beyond d: those of the row's beginning, for nobody)
-  int32_t k_at[K::KP], v_at[K::VP];
+  // where the lane's pieces lie behind a tile's first row, in bytes (channels beyond d: the next row's or nothing, for nobody)
+  const int row_bytes = (int)(c.row * sizeof(E));
+  const int k_at = n * row_bytes + g * (K::KN * (int)sizeof(E));
+  int v_at[4];
 #pragma unroll
-  for (int i = 0; i < K::KP; ++i) {
-    const int at = (4 * i + g) * K::KN;
-    k_at[i] = (int32_t)(n * c.row) + (at < c.d ? at : 0);
-  }
-#pragma unroll
-  for (int i = 0; i < K::VP; ++i) {
-    const int at = (16 * i + n) * K::VN;
-    v_at[i] = (int32_t)(4 * g * c.row) + (at < c.d ? at : 0);
-  }
-  const int32_t row = (int32_t)c.row;
+  for (int j = 0; j < 4; ++j) v_at[j] = (4 * g + j) * row_bytes + n * (K::VN * (int)sizeof(E));
+  const uint32_t tile_bytes = 15u * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E));
   const E *kx = static_cast<const E*>(c.k.x) + head * c.head, *vx = static_cast<const E*>(c.v.x) + head * c.head;
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
-  const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)col.request * a.blocks_per_inst);
+  const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)request * a.blocks_per_inst);
 
-  // this wave's steps: keys from + (wave + 4 i) * 16 KT on; its place in the blocks moves with it
-  constexpr int STEP = 16 * K::KT;
-  const auto load = [&](int key, StepKeys<K, E>& s) {
+  // this wave's steps: keys from + (wave + 4 i) * STEP on.  Its place in the blocks moves with it, and the blocks' numbers are asked for a step ahead
+  struct Place { int page, off; } at{0, 0};
+  const int turn_pages = TURN / c.block_rows, turn_rows = TURN - turn_pages * c.block_rows;
+  const auto forward = [&](Place& w, int pages, int rows) {
+    w.page += pages;
+    w.off += rows;
+    if (w.off >= c.block_rows) {
+      w.off -= c.block_rows;
+      ++w.page;
+    }
+  };
+  int blocks[K::KT];                                         // of the step that is loaded next
+  const auto ask = [&](int left) {
+    Place w = at;
 #pragma unroll
     for (int kt = 0; kt < K::KT; ++kt) {
-      const uint32_t at = (uint32_t)key + 16 * kt;
-      const int page = (int)(at / (uint32_t)c.block_rows), off = (int)(at - (uint32_t)page * c.block_rows);
-      const int block = 16 * kt < to - key ? table[page] : -1;
-      s.there[kt] = block >= 0 && block < c.n_blocks;
-      if (s.there[kt]) {
-        const int64_t base = block * c.block + (int64_t)off * c.row;
-        const E *kb = kx + base, *vb = vx + base;
-#pragma unroll
-        for (int i = 0; i < K::KP; ++i) s.k[kt][i] = *reinterpret_cast<const Raw<E, K::KN>*>(kb + k_at[i]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < K::VP; ++i) s.v[kt][j][i] = *reinterpret_cast<const Raw<E, K::VN>*>(vb + v_at[i] + j * row);
-        if constexpr (K::SCALED) {
-          const int64_t sc = ((int64_t)block * H + head) * c.block_rows + off;
-          s.ks[kt] = c.k.scales[sc + n];
-          s.vs[kt] = *reinterpret_cast<const uint32_t*>(c.v.scales + sc + 4 * g);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < K::KP; ++i) clear(s.k[kt][i]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < K::VP; ++i) clear(s.v[kt][j][i]);
-        s.ks[kt] = s.vs[kt] = 0;
-      }
+      blocks[kt] = 16 * kt < left ? table[w.page] : -1;
+      forward(w, 0, 16);
     }
+  };
+  // the step at `at`, with `left` keys from its beginning on (none: nothing is read); goes on to the next one
+  const auto load = [&](int left, StepKeys<K, E>& s) {
+    Place w = at;
+#pragma unroll
+    for (int kt = 0; kt < K::KT; ++kt) {
+      const int block = blocks[kt];
+      s.there[kt] = block >= 0 && block < c.n_blocks;
+      const int64_t base = s.there[kt] ? block * c.block + (int64_t)w.off * c.row : 0;
+      const uint32_t bytes = s.there[kt] ? tile_bytes : 0u;
+      const __amdgpu_buffer_rsrc_t kb = tile_of(kx + base, bytes), vb = tile_of(vx + base, bytes);
+#pragma unroll
+      for (int i = 0; i < K::KP; ++i) fetch<K::ONCE>(s.k[kt][i], kb, k_at + i * (4 * K::KN * (int)sizeof(E)));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < K::VP; ++i) fetch<K::ONCE>(s.v[kt][j][i], vb, v_at[j] + i * (16 * K::VN * (int)sizeof(E)));
+      if constexpr (K::SCALED) {
+        const int64_t sc = s.there[kt] ? ((int64_t)block * H + head) * c.block_rows + w.off : 0;
+        const uint32_t marks = s.there[kt] ? 16u : 0u;
+        s.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.k.scales + sc, marks), n, 0, 0);
+        s.vs[kt] = __builtin_amdgcn_raw_buffer_load_b32(tile_of(c.v.scales + sc, marks), 4 * g, 0, 0);
+      }
+      forward(w, 0, 16);
+    }
+    forward(at, turn_pages, turn_rows);
+    ask(left - TURN);
   };
 
   const auto scale_of_v = [&](const StepKeys<K, E>& s, int kt, int j) { return e4m3_scale_value(s.vs[kt] >> (8 * j) & 255u); };
@@ -394,7 +544,7 @@ __global__ __launch_bounds__(ATT_THREADS) void paged_attention_kernel(PagedView 
               if (none) clear(s.v[kt][j][i]);
               else drop_odd(s.v[kt][j][i]);
             }
-            if (K::SCALED && none) s.vs[kt] &= ~(255u << (8 * j));
+            if constexpr (K::SCALED) s.vs[kt] = none ? s.vs[kt] & ~(255u << (8 * j)) : s.vs[kt];
           }
         }
     }
@@ -410,42 +560,46 @@ __global__ __launch_bounds__(ATT_THREADS) void paged_attention_kernel(PagedView 
             for (int t = 0; t < NT; ++t) o[t][i * 4 + e] = mfma(v[e], x[t][0][j], o[t][i * 4 + e]);
         }
     } else {
-      u32x4 w[NT];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-        w[t] = u32x4{pack2(x[t][0][0], x[t][0][1]), pack2(x[t][0][2], x[t][0][3]), pack2(x[t][1][0], x[t][1][1]), pack2(x[t][1][2], x[t][1][3])};
+      for (int h = 0; h < K::KT; h += 2) {
+        u32x4 w[NT];
 #pragma unroll
-      for (int i = 0; i < K::VP; ++i) {
-        // [key][channel pair] to [channel][key pair]
-        using P = decltype(pairs(s.v[0][0][0], 1.f));
-        P v[8];
+        for (int t = 0; t < NT; ++t)
+          w[t] = u32x4{pack2(x[t][h][0], x[t][h][1]), pack2(x[t][h][2], x[t][h][3]), pack2(x[t][h + 1][0], x[t][h + 1][1]), pack2(x[t][h + 1][2], x[t][h + 1][3])};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = pairs(s.v[j / 4][j % 4][i], K::SCALED ? scale_of_v(s, j / 4, j % 4) : 1.f);
+        for (int i = 0; i < K::VP; ++i) {
+          // [key][channel pair] to [channel][key pair]
+          using P = decltype(pairs(s.v[0][0][0], 1.f));
+          P v[8];
 #pragma unroll
-        for (int e = 0; e < K::VN; ++e) {
-          u32x4 f;
+          for (int j = 0; j < 8; ++j) v[j] = pairs(s.v[h + j / 4][j % 4][i], K::SCALED ? scale_of_v(s, h + j / 4, j % 4) : 1.f);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            f[j] = __builtin_amdgcn_perm(v[2 * j + 1][e / 2], v[2 * j][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+          for (int e = 0; e < K::VN; ++e) {
+            u32x4 f;
 #pragma unroll
-          for (int t = 0; t < NT; ++t) o[t][i * K::VN + e] = mfma(f, w[t], o[t][i * K::VN + e]);
+            for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(v[2 * j + 1][e / 2], v[2 * j][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t][i * K::VN + e] = mfma(f, w[t], o[t][i * K::VN + e]);
+          }
         }
       }
     }
   };
 
   // two steps at a time: one's keys are on their way while the other's are used
-  {
+  if (to - from > wave * STEP) {
     StepKeys<K, E> s0, s1;
-    int key = to - from > wave * STEP ? from + wave * STEP : to;
-    constexpr int TURN = STEP * ATT_WAVES;
-    if (key < to) load(key, s0);
-    while (key < to) {
-      if (to - key > TURN) load(key + TURN, s1);
+    int key = from + wave * STEP;
+    at.page = (int)((uint32_t)key / (uint32_t)c.block_rows);
+    at.off = (int)((uint32_t)key - (uint32_t)at.page * c.block_rows);
+    ask(to - key);
+    load(to - key, s0);
+    for (;;) {
+      load(to - key - TURN, s1);
       compute(key, s0);
       if (to - key <= TURN) break;
       key += TURN;
-      if (to - key > TURN) load(key + TURN, s0);
+      load(to - key - TURN, s0);
       compute(key, s1);
       if (to - key <= TURN) break;
       key += TURN;
@@ -453,12 +607,10 @@ __global__ __launch_bounds__(ATT_THREADS) void paged_attention_kernel(PagedView 
   }
 
   // the waves' sums, score rows of 16 at a time
-  __shared__ float sums[ATT_WAVES][16][K::PAD];
-  __shared__ float2 marks[ATT_WAVES][16];
-  __shared__ bool odds[ATT_WAVES];
   const bool wave_odd = __any(odd);
   if (lane == 0) odds[wave] = wave_odd;
-  const int64_t place = (((int64_t)slot * H + head) * p.parts + pi) * p.tile;
+  const int w = blockIdx.x;
+  const int64_t place = (int64_t)(2 * w + (turn == 0)) * p.tile;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     float zt = z[t];
@@ -473,26 +625,18 @@ __global__ __launch_bounds__(ATT_THREADS) void paged_attention_kernel(PagedView 
 #pragma unroll
         for (int e = 0; e < K::VN; ++e) sums[wave][n][(16 * i + 4 * g + j) * K::VN + e] = o[t][i * K::VN + e][j];
     __syncthreads();
-    constexpr int EACH = 4, PER = D / EACH;
+    constexpr int PER = D / 4;
     for (int i = threadIdx.x; i < 16 * PER; i += ATT_THREADS) {
-      const int rr = i / PER, at = i % PER * EACH, r = 16 * t + rr;
+      const int rr = i / PER, at = i % PER * 4, r = 16 * t + rr;
       if (r >= col.rows || at >= c.d) continue;
-      float top = MINUS_INF, Z = 0.f;
+      float top = marks[0][rr].x, Z = marks[0][rr].y;
+      f32x4 y = *reinterpret_cast<const f32x4*>(&sums[0][rr][at]);
+      bool any_odd = odds[0];
 #pragma unroll
-      for (int w = 0; w < ATT_WAVES; ++w) top = fmaxf(top, marks[w][rr].x);
-      f32x4 y{};
-#pragma unroll
-      for (int w = 0; w < ATT_WAVES; ++w) {
-        const float2 mz = marks[w][rr];
-        // (a wave without keys: 0, also where all are; an infinite or undefined score makes a NaN of z already)
-        const float by = mz.x == MINUS_INF ? 0.f : mz.x == top ? 1.f : __builtin_amdgcn_exp2f((mz.x - top) * a.scale2);
-        Z += mz.x == MINUS_INF && mz.y == mz.y ? 0.f : by == 0.f && mz.y != mz.y ? mz.y : mz.y * by;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) y[e] += mz.x == MINUS_INF ? 0.f : sums[w][rr][at + e] * by;
+      for (int v = 1; v < ATT_WAVES; ++v) {
+        join(top, Z, y, marks[v][rr].x, marks[v][rr].y, *reinterpret_cast<const f32x4*>(&sums[v][rr][at]), a.scale2);
+        any_odd |= odds[v];
       }
-      bool any_odd = false;
-#pragma unroll
-      for (int w = 0; w < ATT_WAVES; ++w) any_odd |= odds[w];
       if (any_odd) {
         const int upto = min(to - 1, col.last(r, G));
         for (int key = max(from, first_last + 1); key <= upto; ++key) {
@@ -500,126 +644,135 @@ __global__ __launch_bounds__(ATT_THREADS) void paged_attention_kernel(PagedView 
           if (block < 0 || block >= c.n_blocks) continue;
           const E* v = vx + block * c.block + (int64_t)off * c.row;
           const uint32_t vs = K::SCALED ? c.v.scales[((int64_t)block * H + head) * c.block_rows + off] : 0u;
-          for (int e = 0; e < EACH; ++e) {
+          for (int e = 0; e < 4; ++e) {
             const float f = number(v, at + e, vs);
             if (f - f != 0.f) y[e] += f;
           }
         }
       }
-      if (cut) {
-        if (at == 0) part.mz[place + r] = float2{top, Z};
-        *reinterpret_cast<f32x4*>(part.sums + (place + r) * c.d + at) = y;
-        continue;
-      }
-      const int row_in = col.row0 + r;
-      const int64_t to_row = (int64_t)(col.token0 + row_in / G) * a.Hq + head * G + row_in % G;
-      const float inv = Z == 0.f ? 0.f : 1.f / Z;
-      if (at == 0 && a.lse) a.lse[to_row] = Z == 0.f ? MINUS_INF : (__builtin_amdgcn_logf(Z) + top * a.scale2) * 0.69314718055994530942f;
-      if constexpr (K::F32) {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to_row * c.d + at) = y * inv;
+      if (!cut) {
+        put_out<Q>(c, a, col, head, G, r, at, top, Z, y);
       } else {
-        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to_row * c.d + at) = u32x2{pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv)};
+        if (at == 0) store_pair(part.mz + place + r, top, Z);
+        store_pair(part.sums + (place + r) * c.d + at, y[0], y[1]);
+        store_pair(part.sums + (place + r) * c.d + at + 2, y[2], y[3]);
       }
     }
   }
-}
+  if (!shares) return;
 
-// The parts of a score row, in their order: a workgroup has one row, its threads four channels each of every eighth (or so) part.
-template <typename Q>
-__global__ __launch_bounds__(JOIN_THREADS) void paged_join_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
-  const int H = c.Hkv, G = a.Hq / H;
-  const int r = blockIdx.x % p.tile, head = blockIdx.x / p.tile % H, slot = blockIdx.x / p.tile / H;
-  const Column col = find_column(a, c.block_rows, G, p.tile, slot);
-  const int keys = col.keys(G);
-  if (r >= col.rows || keys <= p.part_rows) return;
-  const int parts = min(p.parts, (keys + p.part_rows - 1) / p.part_rows);
-  __shared__ f32x4 sums[JOIN_THREADS];
-  __shared__ float zs[JOIN_THREADS];
-  const int lanes = c.d / 4, groups = JOIN_THREADS / lanes, mine = threadIdx.x / lanes, at = threadIdx.x % lanes * 4;
-  const int64_t place = ((int64_t)slot * H + head) * p.parts * p.tile + r;
-  float top = MINUS_INF;
-  for (int i = 0; i < parts; ++i) top = fmaxf(top, part.mz[place + (int64_t)i * p.tile].x);
-  f32x4 y{};
-  float Z = 0.f;
-  if (mine < groups) {
-    for (int i = mine; i < parts; i += groups) {
-      const int64_t row = place + (int64_t)i * p.tile;
-      const float2 mz = part.mz[row];
-      const f32x4 v = *reinterpret_cast<const f32x4*>(part.sums + row * c.d + at);
-      const float by = mz.x == MINUS_INF ? 0.f : mz.x == top ? 1.f : __builtin_amdgcn_exp2f((mz.x - top) * a.scale2);
-      Z += by == 0.f ? (mz.y != mz.y ? mz.y : 0.f) : mz.y * by;
-      y += v * by;
+  if (cut) {
+    // the workgroups of this column, and whether this one is the last of them
+    const int first = (int)(((begin + 1) * shares - 1) / total), count = (int)(((begin + turns) * shares - 1) / total) - first + 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                         // (what this wave stored has arrived)
+    __syncthreads();
+    if (threadIdx.x == 0) found[3] = count_in(part.counts + first, part.nonce, count);
+    __syncthreads();
+    if (found[3]) {
+      // four channels of a row a thread, and as many groups of ranges as there are threads for
+      const int per = c.d / 4, items = col.rows * per, groups = max(1, min(count, ATT_THREADS / items));
+      float* const shared_sums = &sums[0][0][0];                             // [ATT_THREADS][4], then m and z
+      f32x2* const shared_mz = reinterpret_cast<f32x2*>(shared_sums + 4 * ATT_THREADS);
+      for (int i0 = 0; i0 < items; i0 += groups > 1 ? items : ATT_THREADS) {
+        const int grp = groups > 1 ? threadIdx.x / items : 0, item = groups > 1 ? threadIdx.x % items : i0 + threadIdx.x;
+        const int r = item / per, at = item % per * 4;
+        const bool on = item < items && grp < groups;
+        float top = MINUS_INF, Z = 0.f;
+        f32x4 y{};
+        constexpr int U = 4;
+        if (on) {
+          for (int k = grp; k < count; k += U * groups) {
+            f32x2 mz[U], s0[U], s1[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const int kk = min(k + u * groups, count - 1);
+              const int64_t row = (int64_t)(2 * (first + kk) + (kk == 0)) * p.tile + r;
+              mz[u] = load_pair(part.mz + row);
+              s0[u] = load_pair(part.sums + row * c.d + at);
+              s1[u] = load_pair(part.sums + row * c.d + at + 2);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (k + u * groups < count) join(top, Z, y, mz[u][0], mz[u][1], f32x4{s0[u][0], s0[u][1], s1[u][0], s1[u][1]}, a.scale2);
+          }
+        }
+        if (groups > 1) {
+          *reinterpret_cast<f32x4*>(shared_sums + 4 * threadIdx.x) = y;
+          shared_mz[threadIdx.x] = f32x2{top, Z};
+          __syncthreads();
+          for (int k = 1; on && grp == 0 && k < groups; ++k)
+            join(top, Z, y, shared_mz[k * items + item][0], shared_mz[k * items + item][1], *reinterpret_cast<const f32x4*>(shared_sums + 4 * (k * items + item)), a.scale2);
+        }
+        if (on && grp == 0) put_out<Q>(c, a, col, head, G, r, at, top, Z, y);
+      }
     }
   }
-  sums[threadIdx.x] = y;
-  zs[threadIdx.x] = Z;
-  __syncthreads();
-  if (mine != 0) return;
-  for (int i = 1; i < groups; ++i) {
-    y += sums[i * lanes + threadIdx.x];
-    Z += zs[i * lanes + threadIdx.x];
+  left -= turns_here;
+  if (left <= 0) return;
+  // the next column
+  begin += turns;
+  turn = 0;
+  if (++tile_at >= tiles_of(req, G, p.tile)) {
+    tile_at = 0;
+    if (++head == H) {
+      head = 0;
+      do {
+        if (++request >= a.n) return;
+      } while (tiles_of(request_of(a, c.block_rows, request), G, p.tile) == 0);
+    }
   }
-  const int row_in = col.row0 + r;
-  const int64_t to_row = (int64_t)(col.token0 + row_in / G) * a.Hq + head * G + row_in % G;
-  const float inv = Z == 0.f ? 0.f : 1.f / Z;
-  if (at == 0 && a.lse) a.lse[to_row] = Z == 0.f ? MINUS_INF : (__builtin_amdgcn_logf(Z) + top * a.scale2) * 0.69314718055994530942f;
-  if constexpr (std::is_same<Q, float>::value) {
-    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to_row * c.d + at) = y * inv;
-  } else {
-    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to_row * c.d + at) = u32x2{pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv)};
+  __syncthreads();                                           // (the LDS is free)
   }
 }
 
 // ---- the host's part -------------------------------------------------------------------------
 
-constexpr int64_t MOST_PARTS = 4096;      // of a call, beside one of every column
-
 int tiles_of_rows(int dtype, int d, int n, int64_t n_tokens, int G) {
   const int64_t rows = (n_tokens + n - 1) / n * G;                   // of a request, on average
-  const int most = dtype == LAQ_F32 || d > 128 ? 2 : 4;
-  return rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+  const int most = d > 128 ? 1 : dtype == LAQ_F32 ? 2 : 4;
+  return rows <= 16 || most == 1 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
 }
 
-AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, bool has_start, int max_rows, bool may_cut) {
+// Workgroups that share a call out: as many as the device holds of the kernels (256 compute units; registers).
+int resident(int d) { return d <= 64 ? 1024 : d <= 128 ? 512 : 256; }
+
+// max_rows 0: the most shares that a call of any bound has.
+AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, bool has_start, int max_rows, bool may_share) {
   const int G = Hq / c.Hkv;
   AttPlan p;
   p.tile = 16 * tiles_of_rows(dtype, c.d, n, n_tokens, G);
-  const int64_t slots = has_start ? n_tokens * G / p.tile + n : (int64_t)n * ((G + p.tile - 1) / p.tile);
-  p.slots = (int32_t)(slots < 0x7fffffff ? slots : 0x7fffffff);
-  p.parts = 1;
-  p.part_rows = 0x7fffffff;
-  if (!may_cut) return p;
-  const int64_t columns = slots * c.Hkv;
-  // as many parts as keep the device busy and a workspace small, none shorter than two turns of a workgroup
-  int64_t rows = ((int64_t)max_rows * columns / MOST_PARTS + 127) / 128 * 128;
-  if (rows < 256) rows = 256;
-  if (max_rows > rows) {
-    p.part_rows = (int32_t)rows;
-    p.parts = (int32_t)((max_rows + rows - 1) / rows);
+  const int64_t columns = has_start ? n_tokens * G / p.tile + n : (int64_t)n * ((G + p.tile - 1) / p.tile);
+  p.columns = (int32_t)(columns < 0x7fffffff ? columns : 0x7fffffff);
+  p.shares = may_share ? resident(c.d) : 0;
+  if (may_share && max_rows > 0) {
+    const int turn = ATT_WAVES * 16 * (dtype == LAQ_F32 ? 1 : c.type == LAQ_E4M3 ? 4 : 2);
+    const int64_t turns = columns * c.Hkv * (((int64_t)max_rows + turn - 1) / turn);
+    if (turns < p.shares) p.shares = (int32_t)turns;
   }
   return p;
 }
 
-struct Bytes { size_t mz, sums; };
+struct Bytes {
+  size_t counts, mz, sums;
+  size_t all() const { return counts + mz + sums; }
+};
 Bytes bytes_of(const PagedView& c, const AttPlan& p) {
-  if (p.parts == 1) return Bytes{0, 0};
-  const size_t rows = (size_t)p.slots * c.Hkv * p.parts * p.tile;
-  return Bytes{(rows * sizeof(float2) + 255) / 256 * 256, rows * c.d * sizeof(float)};
+  const size_t rows = (size_t)p.shares * 2 * p.tile;
+  return Bytes{((size_t)p.shares * 8 + 255) / 256 * 256, rows * sizeof(float2), rows * c.d * sizeof(float)};
 }
 
 template <typename Q, typename E, int D>
 hipError_t start_attention(const PagedView& c, const PagedAttention& a, const AttPlan& p, const Partials& part, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)p.slots * c.Hkv * p.parts));
+  const dim3 grid((unsigned)(p.shares ? p.shares : (int64_t)p.columns * c.Hkv));
   switch (p.tile) {
     case 16: hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 1>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part); break;
-    case 32: hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 2>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part); break;
+    case 32:
+      if constexpr (D <= 128) hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 2>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
+      break;
     default:
       if constexpr (!std::is_same<Q, float>::value && D <= 128)
         hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 4>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.parts == 1) return e;
-  hipLaunchKernelGGL((paged_join_kernel<Q>), dim3((unsigned)((int64_t)p.slots * c.Hkv * p.tile)), dim3(JOIN_THREADS), 0, st, c, a, p, part);
   return hipGetLastError();
 }
 
@@ -632,22 +785,23 @@ hipError_t by_size(const PagedView& c, const PagedAttention& a, const AttPlan& p
 
 }  // namespace
 
-size_t paged_attention_bytes(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows) {
-  const AttPlan with = plan_of(c, Hq, dtype, n, n_tokens, true, max_rows, true), without = plan_of(c, Hq, dtype, n, n_tokens, false, max_rows, true);
-  const Bytes x = bytes_of(c, with), y = bytes_of(c, without);
-  return x.mz + x.sums > y.mz + y.sums ? x.mz + x.sums : y.mz + y.sums;
+size_t paged_attention_bytes(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, int) {
+  return bytes_of(c, plan_of(c, Hq, dtype, n, n_tokens, true, 0, true)).all();
 }
 
 bool paged_attention_fits(const PagedView& c, int dtype, const PagedAttention& a, bool cut) {
   const AttPlan p = plan_of(c, a.Hq, dtype, a.n, a.n_tokens, a.start != nullptr, a.max_rows, cut);
-  const int64_t columns = (int64_t)p.slots * c.Hkv;
-  return columns * p.parts < (1 << 24) && (p.parts == 1 || columns * p.tile < (1 << 24));
+  return p.shares || (int64_t)p.columns * c.Hkv < (1 << 24);
 }
 
 hipError_t launch_paged_attention(const PagedView& c, int dtype, const PagedAttention& a, void* ws, hipStream_t st) {
+  static std::atomic<uint32_t> launches{(uint32_t)(std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull >> 32)};
   const AttPlan p = plan_of(c, a.Hq, dtype, a.n, a.n_tokens, a.start != nullptr, a.max_rows, ws != nullptr);
   const Bytes b = bytes_of(c, p);
-  const Partials part{static_cast<float2*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + b.mz)};
+  char* const at = static_cast<char*>(ws);
+  Partials part{reinterpret_cast<unsigned long long*>(at), reinterpret_cast<float2*>(at + b.counts), reinterpret_cast<float*>(at + b.counts + b.mz), 0};
+  if (ws)
+    do part.nonce = launches.fetch_add(1); while (part.nonce == 0);          // 0 is a count that was set back
   if (dtype == LAQ_BF16)
     return c.type == LAQ_BF16 ? by_size<uint16_t, uint16_t>(c, a, p, part, st) : by_size<uint16_t, E4m3>(c, a, p, part, st);
   switch (c.type) {
