@@ -29,6 +29,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+#ifndef MW
+#define MW 2
+#endif
+#ifndef RES
+#define RES 512
+#endif
+#ifndef RES64
+#define RES64 1024
+#endif
 constexpr int ATT_WAVES = 4, ATT_THREADS = 64 * ATT_WAVES;
 constexpr float MINUS_INF = -__builtin_inff();
 
@@ -211,7 +220,9 @@ struct StepKeys {
   Raw<E, K::KN> k[K::KT][K::KP];
   Raw<E, K::VN> v[K::KT][4][K::VP];
   uint32_t ks[K::KT], vs[K::KT];                             // SCALED: of this lane's key row; of its four keys of V
-  bool there[K::KT];
+  // of the step that is read next: where its tiles begin (numbers; scales), and how many bytes of each there are (0: not there)
+  int64_t base[K::KT], scales[K::KT];
+  uint32_t bytes[K::KT];
 };
 // A tile's rows, read through a buffer descriptor: reads behind its end give zeros without memory traffic, and nothing at all is read of a tile that is not
 // there.  So the reads of a step are issued whatever the step has, and the wait for a step's keys can leave those of the next one on their way (with
@@ -228,24 +239,17 @@ __device__ __forceinline__ void fetch(R& r, __amdgpu_buffer_rsrc_t tile, int at)
 }
 
 // The ranges of columns that several workgroups share.  A workgroup has two places: 2w for a column that began in another workgroup's share, 2w + 1 for one
-// that begins in its own and goes on; a place has mz[tile] (m and z) and sums[tile][d].  A workgroup that is done with a range counts itself in at
-// counts[the workgroup that the column begins in]; the last one to do so joins the ranges, in their order, and sets the count back.  A count is the
-// launch's nonce and a number: whatever else lies in the workspace is no count, and a replayed launch, whose nonce is the same, finds none of its own.
+// that begins in its own and goes on; a place has mz[tile] (m and z), sums[tile][d] and a mark.  A workgroup that is done with a range writes the launch's nonce
+// there, after its sums have arrived, and then looks at the marks of all ranges of the column: who finds all of them joins the ranges, in their order, and
+// clears the marks, so that a replayed launch, whose nonce is the same, finds none of its own; whatever else lies in the workspace is no mark.  Two may find all
+// of them (both write the same); one that comes to look when another has begun to clear finds that it is not needed.  (Counting in by compare and swap: 64
+// workgroups of a column take turns, one request of 32768 rows x 8 heads 61 us.)
 struct Partials {
-  unsigned long long* counts;
+  unsigned long long* marks;
   float2* mz;
   float* sums;
   uint32_t nonce;
 };
-// True for the last one of `count` workgroups.
-__device__ __forceinline__ bool count_in(unsigned long long* at, uint32_t nonce, int count) {
-  unsigned long long was = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), is;
-  do is = (uint32_t)(was >> 32) == nonce ? was + 1 : (unsigned long long)nonce << 32 | 1;
-  while (!__hip_atomic_compare_exchange_strong(at, &was, is, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-  if ((int)(uint32_t)is != count) return false;
-  __hip_atomic_store(at, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return true;
-}
 
 // Four numbers of the output from sums and the sum of weights, and the logarithm.
 template <typename Q>
@@ -261,13 +265,13 @@ __device__ __forceinline__ void put_out(const PagedView& c, const PagedAttention
 }
 
 template <typename Q, typename E, int D, int NT>
-__global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
+__global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
   using K = Kinds<Q, E, D, NT>;
   constexpr int STEP = 16 * K::KT, TURN = STEP * ATT_WAVES;
   __shared__ float sums[ATT_WAVES][16][K::PAD];
   __shared__ float2 marks[ATT_WAVES][16];
   __shared__ bool odds[ATT_WAVES];
-  __shared__ int64_t found[4];
+  __shared__ int64_t found[3];
   const int H = c.Hkv, G = a.Hq / H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
 
@@ -308,7 +312,10 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
       all_tiles += waves[w][1];
     }
     if (all_tiles > p.columns || total <= 0) return;                         // (a start that makes no sense)
-    if (shares > total) shares = (int)total;
+#ifndef MT
+#define MT 1
+#endif
+    if (shares > (total + MT - 1) / MT) shares = (int)((total + MT - 1) / MT);
     const int w = blockIdx.x;
     if (w >= shares) return;
     const int64_t x0 = total * w / shares;
@@ -390,7 +397,6 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
   int v_at[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) v_at[j] = (4 * g + j) * row_bytes + n * (K::VN * (int)sizeof(E));
-  const uint32_t tile_bytes = 15u * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E));
   const E *kx = static_cast<const E*>(c.k.x) + head * c.head, *vx = static_cast<const E*>(c.v.x) + head * c.head;
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
   const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)request * a.blocks_per_inst);
@@ -415,35 +421,43 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
       forward(w, 0, 16);
     }
   };
-  // the step at `at`, with `left` keys from its beginning on (none: nothing is read); goes on to the next one
-  const auto load = [&](int left, StepKeys<K, E>& s) {
+  // The step at `at`, with `left` keys from its beginning on (none: nothing is read).  Rows behind them are not read: zeros.  K first, which moves what is
+  // there and where it lies to s; then V, which goes on to the next step.
+  const auto load_k = [&](int left, StepKeys<K, E>& s) {
     Place w = at;
 #pragma unroll
     for (int kt = 0; kt < K::KT; ++kt) {
       const int block = blocks[kt];
-      s.there[kt] = block >= 0 && block < c.n_blocks;
-      const int64_t base = s.there[kt] ? block * c.block + (int64_t)w.off * c.row : 0;
-      const uint32_t bytes = s.there[kt] ? tile_bytes : 0u;
-      const __amdgpu_buffer_rsrc_t kb = tile_of(kx + base, bytes), vb = tile_of(vx + base, bytes);
+      const bool there = block >= 0 && block < c.n_blocks;
+      const int rows = min(16, left - 16 * kt);
+      s.bytes[kt] = there ? (uint32_t)(rows - 1) * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E)) : 0u;
+      s.base[kt] = there ? block * c.block + (int64_t)w.off * c.row : 0;
+      const __amdgpu_buffer_rsrc_t kb = tile_of(kx + s.base[kt], s.bytes[kt]);
 #pragma unroll
       for (int i = 0; i < K::KP; ++i) fetch<K::ONCE>(s.k[kt][i], kb, k_at + i * (4 * K::KN * (int)sizeof(E)));
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < K::VP; ++i) fetch<K::ONCE>(s.v[kt][j][i], vb, v_at[j] + i * (16 * K::VN * (int)sizeof(E)));
       if constexpr (K::SCALED) {
-        const int64_t sc = s.there[kt] ? ((int64_t)block * H + head) * c.block_rows + w.off : 0;
-        const uint32_t marks = s.there[kt] ? 16u : 0u;
-        s.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.k.scales + sc, marks), n, 0, 0);
-        s.vs[kt] = __builtin_amdgcn_raw_buffer_load_b32(tile_of(c.v.scales + sc, marks), 4 * g, 0, 0);
+        s.scales[kt] = there ? ((int64_t)block * H + head) * c.block_rows + w.off : 0;
+        s.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.k.scales + s.scales[kt], there ? 16u : 0u), n, 0, 0);
       }
       forward(w, 0, 16);
     }
     forward(at, turn_pages, turn_rows);
     ask(left - TURN);
   };
+  const auto load_v = [&](StepKeys<K, E>& s) {
+#pragma unroll
+    for (int kt = 0; kt < K::KT; ++kt) {
+      const __amdgpu_buffer_rsrc_t vb = tile_of(vx + s.base[kt], s.bytes[kt]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < K::VP; ++i) fetch<K::ONCE>(s.v[kt][j][i], vb, v_at[j] + i * (16 * K::VN * (int)sizeof(E)));
+      if constexpr (K::SCALED) s.vs[kt] = __builtin_amdgcn_raw_buffer_load_b32(tile_of(c.v.scales + s.scales[kt], s.bytes[kt] ? 16u : 0u), 4 * g, 0, 0);
+    }
+  };
 
   const auto scale_of_v = [&](const StepKeys<K, E>& s, int kt, int j) { return e4m3_scale_value(s.vs[kt] >> (8 * j) & 255u); };
+  // one step, and the reads of the next one: its K as soon as this one's is used, its V likewise, so that about a step is on its way at any time
   const auto compute = [&](int key, StepKeys<K, E>& s) {
     f32x4 x[NT][K::KT];
 #pragma unroll
@@ -468,11 +482,14 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
         }
       }
     }
-    bool all_there = true;
-#pragma unroll
-    for (int kt = 0; kt < K::KT; ++kt) all_there &= s.there[kt];
-    const bool edge = !all_there || key > first_last - (STEP - 1);   // a key that not every row sees
     const int left = to - key;                                       // (keys of the step as far as `left`; sums with key could pass 2^31)
+    bool there[K::KT], edge = min(left, first_last - key + 1) < STEP;   // a key that not every row sees
+#pragma unroll
+    for (int kt = 0; kt < K::KT; ++kt) {
+      there[kt] = s.bytes[kt] != 0;
+      edge |= !there[kt];
+    }
+    load_k(left - TURN, s);
     if (edge) {
 #pragma unroll
       for (int kt = 0; kt < K::KT; ++kt)
@@ -482,7 +499,8 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
           // (keys behind this range belong to nobody here)
 #pragma unroll
           for (int t = 0; t < NT; ++t)
-            if (!s.there[kt] || at >= left || at > last[t] - key) x[t][kt][j] = MINUS_INF;
+            if (!there[kt] || at >= left || at > last[t] - key) x[t][kt][j] = MINUS_INF;
+          if constexpr (K::SCALED) s.vs[kt] = at >= left ? s.vs[kt] & ~(255u << (8 * j)) : s.vs[kt];      // (255 makes a NaN of the zeros)
         }
     }
     // the reference moves where a score is far above it
@@ -525,8 +543,8 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
           z[t] += w;
         }
     // V of keys that some rows do not see: a weight of 0 does not keep an infinity or a NaN out.  They are 0 here, and what rows that see them get is
-    // added at the end.  Nothing of keys that nobody sees here
-    if (edge) {
+    // added at the end.  (Of keys that nobody sees here nothing was read.)
+    if (key > first_last - STEP + 1 && first_last < to - 1) {
 #pragma unroll
       for (int kt = 0; kt < K::KT; ++kt)
 #pragma unroll
@@ -538,7 +556,7 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
 #pragma unroll
             for (int i = 0; i < K::VP; ++i) bad |= has_odd(s.v[kt][j][i], vs);
             odd |= bad && at < left;
-            const bool none = at >= left || vs == 255u;
+            const bool none = vs == 255u;
 #pragma unroll
             for (int i = 0; i < K::VP; ++i) {
               if (none) clear(s.v[kt][j][i]);
@@ -584,23 +602,19 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
         }
       }
     }
+    load_v(s);
   };
 
-  // two steps at a time: one's keys are on their way while the other's are used
   if (to - from > wave * STEP) {
-    StepKeys<K, E> s0, s1;
+    StepKeys<K, E> s;
     int key = from + wave * STEP;
     at.page = (int)((uint32_t)key / (uint32_t)c.block_rows);
     at.off = (int)((uint32_t)key - (uint32_t)at.page * c.block_rows);
     ask(to - key);
-    load(to - key, s0);
+    load_k(to - key, s);
+    load_v(s);
     for (;;) {
-      load(to - key - TURN, s1);
-      compute(key, s0);
-      if (to - key <= TURN) break;
-      key += TURN;
-      load(to - key - TURN, s0);
-      compute(key, s1);
+      compute(key, s);
       if (to - key <= TURN) break;
       key += TURN;
     }
@@ -664,11 +678,17 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
   if (cut) {
     // the workgroups of this column, and whether this one is the last of them
     const int first = (int)(((begin + 1) * shares - 1) / total), count = (int)(((begin + turns) * shares - 1) / total) - first + 1;
+    const auto place_of = [&](int k) { return 2 * (first + k) + (k == 0); };
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                         // (what this wave stored has arrived)
     __syncthreads();
-    if (threadIdx.x == 0) found[3] = count_in(part.counts + first, part.nonce, count);
+    if (threadIdx.x == 0) __hip_atomic_store(part.marks + 2 * w + (turn == 0), (unsigned long long)part.nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (found[3]) {
+    bool all = true;
+    for (int k = threadIdx.x; k < count; k += ATT_THREADS)
+      all &= __hip_atomic_load(part.marks + place_of(k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == part.nonce;
+    if (__syncthreads_and(all)) {
+      for (int k = threadIdx.x; k < count; k += ATT_THREADS) __hip_atomic_store(part.marks + place_of(k), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       // four channels of a row a thread, and as many groups of ranges as there are threads for
       const int per = c.d / 4, items = col.rows * per, groups = max(1, min(count, ATT_THREADS / items));
       float* const shared_sums = &sums[0][0][0];                             // [ATT_THREADS][4], then m and z
@@ -679,14 +699,17 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? 2 : 1) void page
         const bool on = item < items && grp < groups;
         float top = MINUS_INF, Z = 0.f;
         f32x4 y{};
-        constexpr int U = 4;
+#ifndef FU
+#define FU 4
+#endif
+        constexpr int U = FU;
         if (on) {
           for (int k = grp; k < count; k += U * groups) {
             f32x2 mz[U], s0[U], s1[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
               const int kk = min(k + u * groups, count - 1);
-              const int64_t row = (int64_t)(2 * (first + kk) + (kk == 0)) * p.tile + r;
+              const int64_t row = (int64_t)place_of(kk) * p.tile + r;
               mz[u] = load_pair(part.mz + row);
               s0[u] = load_pair(part.sums + row * c.d + at);
               s1[u] = load_pair(part.sums + row * c.d + at + 2);
@@ -734,7 +757,7 @@ int tiles_of_rows(int dtype, int d, int n, int64_t n_tokens, int G) {
 }
 
 // Workgroups that share a call out: as many as the device holds of the kernels (256 compute units; registers).
-int resident(int d) { return d <= 64 ? 1024 : d <= 128 ? 512 : 256; }
+int resident(int d) { return d <= 64 ? RES64 : d <= 128 ? RES : 256; }
 
 // max_rows 0: the most shares that a call of any bound has.
 AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, bool has_start, int max_rows, bool may_share) {
@@ -747,18 +770,18 @@ AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, 
   if (may_share && max_rows > 0) {
     const int turn = ATT_WAVES * 16 * (dtype == LAQ_F32 ? 1 : c.type == LAQ_E4M3 ? 4 : 2);
     const int64_t turns = columns * c.Hkv * (((int64_t)max_rows + turn - 1) / turn);
-    if (turns < p.shares) p.shares = (int32_t)turns;
+    if ((turns + MT - 1) / MT < p.shares) p.shares = (int32_t)((turns + MT - 1) / MT);
   }
   return p;
 }
 
 struct Bytes {
-  size_t counts, mz, sums;
-  size_t all() const { return counts + mz + sums; }
+  size_t marks, mz, sums;
+  size_t all() const { return marks + mz + sums; }
 };
 Bytes bytes_of(const PagedView& c, const AttPlan& p) {
   const size_t rows = (size_t)p.shares * 2 * p.tile;
-  return Bytes{((size_t)p.shares * 8 + 255) / 256 * 256, rows * sizeof(float2), rows * c.d * sizeof(float)};
+  return Bytes{((size_t)p.shares * 16 + 255) / 256 * 256, rows * sizeof(float2), rows * c.d * sizeof(float)};
 }
 
 template <typename Q, typename E, int D>
@@ -799,9 +822,9 @@ hipError_t launch_paged_attention(const PagedView& c, int dtype, const PagedAtte
   const AttPlan p = plan_of(c, a.Hq, dtype, a.n, a.n_tokens, a.start != nullptr, a.max_rows, ws != nullptr);
   const Bytes b = bytes_of(c, p);
   char* const at = static_cast<char*>(ws);
-  Partials part{reinterpret_cast<unsigned long long*>(at), reinterpret_cast<float2*>(at + b.counts), reinterpret_cast<float*>(at + b.counts + b.mz), 0};
+  Partials part{reinterpret_cast<unsigned long long*>(at), reinterpret_cast<float2*>(at + b.marks), reinterpret_cast<float*>(at + b.marks + b.mz), 0};
   if (ws)
-    do part.nonce = launches.fetch_add(1); while (part.nonce == 0);          // 0 is a count that was set back
+    do part.nonce = launches.fetch_add(1); while (part.nonce == 0);          // 0 is a mark that was cleared
   if (dtype == LAQ_BF16)
     return c.type == LAQ_BF16 ? by_size<uint16_t, uint16_t>(c, a, p, part, st) : by_size<uint16_t, E4m3>(c, a, p, part, st);
   switch (c.type) {
