@@ -142,15 +142,17 @@ __device__ __forceinline__ u32x4 pairs(const Raw<E4m3, 8>& r, float s) {
   return u32x4{pair_of(r.x[0], s, false), pair_of(r.x[0], s, true), pair_of(r.x[1], s, false), pair_of(r.x[1], s, true)};
 }
 __device__ __forceinline__ u32x2 pairs(const Raw<E4m3, 4>& r, float s) { return u32x2{pair_of(r.x, s, false), pair_of(r.x, s, true)}; }
-// As fp32.
-__device__ __forceinline__ f32x4 floats(const Raw<float, 4>& r, float) { return __builtin_bit_cast(f32x4, r.x); }
-__device__ __forceinline__ f32x4 floats(const Raw<uint16_t, 4>& r, float) {
+// As fp32: numbers 4 part and on.
+__device__ __forceinline__ f32x4 floats(const Raw<float, 4>& r, int, float) { return __builtin_bit_cast(f32x4, r.x); }
+__device__ __forceinline__ f32x4 floats(const Raw<uint16_t, 4>& r, int, float) {
   return __builtin_bit_cast(f32x4, (u32x4{r.x[0] << 16, r.x[0] & 0xffff0000u, r.x[1] << 16, r.x[1] & 0xffff0000u}));
 }
-__device__ __forceinline__ f32x4 floats(const Raw<E4m3, 4>& r, float s) {
+__device__ __forceinline__ f32x4 floats(const Raw<uint16_t, 8>& r, int part, float) { return floats(Raw<uint16_t, 4>{u32x2{r.x[2 * part], r.x[2 * part + 1]}}, 0, 0.f); }
+__device__ __forceinline__ f32x4 floats(const Raw<E4m3, 4>& r, int, float s) {
   const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(r.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(r.x, true);
   return f32x4{a[0] * s, a[1] * s, b[0] * s, b[1] * s};
 }
+__device__ __forceinline__ f32x4 floats(const Raw<E4m3, 8>& r, int part, float s) { return floats(Raw<E4m3, 4>{r.x[part]}, 0, s); }
 
 // A number of a row of V.
 __device__ __forceinline__ float number(const float* row, int i, uint32_t) { return row[i]; }
@@ -208,8 +210,11 @@ struct Kinds {
   static constexpr bool F32 = std::is_same<Q, float>::value, SCALED = std::is_same<E, E4m3>::value;
   static constexpr int KT = F32 ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
   static constexpr int KN = F32 ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
+  // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on
+  static constexpr int KW = 16 / (KN * (int)sizeof(E));
+  static constexpr __host__ __device__ int k_channel(int i, int g) { return i / KW * (4 * KW * KN) + g * (KW * KN) + i % KW * KN; }
   static constexpr bool ONCE = NT == 1;                      // one workgroup reads a row: past the caches
-  static constexpr int VN = F32 || D == 64 ? 4 : 8, VP = D / (16 * VN);
+  static constexpr int VN = std::is_same<E, float>::value || D == 64 ? 4 : 8, VP = D / (16 * VN);
   static constexpr int OT = D / 16;                          // output tiles
   static constexpr int PAD = D + 4;
 };
@@ -232,10 +237,29 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_of(const void* p, uint32_
 }
 template <bool ONCE, typename R>
 __device__ __forceinline__ void fetch(R& r, __amdgpu_buffer_rsrc_t tile, int at) {
-  constexpr int PAST = ONCE ? 2 : 0;                         // nt
+#ifndef NTV
+#define NTV 2
+#endif
+  constexpr int PAST = ONCE ? NTV : 0;                       // nt
   if constexpr (sizeof(r.x) == 16) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b128(tile, at, 0, PAST));
   else if constexpr (sizeof(r.x) == 8) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b64(tile, at, 0, PAST));
   else r.x = __builtin_amdgcn_raw_buffer_load_b32(tile, at, 0, PAST);
+}
+
+// W pieces side by side, 16 bytes together.
+template <bool ONCE, int W, typename R>
+__device__ __forceinline__ void fetch_wide(R* r, __amdgpu_buffer_rsrc_t tile, int at) {
+  struct Wide { u32x4 x; } w;
+  fetch<ONCE>(w, tile, at);
+  if constexpr (W == 1) {
+    r[0].x = w.x;
+  } else if constexpr (W == 2) {
+    r[0].x = u32x2{w.x[0], w.x[1]};
+    r[1].x = u32x2{w.x[2], w.x[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i].x = w.x[i];
+  }
 }
 
 // The ranges of columns that several workgroups share.  A workgroup has two places: 2w for a column that began in another workgroup's share, 2w + 1 for one
@@ -372,7 +396,7 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
     const Q* src = static_cast<const Q*>(a.q.x) + (int64_t)(col.token0 + rr / G) * a.q.token + (int64_t)(head * G + rr % G) * a.q.head;
 #pragma unroll
     for (int i = 0; i < K::KP; ++i) {
-      const int at = (4 * i + g) * K::KN;
+      const int at = K::k_channel(i, g);
       q[t][i] = on && at < c.d ? *reinterpret_cast<const u32x4*>(src + at) : u32x4{};
     }
   }
@@ -393,7 +417,7 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
 
   // where the lane's pieces lie behind a tile's first row, in bytes (channels beyond d: the next row's or nothing, for nobody)
   const int row_bytes = (int)(c.row * sizeof(E));
-  const int k_at = n * row_bytes + g * (K::KN * (int)sizeof(E));
+  const int k_at = n * row_bytes + g * 16;
   int v_at[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) v_at[j] = (4 * g + j) * row_bytes + n * (K::VN * (int)sizeof(E));
@@ -434,7 +458,7 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
       s.base[kt] = there ? block * c.block + (int64_t)w.off * c.row : 0;
       const __amdgpu_buffer_rsrc_t kb = tile_of(kx + s.base[kt], s.bytes[kt]);
 #pragma unroll
-      for (int i = 0; i < K::KP; ++i) fetch<K::ONCE>(s.k[kt][i], kb, k_at + i * (4 * K::KN * (int)sizeof(E)));
+      for (int i = 0; i < K::KP; i += K::KW) fetch_wide<K::ONCE, K::KW>(&s.k[kt][i], kb, k_at + i / K::KW * 64);
       if constexpr (K::SCALED) {
         s.scales[kt] = there ? ((int64_t)block * H + head) * c.block_rows + w.off : 0;
         s.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.k.scales + s.scales[kt], there ? 16u : 0u), n, 0, 0);
@@ -468,15 +492,15 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
 #pragma unroll
       for (int i = 0; i < K::KP; ++i) {
         if constexpr (K::F32) {
-          f32x4 k = floats(s.k[kt][i], ks);
-          if (c.d != D && (4 * i + g) * K::KN >= c.d) k = f32x4{};
+          f32x4 k = floats(s.k[kt][i], 0, ks);
+          if (c.d != D && K::k_channel(i, g) >= c.d) k = f32x4{};
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[t][kt] = mfma(k[e], __uint_as_float(q[t][i][e]), x[t][kt]);
         } else {
           u32x4 k = pairs(s.k[kt][i], ks);
-          if (c.d != D && (4 * i + g) * K::KN >= c.d) k = u32x4{};
+          if (c.d != D && K::k_channel(i, g) >= c.d) k = u32x4{};
 #pragma unroll
           for (int t = 0; t < NT; ++t) x[t][kt] = mfma(k, q[t][i], x[t][kt]);
         }
@@ -571,11 +595,14 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < K::VP; ++i) {
-          const f32x4 v = floats(s.v[0][j][i], K::SCALED ? scale_of_v(s, 0, j) : 1.f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int h = 0; h < K::VN; h += 4) {
+            const f32x4 v = floats(s.v[0][j][i], h / 4, K::SCALED ? scale_of_v(s, 0, j) : 1.f);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) o[t][i * 4 + e] = mfma(v[e], x[t][0][j], o[t][i * 4 + e]);
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int t = 0; t < NT; ++t) o[t][i * K::VN + h + e] = mfma(v[e], x[t][0][j], o[t][i * K::VN + h + e]);
+          }
         }
     } else {
 #pragma unroll
