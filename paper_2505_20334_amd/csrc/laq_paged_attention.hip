@@ -47,6 +47,8 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 acc) {
 }
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0); }
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // How the launch is cut, from what the host knows.
 struct AttPlan {
   int32_t tile;                          // score rows of a column
@@ -90,6 +92,11 @@ __device__ __forceinline__ int find_request(const PagedAttention& a, int G, int 
   return __builtin_amdgcn_readfirstlane(min(lo, a.n - 1));
 }
 
+// a / b of numbers that are not negative, in 32 bits where they fit (64 take a hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (uint64_t)(a | b) >> 32 ? (int64_t)((uint64_t)a / (uint64_t)b) : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 // What a column is: a tile of score rows of a request.
 struct Column {
   int row0, rows;                        // its first score row in the request, and their number (0: no such column)
@@ -102,6 +109,12 @@ __device__ __forceinline__ Column column_of(const Request& r, int G, int tile, i
   if (t < 0 || row0 >= all) return Column{0, 0, 0, 1, 0};
   return Column{(int)row0, (int)min((int64_t)tile, all - row0), r.token0, r.tokens, r.held};
 }
+
+// Where a share begins.
+struct Found {
+  Request r;
+  int request, head, tile, turn;
+};
 
 // Partial sums m (a score, not scaled), z and y of score rows, joined.
 __device__ __forceinline__ void join(float& m, float& z, f32x4& y, float m2, float z2, f32x4 y2, float scale2) {
@@ -295,17 +308,18 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
   __shared__ float sums[ATT_WAVES][16][K::PAD];
   __shared__ float2 marks[ATT_WAVES][16];
   __shared__ bool odds[ATT_WAVES];
-  __shared__ int64_t found[3];
+  __shared__ Found found;
   const int H = c.Hkv, G = a.Hq / H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
 
   // Where this workgroup begins.  All keys of all columns are a line of turns, request after request, of each its heads, of each its tiles, of each the turns
   // of the request's rows (a column of a request's earlier tokens has turns in which it sees nothing); a share is as many turns of it as any other.
-  int request, head;
-  int64_t tile_at, turn = 0, left = 1, total = 0, begin = 0;                 // turn in the column; turns of the share; of all; where the column begins on the line
+  Request req;
+  int request, head, turn = 0, more = 0;                                     // turn in the column; shares that have a turn more than the others
+  int64_t tile_at, left = 1, total = 0, each = 0, begin = 0;                 // turns of the share; of all; of a share; where the column begins on the line
   int shares = p.shares;
   if (shares) {
-    const int each = (a.n + ATT_THREADS - 1) / ATT_THREADS, i0 = min(a.n, (int)threadIdx.x * each), i1 = min(a.n, i0 + each);
+    const int per = (a.n + ATT_THREADS - 1) / ATT_THREADS, i0 = (int)min((int64_t)a.n, (int64_t)threadIdx.x * per), i1 = (int)min((int64_t)a.n, (int64_t)i0 + per);
     int64_t mine = 0, tiles = 0;
     for (int i = i0; i < i1; ++i) {
       const Request r = request_of(a, c.block_rows, i);
@@ -326,7 +340,7 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
       waves[wave][0] = upto;
       waves[wave][1] = tiles;
     }
-    if (threadIdx.x == 0) found[0] = -1;
+    if (threadIdx.x == 0) found.request = -1;
     __syncthreads();
     int64_t before = upto - mine, all_tiles = 0;
 #pragma unroll
@@ -342,47 +356,49 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
     if (shares > (total + MT - 1) / MT) shares = (int)((total + MT - 1) / MT);
     const int w = blockIdx.x;
     if (w >= shares) return;
-    const int64_t x0 = total * w / shares;
-    left = total * (w + 1) / shares - x0;
+    each = quotient(total, shares);
+    more = (int)(total - each * shares);
+    const int64_t x0 = each * w + min(w, more);
+    left = each + (w < more);
     if (x0 >= before && x0 < before + mine) {
       int64_t at = before;
       for (int i = i0; i < i1; ++i) {
         const Request r = request_of(a, c.block_rows, i);
-        const int64_t turns = (r.held + TURN - 1) / TURN + (r.held == 0), all = turns * H * tiles_of(r, G, p.tile);
+        const int turns = (r.held + TURN - 1) / TURN + (r.held == 0), tiles_here = tiles_of(r, G, p.tile);
+        const int64_t all = (int64_t)turns * H * tiles_here;
         if (x0 < at + all) {
-          found[0] = i;
-          found[1] = (x0 - at) / turns;
-          found[2] = (x0 - at) % turns;
+          const int64_t column = quotient(x0 - at, turns);
+          const int turn_at = (int)(x0 - at - column * turns), head_at = (int)column / tiles_here;      // (columns of a request: less than 2^31)
+          found = Found{r, i, head_at, (int)column - head_at * tiles_here, turn_at};
           break;
         }
         at += all;
       }
     }
     __syncthreads();
-    if (found[0] < 0) return;
-    request = __builtin_amdgcn_readfirstlane((int)found[0]);
-    const int tiles_here = tiles_of(request_of(a, c.block_rows, request), G, p.tile);
-    const int64_t column = found[1];
-    head = __builtin_amdgcn_readfirstlane((int)(column / tiles_here));
-    tile_at = __builtin_amdgcn_readfirstlane((int)(column % tiles_here));
-    turn = __builtin_amdgcn_readfirstlane((int)found[2]);
+    if (found.request < 0) return;
+    req = Request{uniform(found.r.token0), uniform(found.r.tokens), uniform(found.r.held)};
+    request = uniform(found.request);
+    head = uniform(found.head);
+    tile_at = uniform(found.tile);
+    turn = uniform(found.turn);
     begin = x0 - turn;
   } else {
     head = blockIdx.x % H;
     const int slot = blockIdx.x / H;
     request = find_request(a, G, p.tile, slot);
     tile_at = slot - first_column(a, G, p.tile, request);
+    req = request_of(a, c.block_rows, request);
   }
 
   for (;;) {
-  const Request req = request_of(a, c.block_rows, request);
   const Column col = column_of(req, G, p.tile, tile_at);
   const int turns = shares ? (req.held + TURN - 1) / TURN + (req.held == 0) : 1;
-  const int turns_here = (int)min((int64_t)turns - turn, left);
+  const int turns_here = (int)min((int64_t)(turns - turn), left);
   if (col.rows == 0 && !shares) return;
   const bool cut = shares && turns_here < turns;
-  const int keys = col.keys(G), from = (int)min((int64_t)keys, turn * TURN);
-  const int to = shares ? (int)min((int64_t)keys, (turn + turns_here) * TURN) : keys;
+  const int keys = col.keys(G), from = (int)min((int64_t)keys, (int64_t)turn * TURN);
+  const int to = shares ? (int)min((int64_t)keys, (int64_t)(turn + turns_here) * TURN) : keys;
 
   // the score rows of this lane's columns
   int last[NT];
@@ -704,7 +720,9 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
 
   if (cut) {
     // the workgroups of this column, and whether this one is the last of them
-    const int first = (int)(((begin + 1) * shares - 1) / total), count = (int)(((begin + turns) * shares - 1) / total) - first + 1;
+    const int64_t longer = (each + 1) * more;                                // turns of the shares that have one more
+    const auto share_of = [&](int64_t x) { return (int)(x < longer ? quotient(x, each + 1) : more + quotient(x - longer, each)); };
+    const int first = share_of(begin), count = share_of(begin + turns - 1) - first + 1;
     const auto place_of = [&](int k) { return 2 * (first + k) + (k == 0); };
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                         // (what this wave stored has arrived)
     __syncthreads();
@@ -727,9 +745,9 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
         float top = MINUS_INF, Z = 0.f;
         f32x4 y{};
 #ifndef FU
-#define FU 4
+#define FU 8
 #endif
-        constexpr int U = FU;
+        constexpr int U = NT == 1 ? FU : 4;
         if (on) {
           for (int k = grp; k < count; k += U * groups) {
             f32x2 mz[U], s0[U], s1[U];
@@ -768,7 +786,8 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
       head = 0;
       do {
         if (++request >= a.n) return;
-      } while (tiles_of(request_of(a, c.block_rows, request), G, p.tile) == 0);
+        req = request_of(a, c.block_rows, request);
+      } while (req.tokens == 0);
     }
   }
   __syncthreads();                                           // (the LDS is free)
