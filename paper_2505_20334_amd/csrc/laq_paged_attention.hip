@@ -29,15 +29,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-#ifndef MW
-#define MW 2
-#endif
-#ifndef RES
-#define RES 512
-#endif
-#ifndef RES64
-#define RES64 1024
-#endif
 constexpr int ATT_WAVES = 4, ATT_THREADS = 64 * ATT_WAVES;
 constexpr float MINUS_INF = -__builtin_inff();
 
@@ -217,6 +208,13 @@ __device__ __forceinline__ void drop_odd(Raw<E, N>& r) {
     for (int i = 0; i < (int)sizeof(r.x) / 4; ++i) r.x[i] = without_odd(r.x[i], E{});
   }
 }
+// Workgroups that a compute unit holds of a kernel: what their registers leave (the compiler is told to keep to it).
+constexpr int resident(bool f32, bool scaled, int d, int nt) {
+  if (d <= 64) return nt == 1 ? 3 : nt == 2 ? 2 : 1;
+  if (d <= 128) return nt == 1 ? 2 : nt == 2 ? (scaled && !f32 ? 1 : 2) : 1;
+  return 1;
+}
+
 // Q: the queries' numbers (and what the products are made in), E: the cache's, D: head sizes up to D, NT: 16 score rows NT times.
 template <typename Q, typename E, int D, int NT>
 struct Kinds {
@@ -226,6 +224,7 @@ struct Kinds {
   // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on
   static constexpr int KW = 16 / (KN * (int)sizeof(E));
   static constexpr __host__ __device__ int k_channel(int i, int g) { return i / KW * (4 * KW * KN) + g * (KW * KN) + i % KW * KN; }
+  static constexpr int RESIDENT = resident(F32, SCALED, D, NT);      // workgroups of a compute unit (a wave of each on every SIMD)
   static constexpr bool ONCE = NT == 1;                      // one workgroup reads a row: past the caches
   static constexpr int VN = std::is_same<E, float>::value || D == 64 ? 4 : 8, VP = D / (16 * VN);
   static constexpr int OT = D / 16;                          // output tiles
@@ -250,10 +249,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_of(const void* p, uint32_
 }
 template <bool ONCE, typename R>
 __device__ __forceinline__ void fetch(R& r, __amdgpu_buffer_rsrc_t tile, int at) {
-#ifndef NTV
-#define NTV 2
-#endif
-  constexpr int PAST = ONCE ? NTV : 0;                       // nt
+  constexpr int PAST = ONCE ? 2 : 0;                         // nt: 128 requests of 1000 to 8192 rows 371 us, without 416
   if constexpr (sizeof(r.x) == 16) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b128(tile, at, 0, PAST));
   else if constexpr (sizeof(r.x) == 8) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b64(tile, at, 0, PAST));
   else r.x = __builtin_amdgcn_raw_buffer_load_b32(tile, at, 0, PAST);
@@ -302,7 +298,7 @@ __device__ __forceinline__ void put_out(const PagedView& c, const PagedAttention
 }
 
 template <typename Q, typename E, int D, int NT>
-__global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
+__global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
   using K = Kinds<Q, E, D, NT>;
   constexpr int STEP = 16 * K::KT, TURN = STEP * ATT_WAVES;
   __shared__ float sums[ATT_WAVES][16][K::PAD];
@@ -350,10 +346,7 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
       all_tiles += waves[w][1];
     }
     if (all_tiles > p.columns || total <= 0) return;                         // (a start that makes no sense)
-#ifndef MT
-#define MT 1
-#endif
-    if (shares > (total + MT - 1) / MT) shares = (int)((total + MT - 1) / MT);
+    if (shares > total) shares = (int)total;
     const int w = blockIdx.x;
     if (w >= shares) return;
     each = quotient(total, shares);
@@ -744,10 +737,7 @@ __global__ __launch_bounds__(ATT_THREADS, D <= 128 && NT == 1 ? MW : 1) void pag
         const bool on = item < items && grp < groups;
         float top = MINUS_INF, Z = 0.f;
         f32x4 y{};
-#ifndef FU
-#define FU 8
-#endif
-        constexpr int U = NT == 1 ? FU : 4;
+        constexpr int U = NT == 1 ? 8 : 4;
         if (on) {
           for (int k = grp; k < count; k += U * groups) {
             f32x2 mz[U], s0[U], s1[U];
@@ -802,8 +792,7 @@ int tiles_of_rows(int dtype, int d, int n, int64_t n_tokens, int G) {
   return rows <= 16 || most == 1 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
 }
 
-// Workgroups that share a call out: as many as the device holds of the kernels (256 compute units; registers).
-int resident(int d) { return d <= 64 ? RES64 : d <= 128 ? RES : 256; }
+constexpr int COMPUTE_UNITS = 256;
 
 // max_rows 0: the most shares that a call of any bound has.
 AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, bool has_start, int max_rows, bool may_share) {
@@ -812,11 +801,11 @@ AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, 
   p.tile = 16 * tiles_of_rows(dtype, c.d, n, n_tokens, G);
   const int64_t columns = has_start ? n_tokens * G / p.tile + n : (int64_t)n * ((G + p.tile - 1) / p.tile);
   p.columns = (int32_t)(columns < 0x7fffffff ? columns : 0x7fffffff);
-  p.shares = may_share ? resident(c.d) : 0;
+  p.shares = may_share ? COMPUTE_UNITS * resident(dtype == LAQ_F32, c.type == LAQ_E4M3, c.d, p.tile / 16) : 0;
   if (may_share && max_rows > 0) {
     const int turn = ATT_WAVES * 16 * (dtype == LAQ_F32 ? 1 : c.type == LAQ_E4M3 ? 4 : 2);
     const int64_t turns = columns * c.Hkv * (((int64_t)max_rows + turn - 1) / turn);
-    if ((turns + MT - 1) / MT < p.shares) p.shares = (int32_t)((turns + MT - 1) / MT);
+    if (turns < p.shares) p.shares = (int32_t)turns;
   }
   return p;
 }
