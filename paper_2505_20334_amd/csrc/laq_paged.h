@@ -8,6 +8,8 @@ namespace laq {
 
 struct E4m3 { uint8_t x; };              // a number of a cache in 8 bits
 
+constexpr int COMPUTE_UNITS = 256;
+
 struct PagedPlane {                      // K or V
   void* x;
   uint8_t* scales;
@@ -75,6 +77,29 @@ struct PagedAttention {
   void* out;
   float* lse;
 };
+// How the launch is cut, from what the host knows.
+struct AttPlan {
+  int32_t tile;                          // score rows of a column
+  int32_t columns;                       // columns of a KV head over all requests, at most
+  int32_t shares;                        // workgroups that share all keys of all columns out evenly; 0: one workgroup a column
+};
+
+// The ranges of columns that several workgroups share.  A workgroup has two places: 2w for a column that began in another workgroup's share, 2w + 1 for one
+// that begins in its own and goes on; a place has mz[tile] (m and z), sums[tile][d] and a mark.  A workgroup that is done with a range writes the launch's nonce
+// there, after its sums have arrived, and then looks at the marks of all ranges of the column: who finds all of them joins the ranges, in their order, and
+// clears the marks, so that a replayed launch, whose nonce is the same, finds none of its own; whatever else lies in the workspace is no mark.  Two may find all
+// of them (both write the same); one that comes to look when another has begun to clear finds that it is not needed.  (Counting in by compare and swap: 64
+// workgroups of a column take turns, one request of 32768 rows x 8 heads 61 us.)
+struct Partials {
+  unsigned long long* marks;
+  float2* mz;
+  float* sums;
+  uint32_t nonce;
+};
+
+// chunks of a prompt: whether that kernel takes a call, and the call
+bool paged_prompt_call(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens);
+hipError_t launch_paged_prompt(const PagedView& c, const PagedAttention& a, hipStream_t st);
 size_t paged_attention_bytes(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, int max_rows);
 bool paged_attention_fits(const PagedView& c, int dtype, const PagedAttention& a, bool cut);      // in a launch
 hipError_t launch_paged_attention(const PagedView& c, int dtype, const PagedAttention& a, void* ws, hipStream_t st);

@@ -14,204 +14,23 @@
 // A lane's pieces of V are VN channels: its product row m of product e of piece h is channel (16 h + m) VN + e.
 #include <atomic>
 #include <chrono>
-#include <type_traits>
 
-#include "laq_paged.h"
+#include "laq_paged_columns.h"
 
 namespace laq {
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
 constexpr int ATT_WAVES = 4, ATT_THREADS = 64 * ATT_WAVES;
-constexpr float MINUS_INF = -__builtin_inff();
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 acc) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
 }
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0); }
 
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// How the launch is cut, from what the host knows.
-struct AttPlan {
-  int32_t tile;                          // score rows of a column
-  int32_t columns;                       // columns of a KV head over all requests, at most
-  int32_t shares;                        // workgroups that share all keys of all columns out evenly; 0: one workgroup a column
-};
-
-// A request of the call.
-struct Request {
-  int token0, tokens, held;              // tokens 0: none, or numbers that make no sense; held: rows of the cache
-};
-__device__ __forceinline__ Request request_of(const PagedAttention& a, int block_rows, int i) {
-  Request r{i, 1, 0};
-  if (a.start) {
-    const int64_t t0 = a.start[i], t1 = a.start[i + 1];
-    r.token0 = (int)t0;
-    r.tokens = t0 < 0 || t1 <= t0 || t1 > a.n_tokens ? 0 : (int)(t1 - t0);
-  }
-  r.held = max(0, min(a.rows[i], a.blocks_per_inst * block_rows));
-  return r;
-}
-__device__ __forceinline__ int tiles_of(const Request& r, int G, int tile) { return (int)(((int64_t)r.tokens * G + tile - 1) / tile); }
-
-// Where the columns of a request begin if every column has a workgroup: a request of R score rows has ceil(R / tile) columns, and floor(R' / tile) + i, with R'
-// score rows and i requests before it, leaves at least that many between one request and the next.
-__device__ __forceinline__ int64_t first_column(const PagedAttention& a, int G, int tile, int i) {
-  return a.start ? (int64_t)a.start[i] * G / tile + i : (int64_t)i * ((G + tile - 1) / tile);
-}
-// The last request that begins at column `slot` or before it: 64 looked at at a time.
-__device__ __forceinline__ int find_request(const PagedAttention& a, int G, int tile, int slot) {
-  if (!a.start) return min(slot / ((G + tile - 1) / tile), a.n - 1);
-  int lo = 0, n = a.n;
-  const int lane = threadIdx.x & 63;
-  while (n > 1) {
-    const int step = (n + 63) / 64, i = lo + lane * step;
-    const bool before = lane * step < n && first_column(a, G, tile, i) <= slot;
-    const int at = max(__popcll(__ballot(before)) - 1, 0) * step;
-    lo += at;
-    n = max(min(step, n - at), 1);
-  }
-  return __builtin_amdgcn_readfirstlane(min(lo, a.n - 1));
-}
-
-// a / b of numbers that are not negative, in 32 bits where they fit (64 take a hundred instructions).
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  return (uint64_t)(a | b) >> 32 ? (int64_t)((uint64_t)a / (uint64_t)b) : (int64_t)((uint32_t)a / (uint32_t)b);
-}
-
-// What a column is: a tile of score rows of a request.
-struct Column {
-  int row0, rows;                        // its first score row in the request, and their number (0: no such column)
-  int token0, tokens, held;              // of the request
-  __device__ int last(int row, int G) const { return held - tokens + (row0 + row) / G; }      // the last key that a score row sees
-  __device__ int keys(int G) const { return max(0, last(rows - 1, G) + 1); }
-};
-__device__ __forceinline__ Column column_of(const Request& r, int G, int tile, int64_t t) {
-  const int64_t row0 = t * tile, all = (int64_t)r.tokens * G;
-  if (t < 0 || row0 >= all) return Column{0, 0, 0, 1, 0};
-  return Column{(int)row0, (int)min((int64_t)tile, all - row0), r.token0, r.tokens, r.held};
-}
-
-// Where a share begins.
-struct Found {
-  Request r;
-  int request, head, tile, turn;
-};
-
-// Partial sums m (a score, not scaled), z and y of score rows, joined.
-__device__ __forceinline__ void join(float& m, float& z, f32x4& y, float m2, float z2, f32x4 y2, float scale2) {
-  const float top = fmaxf(m, m2);
-  const float by = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale2), by2 = m2 == top ? 1.f : __builtin_amdgcn_exp2f((m2 - top) * scale2);
-  m = top;
-  z = z * by + z2 * by2;
-  y = y * by + y2 * by2;
-}
-
-// Written through to the device's memory, and read from there.
-__device__ __forceinline__ void store_pair(void* p, float a, float b) {
-  __hip_atomic_store(static_cast<unsigned long long*>(p), (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ f32x2 load_pair(const void* p) {
-  const unsigned long long v = __hip_atomic_load(static_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
-}
-
-// N numbers of the cache in a row, as they lie.
-template <typename E, int N> struct Raw;
-template <> struct Raw<float, 4> { u32x4 x; };
-template <> struct Raw<uint16_t, 8> { u32x4 x; };
-template <> struct Raw<uint16_t, 4> { u32x2 x; };
-template <> struct Raw<E4m3, 8> { u32x2 x; };
-template <> struct Raw<E4m3, 4> { uint32_t x; };
-
-template <typename R> __device__ __forceinline__ void clear(R& r) { r.x = {}; }
-
-// As pairs of bf16 (scale: of 8 bits).
-__device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, bool high) {
-  return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))
-              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false));
-}
-__device__ __forceinline__ u32x4 pairs(const Raw<uint16_t, 8>& r, float) { return r.x; }
-__device__ __forceinline__ u32x2 pairs(const Raw<uint16_t, 4>& r, float) { return r.x; }
-__device__ __forceinline__ u32x4 pairs(const Raw<E4m3, 8>& r, float s) {
-  return u32x4{pair_of(r.x[0], s, false), pair_of(r.x[0], s, true), pair_of(r.x[1], s, false), pair_of(r.x[1], s, true)};
-}
-__device__ __forceinline__ u32x2 pairs(const Raw<E4m3, 4>& r, float s) { return u32x2{pair_of(r.x, s, false), pair_of(r.x, s, true)}; }
-// As fp32: numbers 4 part and on.
-__device__ __forceinline__ f32x4 floats(const Raw<float, 4>& r, int, float) { return __builtin_bit_cast(f32x4, r.x); }
-__device__ __forceinline__ f32x4 floats(const Raw<uint16_t, 4>& r, int, float) {
-  return __builtin_bit_cast(f32x4, (u32x4{r.x[0] << 16, r.x[0] & 0xffff0000u, r.x[1] << 16, r.x[1] & 0xffff0000u}));
-}
-__device__ __forceinline__ f32x4 floats(const Raw<uint16_t, 8>& r, int part, float) { return floats(Raw<uint16_t, 4>{u32x2{r.x[2 * part], r.x[2 * part + 1]}}, 0, 0.f); }
-__device__ __forceinline__ f32x4 floats(const Raw<E4m3, 4>& r, int, float s) {
-  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(r.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(r.x, true);
-  return f32x4{a[0] * s, a[1] * s, b[0] * s, b[1] * s};
-}
-__device__ __forceinline__ f32x4 floats(const Raw<E4m3, 8>& r, int part, float s) { return floats(Raw<E4m3, 4>{r.x[part]}, 0, s); }
-
-// A number of a row of V.
-__device__ __forceinline__ float number(const float* row, int i, uint32_t) { return row[i]; }
-__device__ __forceinline__ float number(const uint16_t* row, int i, uint32_t) { return __uint_as_float((uint32_t)row[i] << 16); }
-__device__ __forceinline__ float number(const E4m3* row, int i, uint32_t scale) {
-  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(row[i].x, false);
-  return a[0] * e4m3_scale_value(scale);
-}
-
-// Infinities and NaN among numbers of V.
-template <typename E, int N>
-__device__ __forceinline__ bool has_odd(const Raw<E, N>& r, uint32_t scale) {
-  bool odd = false;
-  if constexpr (std::is_same<E, float>::value) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) odd |= (r.x[i] & 0x7f800000u) == 0x7f800000u;
-  } else if constexpr (std::is_same<E, uint16_t>::value) {
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) odd |= (r.x[i] & 0x7f800000u) == 0x7f800000u || (r.x[i] & 0x7f80u) == 0x7f80u;
-  } else {
-    odd = scale == 255u;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint32_t w;
-      if constexpr (N == 4) w = r.x;
-      else w = r.x[i / 4];
-      odd |= (w >> (8 * (i % 4)) & 0x7fu) == 0x7fu;
-    }
-  }
-  return odd;
-}
-// 0 in their place.
-__device__ __forceinline__ uint32_t without_odd(uint32_t w, float) { return (w & 0x7f800000u) == 0x7f800000u ? 0u : w; }
-__device__ __forceinline__ uint32_t without_odd(uint32_t w, uint16_t) {
-  return ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u) | ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu);
-}
-__device__ __forceinline__ uint32_t without_odd(uint32_t w, E4m3) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r |= (w >> (8 * i) & 0x7fu) == 0x7fu ? 0u : w & 255u << (8 * i);
-  return r;
-}
-template <typename E, int N>
-__device__ __forceinline__ void drop_odd(Raw<E, N>& r) {
-  if constexpr (sizeof(r.x) == 4) {
-    r.x = without_odd(r.x, E{});
-  } else {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(r.x) / 4; ++i) r.x[i] = without_odd(r.x[i], E{});
-  }
-}
 // Workgroups that a compute unit holds of a kernel: what their registers leave (the compiler is told to keep to it).
 constexpr int resident(bool f32, bool scaled, int d, int nt) {
-  if (d <= 64) return nt == 1 ? 3 : nt == 2 ? 2 : 1;
-  if (d <= 128) return nt == 1 ? 2 : nt == 2 ? (scaled && !f32 ? 1 : 2) : 1;
+  if (d <= 64) return nt == 1 ? 3 : 2;
+  if (d <= 128) return nt == 1 || f32 || !scaled ? 2 : 1;
   return 1;
 }
 
@@ -241,20 +60,6 @@ struct StepKeys {
   int64_t base[K::KT], scales[K::KT];
   uint32_t bytes[K::KT];
 };
-// A tile's rows, read through a buffer descriptor: reads behind its end give zeros without memory traffic, and nothing at all is read of a tile that is not
-// there.  So the reads of a step are issued whatever the step has, and the wait for a step's keys can leave those of the next one on their way (with
-// branches around them it waited for both: 96 requests x 8 heads x 6144 rows 428 us).
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_of(const void* p, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
-}
-template <bool ONCE, typename R>
-__device__ __forceinline__ void fetch(R& r, __amdgpu_buffer_rsrc_t tile, int at) {
-  constexpr int PAST = ONCE ? 2 : 0;                         // nt: 128 requests of 1000 to 8192 rows 371 us, without 416
-  if constexpr (sizeof(r.x) == 16) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b128(tile, at, 0, PAST));
-  else if constexpr (sizeof(r.x) == 8) r.x = __builtin_bit_cast(decltype(r.x), __builtin_amdgcn_raw_buffer_load_b64(tile, at, 0, PAST));
-  else r.x = __builtin_amdgcn_raw_buffer_load_b32(tile, at, 0, PAST);
-}
-
 // W pieces side by side, 16 bytes together.
 template <bool ONCE, int W, typename R>
 __device__ __forceinline__ void fetch_wide(R* r, __amdgpu_buffer_rsrc_t tile, int at) {
@@ -271,32 +76,6 @@ __device__ __forceinline__ void fetch_wide(R* r, __amdgpu_buffer_rsrc_t tile, in
   }
 }
 
-// The ranges of columns that several workgroups share.  A workgroup has two places: 2w for a column that began in another workgroup's share, 2w + 1 for one
-// that begins in its own and goes on; a place has mz[tile] (m and z), sums[tile][d] and a mark.  A workgroup that is done with a range writes the launch's nonce
-// there, after its sums have arrived, and then looks at the marks of all ranges of the column: who finds all of them joins the ranges, in their order, and
-// clears the marks, so that a replayed launch, whose nonce is the same, finds none of its own; whatever else lies in the workspace is no mark.  Two may find all
-// of them (both write the same); one that comes to look when another has begun to clear finds that it is not needed.  (Counting in by compare and swap: 64
-// workgroups of a column take turns, one request of 32768 rows x 8 heads 61 us.)
-struct Partials {
-  unsigned long long* marks;
-  float2* mz;
-  float* sums;
-  uint32_t nonce;
-};
-
-// Four numbers of the output from sums and the sum of weights, and the logarithm.
-template <typename Q>
-__device__ __forceinline__ void put_out(const PagedView& c, const PagedAttention& a, const Column& col, int head, int G, int r, int at, float m, float z, f32x4 y) {
-  const int row = col.row0 + r;
-  const int64_t to = (int64_t)(col.token0 + row / G) * a.Hq + head * G + row % G;
-  const float inv = z == 0.f ? 0.f : 1.f / z;
-  if (at == 0 && a.lse) a.lse[to] = z == 0.f ? MINUS_INF : (__builtin_amdgcn_logf(z) + m * a.scale2) * 0.69314718055994530942f;
-  if constexpr (std::is_same<Q, float>::value)
-    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to * c.d + at) = y * inv;
-  else
-    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to * c.d + at) = u32x2{pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv)};
-}
-
 template <typename Q, typename E, int D, int NT>
 __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
   using K = Kinds<Q, E, D, NT>;
@@ -304,94 +83,20 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
   __shared__ float sums[ATT_WAVES][16][K::PAD];
   __shared__ float2 marks[ATT_WAVES][16];
   __shared__ bool odds[ATT_WAVES];
-  __shared__ Found found;
   const int H = c.Hkv, G = a.Hq / H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
 
-  // Where this workgroup begins.  All keys of all columns are a line of turns, request after request, of each its heads, of each its tiles, of each the turns
-  // of the request's rows (a column of a request's earlier tokens has turns in which it sees nothing); a share is as many turns of it as any other.
-  Request req;
-  int request, head, turn = 0, more = 0;                                     // turn in the column; shares that have a turn more than the others
-  int64_t tile_at, left = 1, total = 0, each = 0, begin = 0;                 // turns of the share; of all; of a share; where the column begins on the line
-  int shares = p.shares;
-  if (shares) {
-    const int per = (a.n + ATT_THREADS - 1) / ATT_THREADS, i0 = (int)min((int64_t)a.n, (int64_t)threadIdx.x * per), i1 = (int)min((int64_t)a.n, (int64_t)i0 + per);
-    int64_t mine = 0, tiles = 0;
-    for (int i = i0; i < i1; ++i) {
-      const Request r = request_of(a, c.block_rows, i);
-      const int64_t t = tiles_of(r, G, p.tile);
-      tiles += t;
-      mine += t * H * ((r.held + TURN - 1) / TURN + (r.held == 0));
-    }
-    // sums over the lanes before this one, then over the waves
-    int64_t upto = mine;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-      const int64_t below = __shfl_up(upto, m);
-      if (lane >= m) upto += below;
-      tiles += __shfl_xor(tiles, m);
-    }
-    __shared__ int64_t waves[ATT_WAVES][2];
-    if (lane == 63) {
-      waves[wave][0] = upto;
-      waves[wave][1] = tiles;
-    }
-    if (threadIdx.x == 0) found.request = -1;
-    __syncthreads();
-    int64_t before = upto - mine, all_tiles = 0;
-#pragma unroll
-    for (int w = 0; w < ATT_WAVES; ++w) {
-      if (w < wave) before += waves[w][0];
-      total += waves[w][0];
-      all_tiles += waves[w][1];
-    }
-    if (all_tiles > p.columns || total <= 0) return;                         // (a start that makes no sense)
-    if (shares > total) shares = (int)total;
-    const int w = blockIdx.x;
-    if (w >= shares) return;
-    each = quotient(total, shares);
-    more = (int)(total - each * shares);
-    const int64_t x0 = each * w + min(w, more);
-    left = each + (w < more);
-    if (x0 >= before && x0 < before + mine) {
-      int64_t at = before;
-      for (int i = i0; i < i1; ++i) {
-        const Request r = request_of(a, c.block_rows, i);
-        const int turns = (r.held + TURN - 1) / TURN + (r.held == 0), tiles_here = tiles_of(r, G, p.tile);
-        const int64_t all = (int64_t)turns * H * tiles_here;
-        if (x0 < at + all) {
-          const int64_t column = quotient(x0 - at, turns);
-          const int turn_at = (int)(x0 - at - column * turns), head_at = (int)column / tiles_here;      // (columns of a request: less than 2^31)
-          found = Found{r, i, head_at, (int)column - head_at * tiles_here, turn_at};
-          break;
-        }
-        at += all;
-      }
-    }
-    __syncthreads();
-    if (found.request < 0) return;
-    req = Request{uniform(found.r.token0), uniform(found.r.tokens), uniform(found.r.held)};
-    request = uniform(found.request);
-    head = uniform(found.head);
-    tile_at = uniform(found.tile);
-    turn = uniform(found.turn);
-    begin = x0 - turn;
-  } else {
-    head = blockIdx.x % H;
-    const int slot = blockIdx.x / H;
-    request = find_request(a, G, p.tile, slot);
-    tile_at = slot - first_column(a, G, p.tile, request);
-    req = request_of(a, c.block_rows, request);
-  }
+  __shared__ ShareScan<ATT_WAVES> scan;
+  Share sh;
+  if (!first_range<ATT_THREADS, TURN>(c, a, G, p, scan, sh)) return;
 
   for (;;) {
-  const Column col = column_of(req, G, p.tile, tile_at);
-  const int turns = shares ? (req.held + TURN - 1) / TURN + (req.held == 0) : 1;
-  const int turns_here = (int)min((int64_t)(turns - turn), left);
-  if (col.rows == 0 && !shares) return;
-  const bool cut = shares && turns_here < turns;
-  const int keys = col.keys(G), from = (int)min((int64_t)keys, (int64_t)turn * TURN);
-  const int to = shares ? (int)min((int64_t)keys, (int64_t)(turn + turns_here) * TURN) : keys;
+  const Column col = column_of(sh.req, G, p.tile, sh.tile);
+  const int turns = p.shares ? turns_of<TURN>(sh.req) : 1, turns_here = (int)min((int64_t)(turns - sh.turn), sh.left), head = sh.head;
+  if (col.rows == 0 && !p.shares) return;
+  const bool cut = p.shares && turns_here < turns;
+  const int keys = col.keys(G), from = (int)min((int64_t)keys, (int64_t)sh.turn * TURN);
+  const int to = p.shares ? (int)min((int64_t)keys, (int64_t)(sh.turn + turns_here) * TURN) : keys;
 
   // the score rows of this lane's columns
   int last[NT];
@@ -432,7 +137,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
   for (int j = 0; j < 4; ++j) v_at[j] = (4 * g + j) * row_bytes + n * (K::VN * (int)sizeof(E));
   const E *kx = static_cast<const E*>(c.k.x) + head * c.head, *vx = static_cast<const E*>(c.v.x) + head * c.head;
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
-  const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)request * a.blocks_per_inst);
+  const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)sh.request * a.blocks_per_inst);
 
   // this wave's steps: keys from + (wave + 4 i) * STEP on.  Its place in the blocks moves with it, and the blocks' numbers are asked for a step ahead
   struct Place { int page, off; } at{0, 0};
@@ -659,8 +364,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
   // the waves' sums, score rows of 16 at a time
   const bool wave_odd = __any(odd);
   if (lane == 0) odds[wave] = wave_odd;
-  const int w = blockIdx.x;
-  const int64_t place = (int64_t)(2 * w + (turn == 0)) * p.tile;
+  const int64_t place = (int64_t)sh.place() * p.tile;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     float zt = z[t];
@@ -709,99 +413,28 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
       }
     }
   }
-  if (!shares) return;
-
-  if (cut) {
-    // the workgroups of this column, and whether this one is the last of them
-    const int64_t longer = (each + 1) * more;                                // turns of the shares that have one more
-    const auto share_of = [&](int64_t x) { return (int)(x < longer ? quotient(x, each + 1) : more + quotient(x - longer, each)); };
-    const int first = share_of(begin), count = share_of(begin + turns - 1) - first + 1;
-    const auto place_of = [&](int k) { return 2 * (first + k) + (k == 0); };
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                         // (what this wave stored has arrived)
-    __syncthreads();
-    if (threadIdx.x == 0) __hip_atomic_store(part.marks + 2 * w + (turn == 0), (unsigned long long)part.nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    bool all = true;
-    for (int k = threadIdx.x; k < count; k += ATT_THREADS)
-      all &= __hip_atomic_load(part.marks + place_of(k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == part.nonce;
-    if (__syncthreads_and(all)) {
-      for (int k = threadIdx.x; k < count; k += ATT_THREADS) __hip_atomic_store(part.marks + place_of(k), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      // four channels of a row a thread, and as many groups of ranges as there are threads for
-      const int per = c.d / 4, items = col.rows * per, groups = max(1, min(count, ATT_THREADS / items));
-      float* const shared_sums = &sums[0][0][0];                             // [ATT_THREADS][4], then m and z
-      f32x2* const shared_mz = reinterpret_cast<f32x2*>(shared_sums + 4 * ATT_THREADS);
-      for (int i0 = 0; i0 < items; i0 += groups > 1 ? items : ATT_THREADS) {
-        const int grp = groups > 1 ? threadIdx.x / items : 0, item = groups > 1 ? threadIdx.x % items : i0 + threadIdx.x;
-        const int r = item / per, at = item % per * 4;
-        const bool on = item < items && grp < groups;
-        float top = MINUS_INF, Z = 0.f;
-        f32x4 y{};
-        constexpr int U = NT == 1 ? 8 : 4;
-        if (on) {
-          for (int k = grp; k < count; k += U * groups) {
-            f32x2 mz[U], s0[U], s1[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-              const int kk = min(k + u * groups, count - 1);
-              const int64_t row = (int64_t)place_of(kk) * p.tile + r;
-              mz[u] = load_pair(part.mz + row);
-              s0[u] = load_pair(part.sums + row * c.d + at);
-              s1[u] = load_pair(part.sums + row * c.d + at + 2);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-              if (k + u * groups < count) join(top, Z, y, mz[u][0], mz[u][1], f32x4{s0[u][0], s0[u][1], s1[u][0], s1[u][1]}, a.scale2);
-          }
-        }
-        if (groups > 1) {
-          *reinterpret_cast<f32x4*>(shared_sums + 4 * threadIdx.x) = y;
-          shared_mz[threadIdx.x] = f32x2{top, Z};
-          __syncthreads();
-          for (int k = 1; on && grp == 0 && k < groups; ++k)
-            join(top, Z, y, shared_mz[k * items + item][0], shared_mz[k * items + item][1], *reinterpret_cast<const f32x4*>(shared_sums + 4 * (k * items + item)), a.scale2);
-        }
-        if (on && grp == 0) put_out<Q>(c, a, col, head, G, r, at, top, Z, y);
-      }
-    }
-  }
-  left -= turns_here;
-  if (left <= 0) return;
-  // the next column
-  begin += turns;
-  turn = 0;
-  if (++tile_at >= tiles_of(req, G, p.tile)) {
-    tile_at = 0;
-    if (++head == H) {
-      head = 0;
-      do {
-        if (++request >= a.n) return;
-        req = request_of(a, c.block_rows, request);
-      } while (req.tokens == 0);
-    }
-  }
+  if (!p.shares) return;
+  if (cut) join_ranges<Q, ATT_THREADS, NT == 1 ? 8 : 4, 1>(c, a, part, sh, col, G, p.tile, turns, &sums[0][0][0]);
+  if (!next_column<TURN>(c, a, G, p.tile, turns, turns_here, sh)) return;
   __syncthreads();                                           // (the LDS is free)
   }
 }
 
 // ---- the host's part -------------------------------------------------------------------------
 
-int tiles_of_rows(int dtype, int d, int n, int64_t n_tokens, int G) {
+int tiles_of_rows(int d, int n, int64_t n_tokens, int G) {
   const int64_t rows = (n_tokens + n - 1) / n * G;                   // of a request, on average
-  const int most = d > 128 ? 1 : dtype == LAQ_F32 ? 2 : 4;
-  return rows <= 16 || most == 1 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+  return rows <= 16 || d > 128 ? 1 : 2;
 }
-
-constexpr int COMPUTE_UNITS = 256;
 
 // max_rows 0: the most shares that a call of any bound has.
 AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, bool has_start, int max_rows, bool may_share) {
   const int G = Hq / c.Hkv;
   AttPlan p;
-  p.tile = 16 * tiles_of_rows(dtype, c.d, n, n_tokens, G);
+  p.tile = 16 * tiles_of_rows(c.d, n, n_tokens, G);
   const int64_t columns = has_start ? n_tokens * G / p.tile + n : (int64_t)n * ((G + p.tile - 1) / p.tile);
   p.columns = (int32_t)(columns < 0x7fffffff ? columns : 0x7fffffff);
-  p.shares = may_share ? COMPUTE_UNITS * resident(dtype == LAQ_F32, c.type == LAQ_E4M3, c.d, p.tile / 16) : 0;
+  p.shares = !may_share ? 0 : COMPUTE_UNITS * resident(dtype == LAQ_F32, c.type == LAQ_E4M3, c.d, p.tile / 16);
   if (may_share && max_rows > 0) {
     const int turn = ATT_WAVES * 16 * (dtype == LAQ_F32 ? 1 : c.type == LAQ_E4M3 ? 4 : 2);
     const int64_t turns = columns * c.Hkv * (((int64_t)max_rows + turn - 1) / turn);
@@ -822,15 +455,13 @@ Bytes bytes_of(const PagedView& c, const AttPlan& p) {
 template <typename Q, typename E, int D>
 hipError_t start_attention(const PagedView& c, const PagedAttention& a, const AttPlan& p, const Partials& part, hipStream_t st) {
   const dim3 grid((unsigned)(p.shares ? p.shares : (int64_t)p.columns * c.Hkv));
-  switch (p.tile) {
-    case 16: hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 1>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part); break;
-    case 32:
-      if constexpr (D <= 128) hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 2>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
-      break;
-    default:
-      if constexpr (!std::is_same<Q, float>::value && D <= 128)
-        hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 4>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
+  if constexpr (D <= 128) {
+    if (p.tile == 32) {
+      hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 2>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
+      return hipGetLastError();
+    }
   }
+  hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 1>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
   return hipGetLastError();
 }
 
@@ -844,15 +475,17 @@ hipError_t by_size(const PagedView& c, const PagedAttention& a, const AttPlan& p
 }  // namespace
 
 size_t paged_attention_bytes(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, int) {
+  if (paged_prompt_call(c, Hq, dtype, n, n_tokens)) return 0;
   return bytes_of(c, plan_of(c, Hq, dtype, n, n_tokens, true, 0, true)).all();
 }
 
 bool paged_attention_fits(const PagedView& c, int dtype, const PagedAttention& a, bool cut) {
   const AttPlan p = plan_of(c, a.Hq, dtype, a.n, a.n_tokens, a.start != nullptr, a.max_rows, cut);
-  return p.shares || (int64_t)p.columns * c.Hkv < (1 << 24);
+  return paged_prompt_call(c, a.Hq, dtype, a.n, a.n_tokens) || p.shares || (int64_t)p.columns * c.Hkv < (1 << 24);
 }
 
 hipError_t launch_paged_attention(const PagedView& c, int dtype, const PagedAttention& a, void* ws, hipStream_t st) {
+  if (paged_prompt_call(c, a.Hq, dtype, a.n, a.n_tokens)) return launch_paged_prompt(c, a, st);
   static std::atomic<uint32_t> launches{(uint32_t)(std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull >> 32)};
   const AttPlan p = plan_of(c, a.Hq, dtype, a.n, a.n_tokens, a.start != nullptr, a.max_rows, ws != nullptr);
   const Bytes b = bytes_of(c, p);

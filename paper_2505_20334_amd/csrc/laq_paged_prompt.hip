@@ -1,0 +1,334 @@
+// Attention of many tokens of a request over the paged cache, bf16 (laq_cache_attention for chunks of a prompt).
+//
+// A workgroup has a column of 128 score rows, a wave 32 of them, and goes through all keys that they see, 64 at a time, which lie in LDS for the four waves
+// (two stages in turn: the next one is read while one is used; 8 bits become bf16 on the way).  Products are 32 x 32 x 16 with the keys (S^T = K Q^T), then the
+// channels (O^T = V^T P^T), as the first operand's rows: a lane has 16 keys of one score row of each 32, and they are, as they are, its part of P^T.  V^T is read
+// from LDS by its transposing read.  The 16-byte pieces of a row change places with the row's number so that reads meet in no bank.
+// One pass, exponentials of s - m with a reference m that moves only when a score is more than 8 above it.
+#include "laq_paged_columns.h"
+
+namespace laq {
+
+namespace {
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES, WAVE_ROWS = 32, TILE = WAVES * WAVE_ROWS, STAGE = 64;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* LdsQuad;
+
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 acc) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+
+// Where piece `piece` (eight numbers) of row `row` lies in LDS, in numbers.
+template <int D> __device__ __forceinline__ int k_place(int row, int piece) { return row * D + (piece ^ (row & (D / 8 - 1))) * 8; }
+// (the transposing read takes half pieces of four rows at a time)
+template <int D> __device__ __forceinline__ int v_place(int row, int piece) { return row * D + (piece ^ ((D == 64 ? row >> 1 & 1 : row & 3) << 2)) * 8; }
+
+// Column number `rank` in the order in which the workgroups of up to 64 requests take them: requests with the most rows first, of each the last tiles first.
+// The first 256 workgroups go to a compute unit each, the second 256 beside them, these in the opposite order, so that long columns lie beside short ones.
+__device__ __forceinline__ bool ranked_column(const PagedView& c, const PagedAttention& a, int G, int H, int rank, int* request, int64_t* tile, Request* req) {
+  const int lane = threadIdx.x & 63;
+  Request r{0, 0, 0};
+  if (lane < a.n) r = request_of(a, c.block_rows, lane);
+  const int tiles = lane < a.n ? tiles_of(r, G, TILE) : 0;
+  int before = 0, all = 0;                                             // tiles of requests that come first; of all
+  for (int i = 0; i < a.n; ++i) {
+    const int held = __builtin_amdgcn_readlane(r.held, i), t = __builtin_amdgcn_readlane(tiles, i);
+    if (held > r.held || (held == r.held && i < lane)) before += t;
+    all += t;
+  }
+  const int round = COMPUTE_UNITS / H;
+  if (rank >= round && rank < 2 * round) rank = round + min(2 * round, all) - 1 - rank;
+  if (rank >= all) return false;
+  const uint64_t mine = __ballot(rank >= before && rank < before + tiles);
+  if (mine == 0) return false;
+  const int l = __builtin_ctzll(mine);
+  *request = l;
+  *tile = __builtin_amdgcn_readlane(tiles, l) - 1 - (rank - __builtin_amdgcn_readlane(before, l));
+  *req = Request{__builtin_amdgcn_readlane(r.token0, l), __builtin_amdgcn_readlane(r.tokens, l), __builtin_amdgcn_readlane(r.held, l)};
+  return true;
+}
+
+template <typename E, int D>
+__global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, PagedAttention a) {
+  constexpr bool SCALED = std::is_same<E, E4m3>::value;
+  constexpr int PIECES = D / 8, ROWS = THREADS / PIECES, PASSES = STAGE / ROWS;     // of a row; rows that the workgroup reads at once
+  constexpr int KS = D / 16, DT = D / 32;
+  __shared__ alignas(16) uint16_t k_lds[2][STAGE * D], v_lds[2][STAGE * D];
+  const int H = c.Hkv, G = a.Hq / H;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  const int head = blockIdx.x % H;
+  int request;
+  int64_t tile;
+  Request req;
+  if (a.n <= 64) {
+    if (!ranked_column(c, a, G, H, blockIdx.x / H, &request, &tile, &req)) return;
+  } else {
+    const int slot = blockIdx.x / H;
+    request = find_request(a, G, TILE, slot);
+    tile = slot - first_column(a, G, TILE, request);
+    req = request_of(a, c.block_rows, request);
+  }
+  const Column col = column_of(req, G, TILE, tile);
+  if (col.rows == 0) return;
+  const int to = col.keys(G), first_last = col.last(0, G);             // all rows see the keys up to first_last
+
+  // this wave's score rows
+  const int r = wave * WAVE_ROWS + n;
+  const bool on = r < col.rows;
+  const int last = on ? col.last(r, G) : 0x7fffffff;
+  const int wave_first = col.last(wave * WAVE_ROWS, G);                // (of rows that are not there: more than all keys)
+  const int wave_to = wave * WAVE_ROWS < col.rows ? min(to, col.last(min(wave * WAVE_ROWS + WAVE_ROWS, col.rows) - 1, G) + 1) : 0;
+  const int row = col.row0 + (on ? r : 0);
+  u32x4 q[KS];
+  {
+    const uint16_t* src = static_cast<const uint16_t*>(a.q.x) + (int64_t)(col.token0 + row / G) * a.q.token + (int64_t)(head * G + row % G) * a.q.head;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int at = (2 * i + h) * 8;
+      q[i] = on && at < c.d ? *reinterpret_cast<const u32x4*>(src + at) : u32x4{};
+    }
+  }
+  f32x16 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) o[i] = f32x16{};
+  float m = MINUS_INF, above = MINUS_INF, less = 0.f, z = 0.f;
+  const float margin = 8.f / a.scale2;
+  bool odd = false;                                                    // an infinity or a NaN in V that not every row of the column sees
+
+  // stages: this thread's pieces of 64 rows
+  const int piece = threadIdx.x % PIECES, my_row = threadIdx.x / PIECES, wave_row = wave * (64 / PIECES);
+  const int row_bytes = (int)(c.row * sizeof(E));
+  const int my_at = (my_row & 15) * row_bytes + piece * (8 * (int)sizeof(E));
+  const bool live = piece * 8 < c.d;
+  const E *kx = static_cast<const E*>(c.k.x) + head * c.head, *vx = static_cast<const E*>(c.v.x) + head * c.head;
+  typedef __attribute__((address_space(4))) const int32_t* ConstTable;
+  const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)request * a.blocks_per_inst);
+  Raw<E, 8> k[PASSES], v[PASSES];
+  uint32_t ks[PASSES], vs[PASSES];
+  int page = 0, off = 0, blocks[STAGE / 16];                           // of the stage that is read next
+  uint32_t there_next = 0, there = 0;                                  // a bit for each tile of 16 rows: of the stage on its way; of the one in use
+  const auto ask = [&](int left) {
+    int pg = page, of = off;
+#pragma unroll
+    for (int i = 0; i < STAGE / 16; ++i) {
+      blocks[i] = 16 * i < left ? table[pg] : -1;
+      of += 16;
+      if (of >= c.block_rows) {
+        of = 0;
+        ++pg;
+      }
+    }
+  };
+  const auto load = [&](int left) {
+    int64_t base[STAGE / 16], scales[STAGE / 16];
+    uint32_t bytes[STAGE / 16];
+    there_next = 0;
+#pragma unroll
+    for (int i = 0; i < STAGE / 16; ++i) {
+      const bool is = blocks[i] >= 0 && blocks[i] < c.n_blocks;
+      there_next |= (uint32_t)is << i;
+      base[i] = is ? blocks[i] * c.block + (int64_t)off * c.row : 0;
+      scales[i] = is ? ((int64_t)blocks[i] * H + head) * c.block_rows + off : 0;
+      bytes[i] = is ? (uint32_t)(min(16, left - 16 * i) - 1) * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E)) : 0u;
+      off += 16;
+      if (off >= c.block_rows) {
+        off = 0;
+        ++page;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u) {
+      int t = 0;                                                       // the tile of this wave's rows
+      if constexpr (ROWS == 16) t = u;
+      else t = u * (ROWS / 16) + wave_row / 16;
+      int64_t b = base[0], sc = scales[0];
+      uint32_t by = bytes[0];
+#pragma unroll
+      for (int i = 1; i < STAGE / 16; ++i) {
+        b = t == i ? base[i] : b;
+        sc = t == i ? scales[i] : sc;
+        by = t == i ? bytes[i] : by;
+      }
+      fetch<false>(k[u], tile_of(kx + b, by), my_at);
+      fetch<false>(v[u], tile_of(vx + b, by), my_at);
+      if constexpr (SCALED) {
+        ks[u] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.k.scales + sc, by ? 16u : 0u), my_row & 15, 0, 0);
+        vs[u] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.v.scales + sc, by ? 16u : 0u), my_row & 15, 0, 0);
+      }
+    }
+    ask(left - STAGE);
+  };
+  // the pieces to LDS; `key`, `left`: of the stage
+  const auto put = [&](int buf, int key, int left) {
+    const bool edge = left <= STAGE || key > first_last - STAGE;       // rows behind the end, or that not every row sees
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u) {
+      const int rr = u * ROWS + my_row;
+      if (edge) {
+        if (SCALED && rr >= left) ks[u] = vs[u] = 0;                   // (255 makes a NaN of the zeros)
+        if (rr > first_last - key) {
+          odd |= live && has_odd(v[u], SCALED ? vs[u] : 0u);
+          drop_odd(v[u]);
+          if (SCALED && vs[u] == 255u) {
+            clear(v[u]);
+            vs[u] = 0;
+          }
+        }
+      }
+      const u32x4 kk = pairs(k[u], SCALED ? e4m3_scale_value(ks[u]) : 1.f), vv = pairs(v[u], SCALED ? e4m3_scale_value(vs[u]) : 1.f);
+      *reinterpret_cast<u32x4*>(&k_lds[buf][k_place<D>(rr, piece)]) = live ? kk : u32x4{};
+      *reinterpret_cast<u32x4*>(&v_lds[buf][v_place<D>(rr, piece)]) = live ? vv : u32x4{};
+    }
+  };
+
+  const int v_row = 4 * h + (lane & 15) / 4, v_channel = (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+  const auto compute = [&](int buf, int key) {
+    f32x16 x[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      x[s] = f32x16{};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) x[s] = mfma(*reinterpret_cast<const u32x4*>(&k_lds[buf][k_place<D>(32 * s + n, 2 * i + h)]), q[i], x[s]);
+    }
+    if (key > wave_first - STAGE || there != 15u) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int at = 32 * s + 8 * (e / 4) + 4 * h + e % 4;
+          if (!(there >> (2 * s + e / 8) & 1u) || at >= to - key || at > last - key) x[s][e] = MINUS_INF;
+        }
+    }
+    bool far = false;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) far |= x[s][e] > above;
+    if (__any(far)) {
+      float most = m;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) most = fmaxf(most, x[s][e]);
+      most = fmaxf(most, __shfl_xor(most, 32));
+      if (most > m) {
+        const float by = m == MINUS_INF ? 0.f : __builtin_amdgcn_exp2f((m - most) * a.scale2);
+        m = most;
+        above = most + margin;
+        less = most * a.scale2;
+        z *= by;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] *= by;
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[s][e], a.scale2, -less));
+        sum += x[s][e];
+      }
+      z += sum;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {                                    // 16 keys
+        const u32x4 w{pack2(x[s][8 * t], x[s][8 * t + 1]), pack2(x[s][8 * t + 2], x[s][8 * t + 3]), pack2(x[s][8 * t + 4], x[s][8 * t + 5]),
+                      pack2(x[s][8 * t + 6], x[s][8 * t + 7])};
+        const int row0 = 32 * s + 16 * t + v_row;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          const int ch = 32 * i + v_channel;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)&v_lds[buf][v_place<D>(row0, ch / 8) + (ch & 4)]);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)&v_lds[buf][v_place<D>(row0 + 8, ch / 8) + (ch & 4)]);
+          const uint2 l = __builtin_bit_cast(uint2, lo), u = __builtin_bit_cast(uint2, hi);
+          o[i] = mfma(u32x4{l.x, l.y, u.x, u.y}, w, o[i]);
+        }
+      }
+    }
+  };
+
+  if (to > 0) {
+    ask(to);
+    load(to);
+    put(0, 0, to);
+    there = there_next;
+    load(to - STAGE);                                                  // (behind the end nothing is read)
+    __syncthreads();
+    int key = 0, buf = 0;
+    for (;;) {
+      if (key < wave_to) compute(buf, key);
+      if (to - key <= STAGE) break;
+      key += STAGE;
+      buf ^= 1;
+      put(buf, key, to - key);
+      there = there_next;
+      load(to - key - STAGE);
+      __syncthreads();
+    }
+  }
+
+  z += __shfl_xor(z, 32);
+  // (whether any wave met one)
+  if (__syncthreads_or(odd) && on) {
+    const int upto = min(to - 1, last);
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int at = 32 * i + 8 * b + 4 * h;
+        if (at >= c.d) continue;
+        for (int key = max(0, first_last + 1); key <= upto; ++key) {
+          const int pg = (int)((uint32_t)key / (uint32_t)c.block_rows), of = key - pg * c.block_rows, block = table[pg];
+          if (block < 0 || block >= c.n_blocks) continue;
+          const E* src = vx + block * c.block + (int64_t)of * c.row;
+          const uint32_t sc = SCALED ? c.v.scales[((int64_t)block * H + head) * c.block_rows + of] : 0u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float f = number(src, at + e, sc);
+            if (f - f != 0.f) o[i][4 * b + e] += f;
+          }
+        }
+      }
+  }
+  if (!on) return;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int at = 32 * i + 8 * b + 4 * h;
+      if (at < c.d) put_out<uint16_t>(c, a, col, head, G, r, at, m, z, f32x4{o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]});
+    }
+}
+
+// Columns of a KV head, at most.
+int64_t columns_of(int G, int n, int64_t n_tokens) { return n_tokens * G / TILE + n; }
+
+}  // namespace
+
+#ifndef PROMPT_ROWS
+#define PROMPT_ROWS 65
+#endif
+#ifndef PROMPT_COLS
+#define PROMPT_COLS 128
+#endif
+bool paged_prompt_call(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens) {
+  const int G = Hq / c.Hkv;
+  const int64_t columns = columns_of(G, n, n_tokens) * c.Hkv;
+  return dtype == LAQ_BF16 && c.d <= 128 && (n_tokens + n - 1) / n * G >= PROMPT_ROWS && columns >= PROMPT_COLS && columns < (1 << 24);
+}
+
+hipError_t launch_paged_prompt(const PagedView& c, const PagedAttention& a, hipStream_t st) {
+  const dim3 grid((unsigned)(columns_of(a.Hq / c.Hkv, a.n, a.n_tokens) * c.Hkv));
+  if (c.type == LAQ_BF16) {
+    if (c.d <= 64) hipLaunchKernelGGL((paged_prompt_kernel<uint16_t, 64>), grid, dim3(THREADS), 0, st, c, a);
+    else hipLaunchKernelGGL((paged_prompt_kernel<uint16_t, 128>), grid, dim3(THREADS), 0, st, c, a);
+  } else {
+    if (c.d <= 64) hipLaunchKernelGGL((paged_prompt_kernel<E4m3, 64>), grid, dim3(THREADS), 0, st, c, a);
+    else hipLaunchKernelGGL((paged_prompt_kernel<E4m3, 128>), grid, dim3(THREADS), 0, st, c, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace laq
