@@ -11,6 +11,9 @@ namespace laq {
 
 namespace {
 
+#ifndef KO
+#define KO 0x406
+#endif
 constexpr int WAVES = 4, THREADS = 64 * WAVES, WAVE_ROWS = 32, TILE = WAVES * WAVE_ROWS, STAGE = 64;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -19,6 +22,9 @@ typedef __attribute__((address_space(3))) s16x4* LdsQuad;
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 acc) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
 }
+
+// LDS and memory operations and products stay on their side; other instructions may pass.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(KO); }
 
 // Where piece `piece` (eight numbers) of row `row` lies in LDS, in numbers.
 template <int D> __device__ __forceinline__ int k_place(int row, int piece) { return row * D + (piece ^ (row & (D / 8 - 1))) * 8; }
@@ -127,10 +133,11 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
     there_next = 0;
 #pragma unroll
     for (int i = 0; i < STAGE / 16; ++i) {
-      const bool is = blocks[i] >= 0 && blocks[i] < c.n_blocks;
+      const bool is = (uint32_t)blocks[i] < (uint32_t)c.n_blocks;      // (-1 is not)
+      const int block = is ? blocks[i] : 0;
       there_next |= (uint32_t)is << i;
-      base[i] = is ? blocks[i] * c.block + (int64_t)off * c.row : 0;
-      scales[i] = is ? ((int64_t)blocks[i] * H + head) * c.block_rows + off : 0;
+      base[i] = block * c.block + (int64_t)off * c.row;
+      if constexpr (SCALED) scales[i] = ((int64_t)block * H + head) * c.block_rows + off;
       bytes[i] = is ? (uint32_t)(min(16, left - 16 * i) - 1) * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E)) : 0u;
       off += 16;
       if (off >= c.block_rows) {
@@ -185,13 +192,36 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
 
   const int v_row = 4 * h + (lane & 15) / 4, v_channel = (lane >> 4 & 1) * 16 + (lane & 3) * 4;
   const auto compute = [&](int buf, int key) {
-    f32x16 x[2];
+    // LDS reads are asked for a group of products ahead, and kept there: left to itself the compiler puts each in front of its product and waits for it
+    constexpr int GROUP = 4, K_GROUPS = 2 * KS / GROUP, PER = KS / GROUP;
+    f32x16 x[2] = {};
+    u32x4 kf[2][GROUP];
+    const auto read_k = [&](int gr, u32x4* f) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      x[s] = f32x16{};
+      for (int j = 0; j < GROUP; ++j) f[j] = *reinterpret_cast<const u32x4*>(&k_lds[buf][k_place<D>(32 * (gr / PER) + n, 2 * (gr % PER * GROUP + j) + h)]);
+    };
+    read_k(0, kf[0]);
 #pragma unroll
-      for (int i = 0; i < KS; ++i) x[s] = mfma(*reinterpret_cast<const u32x4*>(&k_lds[buf][k_place<D>(32 * s + n, 2 * i + h)]), q[i], x[s]);
+    for (int gr = 0; gr < K_GROUPS; ++gr) {
+      if (gr + 1 < K_GROUPS) read_k(gr + 1, kf[(gr + 1) & 1]);
+      keep_order();
+#pragma unroll
+      for (int j = 0; j < GROUP; ++j) x[gr / PER] = mfma(kf[gr & 1][j], q[gr % PER * GROUP + j], x[gr / PER]);
+      keep_order();
     }
+    u32x4 vf[2][DT];
+    const auto read_v = [&](int gr, u32x4* f) {                        // 16 keys
+      const int row0 = 16 * gr + v_row;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        const int ch = 32 * i + v_channel;
+        const uint2 l = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)&v_lds[buf][v_place<D>(row0, ch / 8) + (ch & 4)]));
+        const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)&v_lds[buf][v_place<D>(row0 + 8, ch / 8) + (ch & 4)]));
+        f[i] = u32x4{l.x, l.y, u.x, u.y};
+      }
+    };
+    read_v(0, vf[0]);
+    keep_order();
     if (key > wave_first - STAGE || there != 15u) {
 #pragma unroll
       for (int s = 0; s < 2; ++s)
@@ -224,28 +254,19 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
       }
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      float sum = 0.f;
+    for (int gr = 0; gr < 4; ++gr) {                                   // 16 keys
+      const int s = gr / 2, e0 = gr % 2 * 8;
+      if (gr < 3) read_v(gr + 1, vf[(gr + 1) & 1]);
+      keep_order();
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
+      for (int e = e0; e < e0 + 8; ++e) {
         x[s][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[s][e], a.scale2, -less));
-        sum += x[s][e];
+        z += x[s][e];
       }
-      z += sum;
+      const u32x4 w{pack2(x[s][e0], x[s][e0 + 1]), pack2(x[s][e0 + 2], x[s][e0 + 3]), pack2(x[s][e0 + 4], x[s][e0 + 5]), pack2(x[s][e0 + 6], x[s][e0 + 7])};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {                                    // 16 keys
-        const u32x4 w{pack2(x[s][8 * t], x[s][8 * t + 1]), pack2(x[s][8 * t + 2], x[s][8 * t + 3]), pack2(x[s][8 * t + 4], x[s][8 * t + 5]),
-                      pack2(x[s][8 * t + 6], x[s][8 * t + 7])};
-        const int row0 = 32 * s + 16 * t + v_row;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          const int ch = 32 * i + v_channel;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)&v_lds[buf][v_place<D>(row0, ch / 8) + (ch & 4)]);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)&v_lds[buf][v_place<D>(row0 + 8, ch / 8) + (ch & 4)]);
-          const uint2 l = __builtin_bit_cast(uint2, lo), u = __builtin_bit_cast(uint2, hi);
-          o[i] = mfma(u32x4{l.x, l.y, u.x, u.y}, w, o[i]);
-        }
-      }
+      for (int i = 0; i < DT; ++i) o[i] = mfma(vf[gr & 1][i], w, o[i]);
+      keep_order();
     }
   };
 
