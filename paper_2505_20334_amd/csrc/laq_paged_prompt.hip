@@ -106,8 +106,8 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
   // stages: this thread's pieces of 64 rows
   const int piece = threadIdx.x % PIECES, my_row = threadIdx.x / PIECES, wave_row = wave * (64 / PIECES);
   const int row_bytes = (int)(c.row * sizeof(E));
-  const int my_at = (my_row & 15) * row_bytes + piece * (8 * (int)sizeof(E));
-  const bool live = piece * 8 < c.d;
+  // (channels beyond d: nothing is read, zeros)
+  const int my_at = piece * 8 < c.d ? (my_row & 15) * row_bytes + piece * (8 * (int)sizeof(E)) : 0x7fffffff - 16;
   const E *kx = static_cast<const E*>(c.k.x) + head * c.head, *vx = static_cast<const E*>(c.v.x) + head * c.head;
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
   const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)request * a.blocks_per_inst);
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
       if (edge) {
         if (SCALED && rr >= left) ks[u] = vs[u] = 0;                   // (255 makes a NaN of the zeros)
         if (rr > first_last - key) {
-          odd |= live && has_odd(v[u], SCALED ? vs[u] : 0u);
+          odd |= has_odd(v[u], SCALED ? vs[u] : 0u);
           drop_odd(v[u]);
           if (SCALED && vs[u] == 255u) {
             clear(v[u]);
@@ -185,8 +185,8 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
         }
       }
       const u32x4 kk = pairs(k[u], SCALED ? e4m3_scale_value(ks[u]) : 1.f), vv = pairs(v[u], SCALED ? e4m3_scale_value(vs[u]) : 1.f);
-      *reinterpret_cast<u32x4*>(&k_lds[buf][k_place<D>(rr, piece)]) = live ? kk : u32x4{};
-      *reinterpret_cast<u32x4*>(&v_lds[buf][v_place<D>(rr, piece)]) = live ? vv : u32x4{};
+      *reinterpret_cast<u32x4*>(&k_lds[buf][k_place<D>(rr, piece)]) = kk;
+      *reinterpret_cast<u32x4*>(&v_lds[buf][v_place<D>(rr, piece)]) = vv;
     }
   };
 
@@ -231,17 +231,13 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
           if (!(there >> (2 * s + e / 8) & 1u) || at >= to - key || at > last - key) x[s][e] = MINUS_INF;
         }
     }
-    bool far = false;
+    float most = x[0][0];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) far |= x[s][e] > above;
-    if (__any(far)) {
-      float most = m;
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) most = fmaxf(most, x[s][e]);
+      for (int e = 0; e < 16; ++e) most = fmaxf(most, x[s][e]);
+    if (__any(most > above)) {
+      most = fmaxf(most, m);
       most = fmaxf(most, __shfl_xor(most, 32));
       if (most > m) {
         const float by = m == MINUS_INF ? 0.f : __builtin_amdgcn_exp2f((m - most) * a.scale2);
