@@ -22,8 +22,20 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct Eight { float f[8]; };
 
-__device__ __forceinline__ Eight read8(const uint16_t* p) {
-  const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+// Rows that are read once, past the caches where a call has more of them than the caches hold (MANY_BYTES): 16381 tokens x 40 heads of d = 128 rotated 81 -> 73 us,
+// appended and loaded 108 -> 90; in smaller calls, whose rows the caches still have from whoever made them, it costs (2048 tokens 17 -> 24 us).  So are the rows that
+// laq_cache_load writes (32 layers compacted and loaded 99 -> 87 us), but not what is written to a cache, which is read soon.
+constexpr int64_t MANY_BYTES = 128ll << 20;
+template <bool PAST> __device__ __forceinline__ u32x4 get16(const void* p) {
+  return PAST ? __builtin_nontemporal_load(static_cast<const u32x4*>(p)) : *static_cast<const u32x4*>(p);
+}
+template <bool PAST> __device__ __forceinline__ void put16(void* p, u32x4 x) {
+  if constexpr (PAST) __builtin_nontemporal_store(x, static_cast<u32x4*>(p));
+  else *static_cast<u32x4*>(p) = x;
+}
+
+template <bool PAST> __device__ __forceinline__ Eight read8(const uint16_t* p) {
+  const u32x4 x = get16<PAST>(p);
   Eight r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -32,8 +44,8 @@ __device__ __forceinline__ Eight read8(const uint16_t* p) {
   }
   return r;
 }
-__device__ __forceinline__ Eight read8(const float* p) {
-  const u32x4 a = *reinterpret_cast<const u32x4*>(p), b = *reinterpret_cast<const u32x4*>(p + 4);
+template <bool PAST> __device__ __forceinline__ Eight read8(const float* p) {
+  const u32x4 a = get16<PAST>(p), b = get16<PAST>(p + 4);
   Eight r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -45,21 +57,21 @@ __device__ __forceinline__ Eight read8(const float* p) {
 __device__ __forceinline__ float read1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 __device__ __forceinline__ float read1(const float* p) { return *p; }
 
-__device__ __forceinline__ void write8(uint16_t* p, const Eight& v) {
+template <bool PAST = false> __device__ __forceinline__ void write8(uint16_t* p, const Eight& v) {
   u32x4 x;
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v.f[2 * i], v.f[2 * i + 1]}), bf16x2));
-  *reinterpret_cast<u32x4*>(p) = x;
+  put16<PAST>(p, x);
 }
-__device__ __forceinline__ void write8(float* p, const Eight& v) {
+template <bool PAST = false> __device__ __forceinline__ void write8(float* p, const Eight& v) {
   u32x4 a, b;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     a[i] = __float_as_uint(v.f[i]);
     b[i] = __float_as_uint(v.f[4 + i]);
   }
-  *reinterpret_cast<u32x4*>(p) = a;
-  *reinterpret_cast<u32x4*>(p + 4) = b;
+  put16<PAST>(p, a);
+  put16<PAST>(p + 4, b);
 }
 
 // Eight numbers of the cache.
@@ -142,17 +154,36 @@ __device__ __forceinline__ float turned(float x, float c, float other, float s) 
   return a + b;
 }
 
-// T: the tokens' rows; C: the cache's numbers (T itself, where k goes to k_out).  LANES: of a row.  ROPE: 0 none; 1 the two numbers of a pair lie in
-// the same lane, or in the same place of another lane's; 2 anywhere.
-template <typename T, typename C, int LANES, int ROPE, bool CACHE>
+// How a rotation finds the other number of a pair.
+enum { ROPE_NONE, ROPE_PIECES, ROPE_ANY, ROPE_NEIGHBOURS };      // in the same place of another lane's piece; anywhere; in the same piece
+
+// T: the tokens' rows; C: the cache's numbers (T itself, where k goes to k_out).  LANES: of a row.  A workgroup has rows_each rows of each of tokens_each tokens,
+// ROWS at a time, the reads of U times as many under way together.
+template <typename T, typename C, int LANES, int ROPE, bool CACHE, bool PAST>
 __global__ __launch_bounds__(ROWS_THREADS) void token_rows_kernel(TokenCall t, PagedView c, int tokens_each, int rows_each) {
   constexpr int ROWS = ROWS_THREADS / LANES;                         // rows that a workgroup has at once
-  __shared__ float2 turn[ROPE ? 4 * 128 : 1];                        // [tokens_each][rot / 2]: cos, sin
+  constexpr int U = 2;
+  __shared__ alignas(16) float2 turn[ROPE ? 4 * 128 : 1];            // [tokens_each][rot / 2]: cos, sin
   const int col = threadIdx.x % LANES, lane_row = threadIdx.x / LANES;
   const int64_t t0 = (int64_t)blockIdx.x * tokens_each;
   const int tokens = (int)min((int64_t)tokens_each, t.n_tokens - t0);
   const int pairs = t.rope.rot / 2;
-  if constexpr (ROPE != 0) {
+  const bool on = col * 8 < t.d;
+  const int first = blockIdx.y * rows_each, q_rows = t.q.heads, qk_rows = q_rows + t.k.heads, all = qk_rows + t.v.heads;
+  const int here = min(rows_each, all - first), times = (here + ROWS - 1) / ROWS;      // of a token
+  // this lane's row number i of the workgroup (false: none)
+  struct Row { int tok, head, kind; const T* src; };                 // kind 0 q, 1 k, 2 v
+  const auto row_of = [&](int i, Row& r) {
+    r.tok = i / times;
+    const int at = first + (i - r.tok * times) * ROWS + lane_row;
+    if (at >= first + here) return false;
+    r.kind = at < q_rows ? 0 : at < qk_rows ? 1 : 2;
+    r.head = at - (r.kind == 0 ? 0 : r.kind == 1 ? q_rows : qk_rows);
+    const TokenHeads& from = r.kind == 0 ? t.q : r.kind == 1 ? t.k : t.v;
+    r.src = static_cast<const T*>(from.x) + (t0 + r.tok) * from.token + r.head * from.head;
+    return true;
+  };
+  if constexpr (ROPE != ROPE_NONE) {
     for (int i = threadIdx.x; i < tokens * pairs; i += ROWS_THREADS) {
       const int tok = i / pairs, j = i - tok * pairs;
       double s, co;
@@ -161,67 +192,79 @@ __global__ __launch_bounds__(ROWS_THREADS) void token_rows_kernel(TokenCall t, P
     }
     __syncthreads();
   }
-  const bool on = col * 8 < t.d;
-  const int first = blockIdx.y * rows_each, q_rows = t.q.heads, qk_rows = q_rows + t.k.heads, all = qk_rows + t.v.heads;
-  const int end = min(first + rows_each, all);
-  for (int tok = 0; tok < tokens; ++tok) {
-    // what turns this lane's numbers: x * co + other * si
-    float co[8], si[8];
-    int other_col = 0;
-    if constexpr (ROPE != 0) {
+  // (a group's lanes are together in all that follows: a row is read before any of it is written)
+  for (int i0 = 0; i0 < tokens * times; i0 += U) {
+    Row row[U];
+    Eight v[U];
+    bool is[U];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int at = col * 8 + e;
-        const bool in = at < t.rope.rot, upper = t.rope.interleaved ? at & 1 : at >= pairs;
-        const int j = t.rope.interleaved ? at >> 1 : upper ? at - pairs : at;
-        const float2 w = in ? turn[tok * pairs + j] : float2{1.f, 0.f};
-        co[e] = w.x;
-        si[e] = upper ? w.y : -w.y;
-      }
-      other_col = t.rope.interleaved ? col : col * 8 < pairs ? col + pairs / 8 : col - pairs / 8;
+    for (int u = 0; u < U; ++u) {
+      is[u] = i0 + u < tokens * times && row_of(i0 + u, row[u]);
+      v[u] = Eight{};
+      if (is[u] && on) v[u] = read8<PAST>(row[u].src + col * 8);
     }
-    int block = 0, row = 0;
-    const bool kept = CACHE && paged_slot(c, t.slots[t0 + tok], &block, &row);
-    for (int r0 = first; r0 < end; r0 += ROWS) {
-      const int r = r0 + lane_row;
-      if (r >= end) continue;                                        // (a group's lanes together)
-      const bool is_q = r < q_rows, is_k = !is_q && r < qk_rows;
-      const int head = is_q ? r : is_k ? r - q_rows : r - qk_rows;
-      const TokenHeads& from = is_q ? t.q : is_k ? t.k : t.v;
-      const T* src = static_cast<const T*>(from.x) + (t0 + tok) * from.token + head * from.head;
-      Eight v{};
-      if (on) v = read8(src + col * 8);
-      if (ROPE != 0 && (is_q || is_k)) {
-        Eight o = v;
-        if (t.rope.interleaved) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o.f[e] = v.f[e ^ 1];
-        } else if (ROPE == 1) {
+    for (int u = 0; u < U; ++u) {
+      if (!is[u]) continue;
+      const Row& r = row[u];
+      if (ROPE != ROPE_NONE && r.kind < 2) {
+        const float2* const by = turn + r.tok * pairs;
+        if constexpr (ROPE == ROPE_PIECES) {
+          const bool upper = col * 8 >= pairs, in = col * 8 < t.rope.rot;
+          const int other = upper ? col - pairs / 8 : col + pairs / 8, j0 = upper ? col * 8 - pairs : col * 8;
+          Eight o;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o.f[e] = __shfl(v.f[e], other_col, LANES);
+          for (int e = 0; e < 8; ++e) o.f[e] = __shfl(v[u].f[e], other, LANES);
+          if (in) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+              const float4 w = *reinterpret_cast<const float4*>(by + j0 + e);      // (pairs is a multiple of 8)
+              v[u].f[e] = turned(v[u].f[e], w.x, o.f[e], upper ? w.y : -w.y);
+              v[u].f[e + 1] = turned(v[u].f[e + 1], w.z, o.f[e + 1], upper ? w.w : -w.w);
+            }
+          }
+        } else if constexpr (ROPE == ROPE_NEIGHBOURS) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const int j = col * 4 + e / 2;
+            if (j < pairs) {
+              const float2 w = by[j];
+              const float a = v[u].f[e], b = v[u].f[e + 1];
+              v[u].f[e] = turned(a, w.x, b, -w.y);
+              v[u].f[e + 1] = turned(b, w.x, a, w.y);
+            }
+          }
         } else {
+          Eight o{};
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const int at = col * 8 + e;
-            if (at < t.rope.rot) o.f[e] = read1(src + (at < pairs ? at + pairs : at - pairs));
+            if (at < t.rope.rot) o.f[e] = read1(r.src + (at < pairs ? at + pairs : at - pairs));
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int at = col * 8 + e;
+            if (at < t.rope.rot) {
+              const float2 w = by[at < pairs ? at : at - pairs];
+              v[u].f[e] = turned(v[u].f[e], w.x, o.f[e], at < pairs ? -w.y : w.y);
+            }
           }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (col * 8 + e < t.rope.rot) v.f[e] = turned(v.f[e], co[e], o.f[e], si[e]);
       }
-      if (is_q || !CACHE) {
-        const TokenHeads& to = is_q ? t.q_out : t.k_out;
-        if (on) write8(static_cast<T*>(to.x) + (t0 + tok) * to.token + head * to.head + col * 8, v);
-      } else if (kept) {
-        put<C, LANES>(is_k ? c.k : c.v, v, row_at(c, block, head, row), scale_at(c, block, head, row), col, on);
+      if (r.kind == 0 || !CACHE) {
+        const TokenHeads& to = r.kind == 0 ? t.q_out : t.k_out;
+        if (on) write8(static_cast<T*>(to.x) + (t0 + r.tok) * to.token + r.head * to.head + col * 8, v[u]);
+      } else {
+        int block, at;
+        if (paged_slot(c, t.slots[t0 + r.tok], &block, &at))
+          put<C, LANES>(r.kind == 1 ? c.k : c.v, v[u], row_at(c, block, r.head, at), scale_at(c, block, r.head, at), col, on);
       }
     }
   }
 }
 
 // A workgroup has rows of one head of an instance; the list has an entry for each, the slots one for all heads.
-template <typename T, typename C, int LANES>
+template <typename T, typename C, int LANES, bool PAST>
 __global__ __launch_bounds__(ROWS_THREADS) void paged_compact_kernel(PagedView c, int L, KvLayout lay, InstTable tab, int inst0, const T* __restrict__ k,
                                                                      const T* __restrict__ v, const int32_t* __restrict__ idx,
                                                                      const int32_t* __restrict__ slots) {
@@ -238,14 +281,14 @@ __global__ __launch_bounds__(ROWS_THREADS) void paged_compact_kernel(PagedView c
   if (lay.table) from += paged_block_offset(lay, inst0 + li, j, &at);
   from += (int64_t)at * lay.row;
   Eight kv{}, vv{};
-  if (on) kv = read8(k + from);
-  if (on && v) vv = read8(v + from);
+  if (on) kv = read8<PAST>(k + from);
+  if (on && v) vv = read8<PAST>(v + from);
   const int64_t to = row_at(c, block, head, row), scale_to = scale_at(c, block, head, row);
   put<C, LANES>(c.k, kv, to, scale_to, col, on);
   if (v) put<C, LANES>(c.v, vv, to, scale_to, col, on);
 }
 
-template <typename T, typename C, int LANES>
+template <typename T, typename C, int LANES, bool PAST>
 __global__ __launch_bounds__(ROWS_THREADS) void paged_load_kernel(PagedView c, int64_t n_rows, const int32_t* __restrict__ slots, T* __restrict__ k,
                                                                   T* __restrict__ v) {
   constexpr int ROWS = ROWS_THREADS / LANES;
@@ -261,9 +304,9 @@ __global__ __launch_bounds__(ROWS_THREADS) void paged_load_kernel(PagedView c, i
     Eight x{};
     if (there) {
       if constexpr (scaled<C>()) x = read8(static_cast<const E4m3*>(plane.x) + at, e4m3_scale_value(plane.scales[scale]));
-      else x = read8(static_cast<const C*>(plane.x) + at);
+      else x = read8<PAST>(static_cast<const C*>(plane.x) + at);
     }
-    write8(out + r * c.d + col * 8, x);
+    write8<PAST>(out + r * c.d + col * 8, x);
   };
   if (k) one(c.k, k);
   if (v) one(c.v, v);
@@ -290,21 +333,28 @@ hipError_t by_types(int dtype, int type, const F& f) {
 }
 template <typename P> using Of = std::remove_pointer_t<P>;
 
-// How a call's rotation finds the other number of a pair.
-int rope_kind(const RopeArgs& r) { return !r.inv_freq ? 0 : r.interleaved || r.rot % 16 == 0 ? 1 : 2; }
+int rope_kind(const RopeArgs& r) { return !r.inv_freq ? ROPE_NONE : r.interleaved ? ROPE_NEIGHBOURS : r.rot % 16 == 0 ? ROPE_PIECES : ROPE_ANY; }
 
 template <typename T, typename C, int LANES, bool CACHE>
 hipError_t token_rows(const TokenCall& t, const PagedView& c, hipStream_t st) {
   constexpr int ROWS = ROWS_THREADS / LANES;
   const int all = t.q.heads + t.k.heads + t.v.heads;
-  // few tokens: a row a group, so that the call is as short as it can be; many: four tokens to a workgroup, all their heads
-  const bool few = t.n_tokens <= 256;
-  const int tokens_each = few ? 1 : 4, rows_each = few ? ROWS : (all + ROWS - 1) / ROWS * ROWS;
+  // Few tokens: a row a group, so that the call is as short as it can be; more: all heads of a token to a workgroup, of two, of four, whose sines and cosines
+  // and first reads are then made together.  us, 40 heads of d = 128: 512 tokens 5.1, as later ones 5.9; 2048 12.4 : 10.9 : 12.5; 4096 20.2 : 17.9 : 16.8 : 20.3;
+  // 16381 73.2 : 74.3 : 73.6 : 72.8
+  const bool few = t.n_tokens <= 512;
+  const int tokens_each = t.n_tokens <= 2048 ? 1 : t.n_tokens <= 8192 ? 2 : 4, rows_each = few ? ROWS : (all + ROWS - 1) / ROWS * ROWS;
   const dim3 grid((unsigned)((t.n_tokens + tokens_each - 1) / tokens_each), (unsigned)((all + rows_each - 1) / rows_each));
+  const bool past = t.n_tokens * all * t.d * (int64_t)sizeof(T) >= MANY_BYTES;
+  const auto start = [&](auto rope) {
+    if (past) hipLaunchKernelGGL((token_rows_kernel<T, C, LANES, rope(), CACHE, true>), grid, dim3(ROWS_THREADS), 0, st, t, c, tokens_each, rows_each);
+    else hipLaunchKernelGGL((token_rows_kernel<T, C, LANES, rope(), CACHE, false>), grid, dim3(ROWS_THREADS), 0, st, t, c, tokens_each, rows_each);
+  };
   switch (rope_kind(t.rope)) {
-    case 0: hipLaunchKernelGGL((token_rows_kernel<T, C, LANES, 0, CACHE>), grid, dim3(ROWS_THREADS), 0, st, t, c, tokens_each, rows_each); break;
-    case 1: hipLaunchKernelGGL((token_rows_kernel<T, C, LANES, 1, CACHE>), grid, dim3(ROWS_THREADS), 0, st, t, c, tokens_each, rows_each); break;
-    default: hipLaunchKernelGGL((token_rows_kernel<T, C, LANES, 2, CACHE>), grid, dim3(ROWS_THREADS), 0, st, t, c, tokens_each, rows_each); break;
+    case ROPE_NONE: start(std::integral_constant<int, ROPE_NONE>{}); break;
+    case ROPE_PIECES: start(std::integral_constant<int, ROPE_PIECES>{}); break;
+    case ROPE_NEIGHBOURS: start(std::integral_constant<int, ROPE_NEIGHBOURS>{}); break;
+    default: start(std::integral_constant<int, ROPE_ANY>{});
   }
   return hipGetLastError();
 }
@@ -326,8 +376,14 @@ hipError_t launch_paged_compact(const PagedView& c, int dtype, int n, int inst0,
     return by_types(dtype, c.type, [&](auto rows, auto numbers) {
       using T = Of<decltype(rows)>;
       constexpr int ROWS = ROWS_THREADS / lanes();
-      hipLaunchKernelGGL((paged_compact_kernel<T, Of<decltype(numbers)>, lanes()>), dim3((most + ROWS - 1) / ROWS, c.Hkv, n), dim3(ROWS_THREADS), 0, st, c, L,
-                         lay, tab, inst0, static_cast<const T*>(k), static_cast<const T*>(v), idx, slots);
+      const auto start = [&](auto past) {
+        hipLaunchKernelGGL((paged_compact_kernel<T, Of<decltype(numbers)>, lanes(), past()>), dim3((most + ROWS - 1) / ROWS, c.Hkv, n), dim3(ROWS_THREADS), 0, st, c,
+                           L, lay, tab, inst0, static_cast<const T*>(k), static_cast<const T*>(v), idx, slots);
+      };
+      int64_t rows_kept = 0;
+      for (int i = 0; i < n; ++i) rows_kept += tab.bk[i];
+      if (2 * rows_kept * c.Hkv * c.d * (int64_t)sizeof(T) >= MANY_BYTES) start(std::true_type{});
+      else start(std::false_type{});
       return hipGetLastError();
     });
   });
@@ -339,8 +395,12 @@ hipError_t launch_paged_load(const PagedView& c, int dtype, int64_t n_tokens, co
     return by_types(dtype, c.type, [&](auto rows, auto numbers) {
       using T = Of<decltype(rows)>;
       constexpr int ROWS = ROWS_THREADS / lanes();
-      hipLaunchKernelGGL((paged_load_kernel<T, Of<decltype(numbers)>, lanes()>), dim3((unsigned)((n_rows + ROWS - 1) / ROWS)), dim3(ROWS_THREADS), 0, st, c,
-                         n_rows, slots, static_cast<T*>(k), static_cast<T*>(v));
+      const auto start = [&](auto past) {
+        hipLaunchKernelGGL((paged_load_kernel<T, Of<decltype(numbers)>, lanes(), past()>), dim3((unsigned)((n_rows + ROWS - 1) / ROWS)), dim3(ROWS_THREADS), 0, st, c,
+                           n_rows, slots, static_cast<T*>(k), static_cast<T*>(v));
+      };
+      if (2 * n_rows * c.d * (int64_t)sizeof(T) >= MANY_BYTES / 4) start(std::true_type{});
+      else start(std::false_type{});
       return hipGetLastError();
     });
   });
