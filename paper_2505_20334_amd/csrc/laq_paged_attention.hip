@@ -27,10 +27,27 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 acc) {
 }
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0); }
 
+// Eight floats as sums of three bf16 each, each the nearest of what is left: nothing is (down to 2^-126).
+__device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4* parts) {
+  float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t both = pack2(x[2 * i], x[2 * i + 1]);
+      parts[p][i] = both;
+      x[2 * i] -= __uint_as_float(both << 16);
+      x[2 * i + 1] -= __uint_as_float(both & 0xffff0000u);
+    }
+}
+
 // Workgroups that a compute unit holds of a kernel: what their registers leave (the compiler is told to keep to it).
-constexpr int resident(bool f32, bool scaled, int d, int nt) {
-  if (d <= 64) return nt == 1 ? 3 : 2;
-  if (d <= 128) return nt == 1 || f32 || !scaled ? 2 : 1;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int resident(bool f32, int type, int d, int nt) {
+  const bool parts = f32 && type != LAQ_F32;
+  if (d <= 64) return nt == 1 && !parts ? 3 : 2;
+  if (d <= 128) return nt == 1 ? 2 : parts || type == LAQ_E4M3 ? 1 : 2;
   return 1;
 }
 
@@ -38,14 +55,18 @@ constexpr int resident(bool f32, bool scaled, int d, int nt) {
 template <typename Q, typename E, int D, int NT>
 struct Kinds {
   static constexpr bool F32 = std::is_same<Q, float>::value, SCALED = std::is_same<E, E4m3>::value;
-  static constexpr int KT = F32 ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
-  static constexpr int KN = F32 ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
+  // fp32: products of fp32 where the cache is, otherwise of bf16, in which the cache's numbers are exact, with queries and weights as sums of three
+  static constexpr bool FLOATS = std::is_same<E, float>::value;
+  static constexpr int PARTS = F32 && !FLOATS ? 3 : 1;
+  static constexpr bool LATER = PARTS > 1 && !SCALED;        // infinities of V are added at the end wherever they are
+  static constexpr int KT = FLOATS ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
+  static constexpr int KN = FLOATS ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
   // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on
   static constexpr int KW = 16 / (KN * (int)sizeof(E));
   static constexpr __host__ __device__ int k_channel(int i, int g) { return i / KW * (4 * KW * KN) + g * (KW * KN) + i % KW * KN; }
-  static constexpr int RESIDENT = resident(F32, SCALED, D, NT);      // workgroups of a compute unit (a wave of each on every SIMD)
+  static constexpr int RESIDENT = resident(F32, FLOATS ? LAQ_F32 : SCALED ? LAQ_E4M3 : LAQ_BF16, D, NT);      // workgroups of a compute unit (a wave of each on every SIMD)
   static constexpr bool ONCE = NT == 1;                      // one workgroup reads a row: past the caches
-  static constexpr int VN = std::is_same<E, float>::value || D == 64 ? 4 : 8, VP = D / (16 * VN);
+  static constexpr int VN = FLOATS || D == 64 ? 4 : 8, VP = D / (16 * VN);
   static constexpr int OT = D / 16;                          // output tiles
   static constexpr int PAD = D + 4;
 };
@@ -100,7 +121,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
 
   // the score rows of this lane's columns
   int last[NT];
-  u32x4 q[NT][K::KP];
+  u32x4 q[NT][K::KP][K::PARTS];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int r = 16 * t + n;
@@ -111,7 +132,13 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
 #pragma unroll
     for (int i = 0; i < K::KP; ++i) {
       const int at = K::k_channel(i, g);
-      q[t][i] = on && at < c.d ? *reinterpret_cast<const u32x4*>(src + at) : u32x4{};
+      const bool in = on && at < c.d;
+      if constexpr (K::PARTS == 1) {
+        q[t][i][0] = in ? *reinterpret_cast<const u32x4*>(src + at) : u32x4{};
+      } else {
+        const f32x4 a4 = in ? *reinterpret_cast<const f32x4*>(src + at) : f32x4{}, b4 = in ? *reinterpret_cast<const f32x4*>(src + at + 4) : f32x4{};
+        split(a4, b4, q[t][i]);
+      }
     }
   }
   const int first_last = col.last(0, G);                     // all rows see the keys up to here
@@ -205,18 +232,20 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
       const float ks = K::SCALED ? e4m3_scale_value(s.ks[kt]) : 1.f;
 #pragma unroll
       for (int i = 0; i < K::KP; ++i) {
-        if constexpr (K::F32) {
+        if constexpr (K::FLOATS) {
           f32x4 k = floats(s.k[kt][i], 0, ks);
           if (c.d != D && K::k_channel(i, g) >= c.d) k = f32x4{};
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[t][kt] = mfma(k[e], __uint_as_float(q[t][i][e]), x[t][kt]);
+            for (int e = 0; e < 4; ++e) x[t][kt] = mfma(k[e], __uint_as_float(q[t][i][0][e]), x[t][kt]);
         } else {
           u32x4 k = pairs(s.k[kt][i], ks);
           if (c.d != D && K::k_channel(i, g) >= c.d) k = u32x4{};
 #pragma unroll
-          for (int t = 0; t < NT; ++t) x[t][kt] = mfma(k, q[t][i], x[t][kt]);
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int part = K::PARTS - 1; part >= 0; --part) x[t][kt] = mfma(k, q[t][i][part], x[t][kt]);
         }
       }
     }
@@ -304,7 +333,29 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
           }
         }
     }
-    if constexpr (K::F32) {
+    if constexpr (K::LATER) {
+      // (the later parts of a weight are 0 or negative, and make a NaN of an infinity)
+      u16x2 most{};
+#pragma unroll
+      for (int kt = 0; kt < K::KT; ++kt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < K::VP; ++i)
+#pragma unroll
+            for (int w = 0; w < K::VN / 2; ++w) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, s.v[kt][j][i].x[w] & 0x7fff7fffu));
+      const bool bad = most[0] >= 0x7f80 || most[1] >= 0x7f80;
+      if (__any(bad)) {
+        odd |= bad;
+#pragma unroll
+        for (int kt = 0; kt < K::KT; ++kt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < K::VP; ++i) drop_odd(s.v[kt][j][i]);
+      }
+    }
+    if constexpr (K::FLOATS) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -321,10 +372,14 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
     } else {
 #pragma unroll
       for (int h = 0; h < K::KT; h += 2) {
-        u32x4 w[NT];
+        u32x4 w[NT][K::PARTS];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-          w[t] = u32x4{pack2(x[t][h][0], x[t][h][1]), pack2(x[t][h][2], x[t][h][3]), pack2(x[t][h + 1][0], x[t][h + 1][1]), pack2(x[t][h + 1][2], x[t][h + 1][3])};
+        for (int t = 0; t < NT; ++t) {
+          if constexpr (K::PARTS == 1)
+            w[t][0] = u32x4{pack2(x[t][h][0], x[t][h][1]), pack2(x[t][h][2], x[t][h][3]), pack2(x[t][h + 1][0], x[t][h + 1][1]), pack2(x[t][h + 1][2], x[t][h + 1][3])};
+          else
+            split(x[t][h], x[t][h + 1], w[t]);
+        }
 #pragma unroll
         for (int i = 0; i < K::VP; ++i) {
           // [key][channel pair] to [channel][key pair]
@@ -338,7 +393,9 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
 #pragma unroll
             for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(v[2 * j + 1][e / 2], v[2 * j][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) o[t][i * K::VN + e] = mfma(f, w[t], o[t][i * K::VN + e]);
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int part = K::PARTS - 1; part >= 0; --part) o[t][i * K::VN + e] = mfma(f, w[t][part], o[t][i * K::VN + e]);
           }
         }
       }
@@ -393,7 +450,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
       }
       if (any_odd) {
         const int upto = min(to - 1, col.last(r, G));
-        for (int key = max(from, first_last + 1); key <= upto; ++key) {
+        for (int key = K::LATER ? from : max(from, first_last + 1); key <= upto; ++key) {
           const int page = (int)((uint32_t)key / (uint32_t)c.block_rows), off = key - page * c.block_rows, block = table[page];
           if (block < 0 || block >= c.n_blocks) continue;
           const E* v = vx + block * c.block + (int64_t)off * c.row;
@@ -434,9 +491,9 @@ AttPlan plan_of(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens, 
   p.tile = 16 * tiles_of_rows(c.d, n, n_tokens, G);
   const int64_t columns = has_start ? n_tokens * G / p.tile + n : (int64_t)n * ((G + p.tile - 1) / p.tile);
   p.columns = (int32_t)(columns < 0x7fffffff ? columns : 0x7fffffff);
-  p.shares = !may_share ? 0 : COMPUTE_UNITS * resident(dtype == LAQ_F32, c.type == LAQ_E4M3, c.d, p.tile / 16);
+  p.shares = !may_share ? 0 : COMPUTE_UNITS * resident(dtype == LAQ_F32, c.type, c.d, p.tile / 16);
   if (may_share && max_rows > 0) {
-    const int turn = ATT_WAVES * 16 * (dtype == LAQ_F32 ? 1 : c.type == LAQ_E4M3 ? 4 : 2);
+    const int turn = ATT_WAVES * 16 * (c.type == LAQ_F32 ? 1 : c.type == LAQ_E4M3 ? 4 : 2);
     const int64_t turns = columns * c.Hkv * (((int64_t)max_rows + turn - 1) / turn);
     if (turns < p.shares) p.shares = (int32_t)turns;
   }
