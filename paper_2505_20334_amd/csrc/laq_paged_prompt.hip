@@ -11,9 +11,6 @@ namespace laq {
 
 namespace {
 
-#ifndef KO
-#define KO 0x406
-#endif
 constexpr int WAVES = 4, THREADS = 64 * WAVES, WAVE_ROWS = 32, TILE = WAVES * WAVE_ROWS, STAGE = 64;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -24,7 +21,7 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 acc) {
 }
 
 // LDS and memory operations and products stay on their side; other instructions may pass.
-__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(KO); }
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x406); }
 
 // Where piece `piece` (eight numbers) of row `row` lies in LDS, in numbers.
 template <int D> __device__ __forceinline__ int k_place(int row, int piece) { return row * D + (piece ^ (row & (D / 8 - 1))) * 8; }
@@ -44,9 +41,9 @@ __device__ __forceinline__ bool ranked_column(const PagedView& c, const PagedAtt
     if (held > r.held || (held == r.held && i < lane)) before += t;
     all += t;
   }
+  if (rank >= all) return false;
   const int round = COMPUTE_UNITS / H;
   if (rank >= round && rank < 2 * round) rank = round + min(2 * round, all) - 1 - rank;
-  if (rank >= all) return false;
   const uint64_t mine = __ballot(rank >= before && rank < before + tiles);
   if (mine == 0) return false;
   const int l = __builtin_ctzll(mine);
@@ -324,16 +321,15 @@ int64_t columns_of(int G, int n, int64_t n_tokens) { return n_tokens * G / TILE 
 
 }  // namespace
 
-#ifndef PROMPT_ROWS
-#define PROMPT_ROWS 65
-#endif
-#ifndef PROMPT_COLS
-#define PROMPT_COLS 128
-#endif
+// With more score rows of a request than the other kernel's tile and enough columns to keep the device busy.  This kernel : the one that shares keys out, us, 32
+// heads on 8: 32 requests of 1000 to 2000 rows, 10 tokens 66 : 80 (d = 64 49 : 43, so there from 64 score rows on), 16 tokens 67 : 82, 32 tokens 87 : 139; 16 of 1000 to 4096, 64 tokens 126 : 210.  128 workgroups: four requests of 8192 rows, 128 tokens 235 : 317,
+// 16 of 2048, 20 tokens 64 : 80, but two of 8192, 256 tokens 234 : 167 and one of 16384, 512 tokens 456 : 310 (many tiles of a request read its keys from the caches
+// there); 64: eight of 4096, 32 tokens 122 : 93, one of 16384, 256 tokens 456 : 171.
 bool paged_prompt_call(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens) {
+  if (dtype != LAQ_BF16 || c.d > 128) return false;
   const int G = Hq / c.Hkv;
-  const int64_t columns = columns_of(G, n, n_tokens) * c.Hkv;
-  return dtype == LAQ_BF16 && c.d <= 128 && (n_tokens + n - 1) / n * G >= PROMPT_ROWS && columns >= PROMPT_COLS && columns < (1 << 24);
+  const int64_t rows = (n_tokens + n - 1) / n * G, tiles = (rows + TILE - 1) / TILE, columns = tiles * n * c.Hkv;
+  return rows >= (c.d <= 64 ? 64 : 33) && columns >= (tiles <= 4 ? 128 : 160) && columns_of(G, n, n_tokens) * c.Hkv < (1 << 24);
 }
 
 hipError_t launch_paged_prompt(const PagedView& c, const PagedAttention& a, hipStream_t st) {

@@ -393,6 +393,68 @@ def test_several_tokens_see_up_to_their_own_row(dtype, kind, Hq, H, d, br, rows,
     c.check(*c.run(split=False), what="whole")
 
 
+PROMPTS = [  # bf16, enough score rows and columns for the kernel of whole prompts: (cache, Hq, H, d, block, lengths, tokens)
+    (BF16, 32, 32, 128, 16, [300, 64, 40, 41], [40, 33, 40, 35]), (E4M3, 32, 32, 128, 64, [300, 200, 40, 129, 37], [40, 64, 40, 65, 1]),
+    (BF16, 32, 32, 96, 48, [300, 140, 50, 0], [129, 128, 50, 3]), (E4M3, 16, 16, 80, 16, [200, 130, 50, 90], [130, 129, 60, 0]), (BF16, 32, 32, 64, 32, [500, 300, 70, 90], [64, 64, 70, 80]),
+    (E4M3, 32, 32, 24, 16, [150, 64, 70, 90], [64, 64, 70, 80]), (BF16, 32, 8, 128, 64, [700, 300, 129, 600], [130, 120, 110, 100]), (BF16, 14, 2, 128, 256, [513], [513]),
+    (E4M3, 28, 4, 128, 16, [1030, 64], [150, 64]), (BF16, 4, 2, 72, 16, [40 + i for i in range(70)], [17 + i % 5 for i in range(70)]), (BF16, 40, 1, 128, 32, [30 + 2 * i for i in range(130)], [1] * 130),
+]
+
+
+@pytest.mark.parametrize("kind,Hq,H,d,br,rows,tokens", PROMPTS)
+def test_prompts(kind, Hq, H, d, br, rows, tokens):
+    print("case:", kind, Hq, H, d, br, rows, tokens, flush=True)
+    c = Case(BF16, kind, Hq, H, d, br, rows, tokens, token_major=br == 64, fused=br == 48)
+    got = c.run()
+    c.check(*got)
+    again = c.run(split=False)
+    c.check(*again)
+    if _laq().laq_cache_attention_workspace_bytes(c.cache, Hq, BF16, len(rows), sum(tokens), max(rows)) == 0:      # (that kernel shares nothing out)
+        assert all(torch.equal(x, y) for x, y in zip(got, again))
+
+
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+def test_blocks_of_prompts_that_are_not_there(kind):
+    c = Case(BF16, kind, 32, 32, 128, 32, [300, 200, 70, 90], [40, 50, 60, 90])
+    for i, page, bad in ((0, 2, -1), (0, 9, c.n_blocks), (1, 0, 2 ** 31 - 1), (2, 0, -5), (3, 1, c.n_blocks)):
+        c.table[i, page] = bad
+        c.hidden[i] |= set(range(32 * page, 32 * page + 32))
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("at", [299, 260, 270, 100, 290])
+def test_odd_numbers_of_prompts_reach_those_that_see_them_alone(kind, what, at):
+    def put(k, v):
+        v[at, 3, 50] = what
+        k[300 + 60, 5, 7] = what
+    c = Case(BF16, kind, 32, 32, 128, 16, [300, 100, 70, 90], [40, 50, 60, 90], special=put)
+    out, lse = c.run()
+    torch.cuda.synchronize()
+    want, odd_lse = torch.zeros(out.shape, dtype=torch.bool), torch.zeros(lse.shape, dtype=torch.bool)
+    first = max(0, at - 260)
+    if kind == E4M3:
+        want[first:40, 3] = True
+    else:
+        want[first:40, 3, 50] = True
+    # a key with a NaN makes one of every token that sees it; one with an infinity of half of them or so (a weight of 0 otherwise)
+    odd_k = ~torch.isfinite(out.cpu())
+    odd_k[:40] = False
+    got = ~torch.isfinite(out.cpu())
+    got[40:] = False
+    assert torch.equal(got, want)
+    if kind != E4M3:
+        x = out.cpu()[first:40, 3, 50]
+        assert x.isnan().all() if math.isnan(what) else (x == what).all()
+    seen = torch.zeros(out.shape[:2], dtype=torch.bool)
+    seen[50:90, 5] = True
+    if math.isnan(what) or kind == E4M3:
+        assert torch.equal(odd_k.all(-1), seen) and torch.equal(odd_k.any(-1), seen)
+    else:
+        assert not (odd_k.any(-1) & ~seen).any()
+
+
 @pytest.mark.parametrize("dtype,kind", [(BF16, BF16), (BF16, E4M3), (F32, F32)])
 def test_rows_that_are_not_there(dtype, kind):
     c = Case(dtype, kind, 8, 2, 64, 32, [900, 700, 64], [3, 1, 2])
@@ -661,6 +723,105 @@ def test_evict_into_the_cache_and_decode_on_it(kind):
     kk, _ = laq.laq_cache_load(cache, back)
     torch.cuda.synchronize()
     assert torch.equal(kk[:64].transpose(0, 1).cpu().double(), plain.held(k1[:H * 64].view(H, 64, d).cpu(), kind))
+
+
+def test_the_calls_without_the_compiled_binding(monkeypatch):
+    laq = _laq()
+    from paper_2505_20334_amd import binding
+    laq.load_library()
+    c = Case(BF16, E4M3, 8, 2, 64, 16, [200, 30], [3, 2])
+    gen = torch.Generator().manual_seed(4)
+    q, k = torch.randn(5, 4, 64, generator=gen).to(BF16).to(DEV), torch.randn(5, 2, 64, generator=gen).to(BF16).to(DEV)
+    p, rope = torch.arange(5, dtype=torch.int32, device=DEV), laq.Rope(laq.laq_rope_frequencies(32, device=DEV), "interleaved")
+    src, idx = torch.randn(2, 2, 40, 64, generator=gen).to(BF16).to(DEV), torch.arange(10, dtype=torch.int32, device=DEV).repeat(4)
+
+    def calls():
+        cache = _pool(4, 2, 16, 64, E4M3)
+        got = list(laq.laq_rope(q, k, p, rope))
+        got.append(laq.laq_cache_append(cache, k, k, p, q=q, positions=p, rope=rope))
+        laq.laq_cache_compact(cache, src, src, idx, [10, 10], torch.arange(20, 40, dtype=torch.int32, device=DEV))
+        got += list(laq.laq_cache_load(cache, torch.arange(-1, 40, dtype=torch.int32, device=DEV), F32)) + list(c.run()) + list(c.run(split=False))
+        torch.cuda.synchronize()
+        return got
+    want = calls()
+    monkeypatch.setattr(binding, "_native", None)
+    for x, y in zip(want, calls()):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype,kind,tokens,row", [(BF16, BF16, 1, 1 << 24), (F32, F32, 3, 1 << 24), (BF16, E4M3, 40, 1 << 24), (BF16, BF16, 2, (1 << 24) - 8)])
+def test_rows_far_apart(dtype, kind, tokens, row):
+    laq = _laq()
+    d, rows, H = 64, 30, 1
+    planes = []
+    for _ in range(2):
+        flat = torch.empty(32 * row, dtype=torch.uint8 if kind == E4M3 else kind, device=DEV).view(kind)
+        planes.append(flat.as_strided((2, H, 16, d), (16 * row, d, row, 1)))
+        planes.append(torch.zeros(2, H, 16, dtype=torch.uint8, device=DEV) if kind == E4M3 else None)
+    cache = laq.PagedCache(*planes)
+    gen = torch.Generator().manual_seed(9)
+    k, v = torch.randn(rows, H, d, generator=gen), torch.randn(rows, H, d, generator=gen)
+    slots = torch.arange(rows, dtype=torch.int32, device=DEV)
+    laq.laq_cache_append(cache, k.to(DEV), v.to(DEV), slots)
+    kk, vv = laq.laq_cache_load(cache, slots, F32)
+    torch.cuda.synchronize()
+    assert torch.equal(kk.cpu().double(), plain.held(k, kind)) and torch.equal(vv.cpu().double(), plain.held(v, kind))
+    c = Case(dtype, kind, 2, H, d, 16, [rows], [min(tokens, rows)])
+    c.cache, c.table, c.k, c.v = cache, torch.tensor([[0, 1]], dtype=torch.int32, device=DEV), plain.held(k, kind), plain.held(v, kind)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype,kind,tokens", [(BF16, BF16, [1, 1, 1]), (F32, E4M3, [3, 1, 2]), (BF16, E4M3, [40, 2, 1])])
+def test_as_many_rows_as_a_table_may_hold(dtype, kind, tokens):
+    """Lengths next to 2^31: all but the last few blocks are not there."""
+    laq = _laq()
+    H, d, br = 1, 64, 4096
+    long = (1 << 31) - br
+    c = Case(dtype, kind, 2, H, d, br, [100, 130, 70], tokens)
+    width = long // br
+    table = torch.full((3, width), -1, dtype=torch.int32, device=DEV)
+    table[:, -1] = c.table[:, 0]
+    rows = torch.tensor([long - br + 100, 130, long - br + 70], dtype=torch.int32, device=DEV)
+    table[1, 0] = c.table[1, 0]
+    c.table, c.rows_d = table, rows
+    for max_rows in (long, 4096):
+        c.check(*c.run(max_rows=max_rows))
+    assert laq.laq_cache_attention_workspace_bytes(c.cache, 2, dtype, 3, sum(tokens), long) < 1 << 30
+
+
+def test_many_workgroups_of_a_column_on_two_streams_and_in_graphs_with_one_workspace():
+    c = Case(BF16, E4M3, 8, 1, 128, 64, [60000], [1])
+    e = Case(F32, F32, 8, 2, 64, 16, [9000, 5, 7000], [2, 1, 3])
+    want, want_e = c.run(), e.run()
+    torch.cuda.synchronize()
+    c.check(*want), e.check(*want_e)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        with torch.cuda.stream(a):
+            got = c.run()
+        with torch.cuda.stream(b):
+            got_e = e.run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got + got_e, want + want_e))
+    laq = _laq()
+    ws = torch.full((max(laq.laq_cache_attention_workspace_bytes(c.cache, 8, BF16, 1, 1, 60000), laq.laq_cache_attention_workspace_bytes(e.cache, 8, F32, 3, 6, 9000)),), 0xA5,
+                    dtype=torch.uint8, device=DEV)
+    outs = [tuple(torch.zeros_like(x) for x in w) for w in (want, want_e)]
+    graphs = []
+    for case, (out, lse) in zip((c, e), outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=a):
+            case.run(out=out, lse=lse, ws=ws)
+        graphs.append(g)
+    for i in range(8):
+        for x in outs[i % 2]:
+            x.fill_(3)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs[i % 2], (want, want_e)[i % 2]))
+        other = (e, c)[i % 2].run(ws=ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(other, (want_e, want)[i % 2]))
 
 
 def test_every_code_and_scale_reads_as_its_number():

@@ -186,9 +186,10 @@ def test_workspaces_of_long_bounds_stay_small():
     c = ctypes.byref(_cache(n_blocks=4))
     for Hq, n, T in ((2, 1, 1), (8, 1, 3), (8, 3, 3), (2, 40, 40), (64, 512, 512), (64, 4, 4096)):
         long = lib.laq_cache_attention_workspace_bytes(c, Hq, 1, n, T, 1 << 30)
-        assert 0 < long < 1 << 31
+        # (none for chunks of a prompt, which are not shared out)
+        assert (long == 0) == (T == 4096) and long < 1 << 31
         for most in ((1 << 31) - 4096, (1 << 31) - 255, (1 << 31) - 16):
-            assert 0 < lib.laq_cache_attention_workspace_bytes(c, Hq, 1, n, T, most) < 1 << 31
+            assert lib.laq_cache_attention_workspace_bytes(c, Hq, 1, n, T, most) == long
 
 
 def test_the_binding_refuses_host_tensors_and_sizes():
@@ -309,6 +310,29 @@ def test_what_is_refused(native):
                                   "torch.vmap(lambda x: laq.laq_cache_compact(cache, x, None, ints(200), [10, 20, 30], ints(60)))(source[None])"])
 def test_a_tensor_without_an_address(call):
     assert outcomes([call])[0].startswith("raised RuntimeError Cannot access data pointer")
+
+
+# what a call makes: number of tensors
+MADE = {"laq.laq_cache_load(paged_cache, ints(3), stream=stream)": 2, "laq.laq_rope(made(3, 8, 128), made(3, 2, 128), ints(3), rope, stream=stream)": 2,
+        "laq.laq_cache_append(paged_cache, made(3, 2, 128), None, ints(3), q=made(3, 8, 128), positions=ints(3), rope=rope, stream=stream)": 1,
+        "laq.laq_cache_attention(made(1, 8, 128), paged_cache, ints(1, 4000), ints(1), want_lse=True, stream=stream)": 3}
+
+
+@pytest.mark.parametrize("call", list(MADE))
+def test_memory_is_taken_under_the_stream_of_the_call(call):
+    import test_streams
+    setup = test_streams.SETUP.replace("    torch.empty = counted\n", """    paged_cache = laq.PagedCache(made(8, 2, 16, 128), None, made(8, 2, 16, 128), None)
+    rope = laq.Rope(made(64, dtype=torch.float32))
+    torch.empty = counted
+""")
+    res = subprocess.run([sys.executable, "-c", setup % ("binding._native = None; " + call)], capture_output=True, text=True, timeout=110)
+    assert res.returncode == 0, res.stderr[-800:]
+    n = MADE[call]
+    own, side, number, default = res.stdout.strip().splitlines()[-4:]
+    # (memory of the inputs is made here too, on the current stream: what follows it is the call's)
+    tails = [line[1:line.index("]")].replace(" ", "").split(",")[-n:] for line in (own, side, number, default)]
+    assert tails == [["0"] * n, ["77"] * n, ["78"] * n, ["0"] * n], (own, side, number, default)
+    assert side.endswith(str([0] * n)) and number.endswith(str([0] * n))
 
 
 def test_the_library_exports_what_its_third_header_declares(repo_root):
