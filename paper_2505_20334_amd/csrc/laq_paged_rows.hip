@@ -84,11 +84,14 @@ __device__ __forceinline__ Eight read8(const E4m3* p, float scale) {
 
 template <typename C> constexpr bool scaled() { return std::is_same<C, E4m3>::value; }
 
-// The largest of x over the LANES lanes of a group.
+// The largest of x over the LANES lanes of a group: neighbours, pairs, and the mirrored other half of 8 and of 16 lanes, without LDS.
 template <int LANES>
 __device__ __forceinline__ uint32_t group_max(uint32_t x) {
-#pragma unroll
-  for (int m = 1; m < LANES; m *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, m));
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xf, 0xf, true));
+  if constexpr (LANES >= 16) x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xf, 0xf, true));
+  if constexpr (LANES >= 32) x = max(x, (uint32_t)__shfl_xor((int)x, 16));
   return x;
 }
 
