@@ -53,7 +53,8 @@ __device__ __forceinline__ bool ranked_column(const PagedView& c, const PagedAtt
   return true;
 }
 
-template <typename E, int D>
+// WIDE: blocks of a multiple of 64 rows, so that a stage lies in one (a stage's 260 scalar instructions in front of 32 products are 130 then).
+template <typename E, int D, bool WIDE>
 __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, PagedAttention a) {
   constexpr bool SCALED = std::is_same<E, E4m3>::value;
   constexpr int PIECES = D / 8, ROWS = THREADS / PIECES, PASSES = STAGE / ROWS;     // of a row; rows that the workgroup reads at once
@@ -103,8 +104,9 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
   // stages: this thread's pieces of 64 rows
   const int piece = threadIdx.x % PIECES, my_row = threadIdx.x / PIECES, wave_row = wave * (64 / PIECES);
   const int row_bytes = (int)(c.row * sizeof(E));
-  // (channels beyond d: nothing is read, zeros)
-  const int my_at = piece * 8 < c.d ? (my_row & 15) * row_bytes + piece * (8 * (int)sizeof(E)) : 0x7fffffff - 16;
+  // (channels beyond d: behind the end, where nothing is read; zeros)
+  const int pass_bytes = piece * 8 < c.d ? ROWS * row_bytes : 0;
+  const int my_at = piece * 8 < c.d ? (WIDE ? my_row : my_row & 15) * row_bytes + piece * (8 * (int)sizeof(E)) : 0x7fffffff - 16;
   const E *kx = static_cast<const E*>(c.k.x) + head * c.head, *vx = static_cast<const E*>(c.v.x) + head * c.head;
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
   const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)request * a.blocks_per_inst);
@@ -113,6 +115,10 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
   int page = 0, off = 0, blocks[STAGE / 16];                           // of the stage that is read next
   uint32_t there_next = 0, there = 0;                                  // a bit for each tile of 16 rows: of the stage on its way; of the one in use
   const auto ask = [&](int left) {
+    if constexpr (WIDE) {
+      blocks[0] = left > 0 ? table[page] : -1;
+      return;
+    }
     int pg = page, of = off;
 #pragma unroll
     for (int i = 0; i < STAGE / 16; ++i) {
@@ -125,6 +131,35 @@ __global__ __launch_bounds__(THREADS, 2) void paged_prompt_kernel(PagedView c, P
     }
   };
   const auto load = [&](int left) {
+    if constexpr (WIDE) {
+      const bool is = (uint32_t)blocks[0] < (uint32_t)c.n_blocks;      // (-1 is not)
+      const int block = is ? blocks[0] : 0;
+      const int64_t base = block * c.block + (int64_t)off * c.row;
+      const uint32_t bytes = is ? (uint32_t)(min(STAGE, left) - 1) * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E)) : 0u;
+      const __amdgpu_buffer_rsrc_t kb = tile_of(kx + base, bytes), vb = tile_of(vx + base, bytes);
+      there_next = is ? 15u : 0u;
+#pragma unroll
+      for (int u = 0; u < PASSES; ++u) {
+        fetch<false>(k[u], kb, my_at + u * pass_bytes);
+        fetch<false>(v[u], vb, my_at + u * pass_bytes);
+      }
+      if constexpr (SCALED) {
+        const int64_t sc = ((int64_t)block * H + head) * c.block_rows + off;
+        const __amdgpu_buffer_rsrc_t ksb = tile_of(c.k.scales + sc, is ? (uint32_t)STAGE : 0u), vsb = tile_of(c.v.scales + sc, is ? (uint32_t)STAGE : 0u);
+#pragma unroll
+        for (int u = 0; u < PASSES; ++u) {
+          ks[u] = __builtin_amdgcn_raw_buffer_load_b8(ksb, my_row + u * ROWS, 0, 0);
+          vs[u] = __builtin_amdgcn_raw_buffer_load_b8(vsb, my_row + u * ROWS, 0, 0);
+        }
+      }
+      off += STAGE;
+      if (off >= c.block_rows) {
+        off = 0;
+        ++page;
+      }
+      ask(left - STAGE);
+      return;
+    }
     int64_t base[STAGE / 16], scales[STAGE / 16];
     uint32_t bytes[STAGE / 16];
     there_next = 0;
@@ -334,13 +369,19 @@ bool paged_prompt_call(const PagedView& c, int Hq, int dtype, int n, int64_t n_t
 
 hipError_t launch_paged_prompt(const PagedView& c, const PagedAttention& a, hipStream_t st) {
   const dim3 grid((unsigned)(columns_of(a.Hq / c.Hkv, a.n, a.n_tokens) * c.Hkv));
-  if (c.type == LAQ_BF16) {
-    if (c.d <= 64) hipLaunchKernelGGL((paged_prompt_kernel<uint16_t, 64>), grid, dim3(THREADS), 0, st, c, a);
-    else hipLaunchKernelGGL((paged_prompt_kernel<uint16_t, 128>), grid, dim3(THREADS), 0, st, c, a);
-  } else {
-    if (c.d <= 64) hipLaunchKernelGGL((paged_prompt_kernel<E4m3, 64>), grid, dim3(THREADS), 0, st, c, a);
-    else hipLaunchKernelGGL((paged_prompt_kernel<E4m3, 128>), grid, dim3(THREADS), 0, st, c, a);
-  }
+  const auto start = [&](auto numbers, auto d, auto wide) {
+    hipLaunchKernelGGL((paged_prompt_kernel<std::remove_pointer_t<decltype(numbers)>, d(), wide()>), grid, dim3(THREADS), 0, st, c, a);
+  };
+  const auto by_size = [&](auto numbers, auto wide) {
+    if (c.d <= 64) start(numbers, std::integral_constant<int, 64>{}, wide);
+    else start(numbers, std::integral_constant<int, 128>{}, wide);
+  };
+  const auto by_type = [&](auto wide) {
+    if (c.type == LAQ_BF16) by_size((uint16_t*)nullptr, wide);
+    else by_size((E4m3*)nullptr, wide);
+  };
+  if (c.block_rows % STAGE == 0) by_type(std::true_type{});
+  else by_type(std::false_type{});
   return hipGetLastError();
 }
 
