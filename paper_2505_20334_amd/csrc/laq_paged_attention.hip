@@ -52,7 +52,7 @@ constexpr int resident(bool f32, int type, int d, int nt) {
 }
 
 // Q: the queries' numbers (and what the products are made in), E: the cache's, D: head sizes up to D, NT: 16 score rows NT times.
-template <typename Q, typename E, int D, int NT>
+template <typename Q, typename E, int D, int NT, bool W>
 struct Kinds {
   static constexpr bool F32 = std::is_same<Q, float>::value, SCALED = std::is_same<E, E4m3>::value;
   // fp32: products of fp32 where the cache is, otherwise of bf16, in which the cache's numbers are exact, with queries and weights as sums of three
@@ -64,6 +64,11 @@ struct Kinds {
   // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on
   static constexpr int KW = 16 / (KN * (int)sizeof(E));
   static constexpr __host__ __device__ int k_channel(int i, int g) { return i / KW * (4 * KW * KN) + g * (KW * KN) + i % KW * KN; }
+  // blocks of a multiple of a step's keys, so that a step lies in one: one descriptor for its tiles
+  // (8 bits, whose steps have four tiles: 128 requests of 1000 to 8192 rows 214 -> 209 us, 12 tokens of fp32 with d = 256 244 -> 199; others +-1 %, and where registers
+  // are short already it costs more: fp32 with d = 128 70 -> 83)
+  static constexpr bool WIDE = W, MAY_BE_WIDE = SCALED && !(F32 && D <= 128 && NT == 1);
+  static constexpr int SPANS = WIDE ? 1 : KT, SPAN = 16 * KT / SPANS;        // descriptors of a step; keys of each
   static constexpr int RESIDENT = resident(F32, FLOATS ? LAQ_F32 : SCALED ? LAQ_E4M3 : LAQ_BF16, D, NT);      // workgroups of a compute unit (a wave of each on every SIMD)
   static constexpr bool ONCE = NT == 1;                      // one workgroup reads a row: past the caches
   static constexpr int VN = FLOATS || D == 64 ? 4 : 8, VP = D / (16 * VN);
@@ -77,9 +82,9 @@ struct StepKeys {
   Raw<E, K::KN> k[K::KT][K::KP];
   Raw<E, K::VN> v[K::KT][4][K::VP];
   uint32_t ks[K::KT], vs[K::KT];                             // SCALED: of this lane's key row; of its four keys of V
-  // of the step that is read next: where its tiles begin (numbers; scales), and how many bytes of each there are (0: not there)
-  int64_t base[K::KT], scales[K::KT];
-  uint32_t bytes[K::KT];
+  // of the step that is read next: where its spans begin (numbers; scales), and how many bytes of each there are (0: not there)
+  int64_t base[K::SPANS], scales[K::SPANS];
+  uint32_t bytes[K::SPANS];
 };
 // W pieces side by side, 16 bytes together.
 template <bool ONCE, int W, typename R>
@@ -97,9 +102,9 @@ __device__ __forceinline__ void fetch_wide(R* r, __amdgpu_buffer_rsrc_t tile, in
   }
 }
 
-template <typename Q, typename E, int D, int NT>
-__global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
-  using K = Kinds<Q, E, D, NT>;
+template <typename Q, typename E, int D, int NT, bool WIDE>
+__global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) void paged_attention_kernel(PagedView c, PagedAttention a, AttPlan p, Partials part) {
+  using K = Kinds<Q, E, D, NT, WIDE>;
   constexpr int STEP = 16 * K::KT, TURN = STEP * ATT_WAVES;
   __shared__ float sums[ATT_WAVES][16][K::PAD];
   __shared__ float2 marks[ATT_WAVES][16];
@@ -162,6 +167,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
   int v_at[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) v_at[j] = (4 * g + j) * row_bytes + n * (K::VN * (int)sizeof(E));
+  const int tile_bytes = 16 * row_bytes;
   const E *kx = static_cast<const E*>(c.k.x) + head * c.head, *vx = static_cast<const E*>(c.v.x) + head * c.head;
   typedef __attribute__((address_space(4))) const int32_t* ConstTable;
   const ConstTable table = (ConstTable)(unsigned long long)(a.table + (int64_t)sh.request * a.blocks_per_inst);
@@ -177,13 +183,13 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
       ++w.page;
     }
   };
-  int blocks[K::KT];                                         // of the step that is loaded next
+  int blocks[K::SPANS];                                      // of the step that is loaded next
   const auto ask = [&](int left) {
     Place w = at;
 #pragma unroll
-    for (int kt = 0; kt < K::KT; ++kt) {
-      blocks[kt] = 16 * kt < left ? table[w.page] : -1;
-      forward(w, 0, 16);
+    for (int i = 0; i < K::SPANS; ++i) {
+      blocks[i] = K::SPAN * i < left ? table[w.page] : -1;
+      forward(w, 0, K::SPAN);
     }
   };
   // The step at `at`, with `left` keys from its beginning on (none: nothing is read).  Rows behind them are not read: zeros.  K first, which moves what is
@@ -191,20 +197,23 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
   const auto load_k = [&](int left, StepKeys<K, E>& s) {
     Place w = at;
 #pragma unroll
-    for (int kt = 0; kt < K::KT; ++kt) {
-      const int block = blocks[kt];
-      const bool there = block >= 0 && block < c.n_blocks;
-      const int rows = min(16, left - 16 * kt);
-      s.bytes[kt] = there ? (uint32_t)(rows - 1) * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E)) : 0u;
-      s.base[kt] = there ? block * c.block + (int64_t)w.off * c.row : 0;
-      const __amdgpu_buffer_rsrc_t kb = tile_of(kx + s.base[kt], s.bytes[kt]);
+    for (int i = 0; i < K::SPANS; ++i) {
+      const bool there = (uint32_t)blocks[i] < (uint32_t)c.n_blocks;         // (-1 is not)
+      const int block = there ? blocks[i] : 0;
+      const int rows = min(K::SPAN, left - K::SPAN * i);
+      s.bytes[i] = there ? (uint32_t)(rows - 1) * (uint32_t)row_bytes + (uint32_t)(c.d * (int)sizeof(E)) : 0u;
+      s.base[i] = block * c.block + (int64_t)w.off * c.row;
+      if constexpr (K::SCALED) s.scales[i] = ((int64_t)block * H + head) * c.block_rows + w.off;
+      forward(w, 0, K::SPAN);
+    }
 #pragma unroll
-      for (int i = 0; i < K::KP; i += K::KW) fetch_wide<K::ONCE, K::KW>(&s.k[kt][i], kb, k_at + i / K::KW * 64);
-      if constexpr (K::SCALED) {
-        s.scales[kt] = there ? ((int64_t)block * H + head) * c.block_rows + w.off : 0;
-        s.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.k.scales + s.scales[kt], there ? 16u : 0u), n, 0, 0);
-      }
-      forward(w, 0, 16);
+    for (int kt = 0; kt < K::KT; ++kt) {
+      const int i = WIDE ? 0 : kt, more = WIDE ? kt * tile_bytes : 0;
+      const __amdgpu_buffer_rsrc_t kb = tile_of(kx + s.base[i], s.bytes[i]);
+#pragma unroll
+      for (int x = 0; x < K::KP; x += K::KW) fetch_wide<K::ONCE, K::KW>(&s.k[kt][x], kb, k_at + more + x / K::KW * 64);
+      if constexpr (K::SCALED)
+        s.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(tile_of(c.k.scales + s.scales[i], s.bytes[i] ? (uint32_t)K::SPAN : 0u), n + (WIDE ? 16 * kt : 0), 0, 0);
     }
     forward(at, turn_pages, turn_rows);
     ask(left - TURN);
@@ -212,12 +221,14 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
   const auto load_v = [&](StepKeys<K, E>& s) {
 #pragma unroll
     for (int kt = 0; kt < K::KT; ++kt) {
-      const __amdgpu_buffer_rsrc_t vb = tile_of(vx + s.base[kt], s.bytes[kt]);
+      const int i = WIDE ? 0 : kt, more = WIDE ? kt * tile_bytes : 0;
+      const __amdgpu_buffer_rsrc_t vb = tile_of(vx + s.base[i], s.bytes[i]);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < K::VP; ++i) fetch<K::ONCE>(s.v[kt][j][i], vb, v_at[j] + i * (16 * K::VN * (int)sizeof(E)));
-      if constexpr (K::SCALED) s.vs[kt] = __builtin_amdgcn_raw_buffer_load_b32(tile_of(c.v.scales + s.scales[kt], s.bytes[kt] ? 16u : 0u), 4 * g, 0, 0);
+        for (int x = 0; x < K::VP; ++x) fetch<K::ONCE>(s.v[kt][j][x], vb, v_at[j] + more + x * (16 * K::VN * (int)sizeof(E)));
+      if constexpr (K::SCALED)
+        s.vs[kt] = __builtin_amdgcn_raw_buffer_load_b32(tile_of(c.v.scales + s.scales[i], s.bytes[i] ? (uint32_t)K::SPAN : 0u), 4 * g + (WIDE ? 16 * kt : 0), 0, 0);
     }
   };
 
@@ -253,7 +264,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT>::RESIDENT)) void p
     bool there[K::KT], edge = min(left, first_last - key + 1) < STEP;   // a key that not every row sees
 #pragma unroll
     for (int kt = 0; kt < K::KT; ++kt) {
-      there[kt] = s.bytes[kt] != 0;
+      there[kt] = s.bytes[WIDE ? 0 : kt] != 0;
       edge |= !there[kt];
     }
     load_k(left - TURN, s);
@@ -512,13 +523,23 @@ Bytes bytes_of(const PagedView& c, const AttPlan& p) {
 template <typename Q, typename E, int D>
 hipError_t start_attention(const PagedView& c, const PagedAttention& a, const AttPlan& p, const Partials& part, hipStream_t st) {
   const dim3 grid((unsigned)(p.shares ? p.shares : (int64_t)p.columns * c.Hkv));
+  const auto start = [&](auto nt, auto wide) {
+    hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, nt(), wide()>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
+  };
+  const auto by_blocks = [&](auto nt) {
+    using K = Kinds<Q, E, D, nt(), true>;
+    if constexpr (K::MAY_BE_WIDE) {
+      if (c.block_rows % (16 * K::KT) == 0) return start(nt, std::true_type{});
+    }
+    start(nt, std::false_type{});
+  };
   if constexpr (D <= 128) {
     if (p.tile == 32) {
-      hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 2>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
+      by_blocks(std::integral_constant<int, 2>{});
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((paged_attention_kernel<Q, E, D, 1>), grid, dim3(ATT_THREADS), 0, st, c, a, p, part);
+  by_blocks(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
 
