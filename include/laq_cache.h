@@ -142,14 +142,17 @@ int laq_cache_load(const laq_cache *cache, int32_t dtype, int64_t n_tokens, cons
  *                 out = sum_j softmax_j(scale * <q, K_j>) V_j over these.  0 where there are none
  *   lse           fp32 [n_tokens, Hq], may be NULL: log sum_j exp(scale * <q, K_j>) (-infinity where there are none): with it two
  *                 attentions over different rows can be joined
- *   ws / ws_bytes optional device scratch.  With at least laq_cache_attention_workspace_bytes() bytes (same arguments), long rows are
- *                 spread over several workgroups; LAQ_ERR_WORKSPACE if given but smaller or not 16-byte aligned.
- *                 With and without it the last bits of `out` may differ
+ *   ws / ws_bytes optional device scratch.  With at least laq_cache_attention_workspace_bytes() bytes (same arguments; 0 for chunks of a
+ *                 prompt; it does not grow with max_rows) the keys of all requests are shared out evenly among as many workgroups as the
+ *                 device holds; without it a KV head's keys are read by one workgroup for every 16 or 32 score rows.  LAQ_ERR_WORKSPACE if given but smaller or not
+ *                 16-byte aligned.  With and without it the last bits of `out` may differ
  * A call that needs more than 2^24 workgroups is LAQ_ERR_UNSUPPORTED.  What the rows behind r, other blocks of the pool and rows that a token does
  * not see hold (infinities and NaN too) does not reach out or lse.
  * bf16: the products of q and K are exact, sums, maxima and weights are fp32, weights are rounded to bf16 for the product with V, out
- * is rounded once.  fp32: all products and sums in fp32.  Weights are up to 2^8 before they are divided by their sum: sums over
- * numbers of V beyond 2^88 may overflow.
+ * is rounded once.  fp32: products and sums in fp32; over caches of bf16 and 8 bits, which are exact in bf16, as bf16 products of queries and weights that are
+ * the sums of three bf16 (2^-24; parts below 2^-126 count as 0).  Weights are up to 2^8 before they are divided by their sum: sums over
+ * numbers of V beyond 2^88 may overflow.  Visible scores that are all -infinity give 0 and an lse of -infinity.  An infinity in V that is seen with a weight so small that fp32
+ * has 0 for it may give a NaN.
  */
 size_t laq_cache_attention_workspace_bytes(const laq_cache *cache, int32_t Hq, int32_t dtype, int32_t n, int64_t n_tokens, int32_t max_rows);
 int laq_cache_attention(const laq_cache *cache, int32_t dtype, float scale, int32_t n, int64_t n_tokens, const int32_t *start, const laq_heads *q,

@@ -1,7 +1,7 @@
 """MI355X-native hot path of Lookahead Q-Cache (LAQ) re-eviction (paper Sec. 4.3, Eq. 4).
 
 The work is done by hand-written HIP kernels behind the C ABI declared in
-``include/laq.h``; this package only marshals arguments (``binding``) and knows how
+``include/laq.h``, ``laq_fp4.h`` and ``laq_cache.h``; this package only marshals arguments (``binding``, ``fp4``, ``paged``) and knows how
 to compile the library (``_build``).  There is no CPU fallback: if the shared
 library is missing the first call builds it with hipcc, and raises if that fails.
 """

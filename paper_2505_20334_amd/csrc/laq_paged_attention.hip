@@ -1,11 +1,19 @@
 // Attention over the paged cache of 32, 16 or 8 bits (include/laq_cache.h: laq_cache_attention).
 //
-// A column is a KV head of a request and a tile of its score rows (row r = query head r % G of the group of the request's token r / G).  A workgroup has
-// a range of a column's keys; its waves take 16 * KT keys each in turn, every wave for all rows of the tile, with its own reference m, sum z and sums O
-// (one pass, exponentials of s - m; m moves only when a score is more than 8 above it, so that the usual step has no maximum over lanes).
-// The waves are folded at the end through LDS, the ranges of a column by a second launch, in a fixed order.
+// A column is a KV head of a request and a tile of 16 or 32 of its score rows (row r = query head r % G of the group of the request's token r / G).  The
+// lengths, which the host does not know, are as unequal as requests are, so the keys of all columns are shared out evenly (laq_paged_columns.h): as many
+// workgroups as the device holds, each with one range of a line of turns, which it finds from the lengths and which may end in one column and go on in the next.
+// (A workgroup for a fixed number of rows and a second launch to join them: 128 requests of 1000 to 8192 rows 542 us, 373 so; a second launch takes 4 to 40.)
+// Of a turn the four waves take 16 * KT keys each, every wave for all rows of the tile, with its own reference m, sum z and sums O (one pass, exponentials of s - m;
+// m moves only when a score is more than 8 above it, so that the usual step has no maximum over lanes).  The waves are folded at the end through LDS, the
+// ranges of a column by the workgroup that finds all of them finished, in a fixed order.
 //
-// No LDS on the way of K and V.  Products have the keys as the first operand's rows, so that a lane has four keys of one score row (column n =
+// Bound: memory.  128 requests x 8 heads x 1000 to 8192 rows of d = 128: bf16 2.43 GB in 369 us, 6.6 TB/s; 8 bits 1.22 GB in 208 us, 5.9 TB/s; 96 x 6144 rows of bf16 6.7 TB/s; the
+// vector units are busy 10 % of the time, the matrix cores 4 % (four requests of 32768 to 131071 rows in 8 bits: 28 and 7 %).  Small calls: dependent trips to memory, about 11 us for 520 rows: lengths (2), table (2), keys (1.5), fold (1),
+// sums and marks of the ranges (3).  fp32 caches with more than 16 score rows: the matrix cores' fp32 rate, an eighth of bf16's for these products.
+//
+// No LDS on the way of K and V, and registers for one step: K's are read again as soon as the scores are made, V's as soon as the sums are, so that about a step of a
+// wave is on its way at any time and its code is there once (two steps in turn, twice the registers and the code: four long requests in 8 bits 191 us, so 172).  Products have the keys as the first operand's rows, so that a lane has four keys of one score row (column n =
 // lane % 16, keys 4g .. 4g + 3 of a tile for lane group g = lane / 16), and all that belongs to a score row lies in lanes n, n + 16, n + 32, n + 48:
 //   S^T = K Q^T   a lane reads pieces of one key row, in the order of the operand (the sum over channels may take them in any order, Q the same)
 //   O^T = V^T P^T P^T is where S^T left it: a lane group's keys are, by definition, its part of the keys summed over.  bf16 (16 x 16 x 32): a lane needs
@@ -41,9 +49,10 @@ __device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4* parts) {
     }
 }
 
-// Workgroups that a compute unit holds of a kernel: what their registers leave (the compiler is told to keep to it).
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
+// Workgroups that a compute unit holds of a kernel: what their registers leave (the compiler is told to keep to it), measured with one more or less: bf16, d = 128, 16 score rows, three
+// 383 us against 371 (128 requests); fp32 over fp32, 32 score rows, one 299 against 253 (4 x 256 tokens over 2048); 8 bits, 32 score rows, two 54.7 against 53.7; in parts, two 92 and 121 against 68.
 constexpr int resident(bool f32, int type, int d, int nt) {
   const bool parts = f32 && type != LAQ_F32;
   if (d <= 64) return nt == 1 && !parts ? 3 : 2;
@@ -61,7 +70,7 @@ struct Kinds {
   static constexpr bool LATER = PARTS > 1 && !SCALED;        // infinities of V are added at the end wherever they are
   static constexpr int KT = FLOATS ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
   static constexpr int KN = FLOATS ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
-  // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on
+  // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on (8 bits read 8 bytes a lane: 128 requests 293 us, so 214)
   static constexpr int KW = 16 / (KN * (int)sizeof(E));
   static constexpr __host__ __device__ int k_channel(int i, int g) { return i / KW * (4 * KW * KN) + g * (KW * KN) + i % KW * KN; }
   // blocks of a multiple of a step's keys, so that a step lies in one: one descriptor for its tiles
