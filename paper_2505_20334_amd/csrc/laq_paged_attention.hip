@@ -67,7 +67,8 @@ struct Kinds {
   // fp32: products of fp32 where the cache is, otherwise of bf16, in which the cache's numbers are exact, with queries and weights as sums of three
   static constexpr bool FLOATS = std::is_same<E, float>::value;
   static constexpr int PARTS = F32 && !FLOATS ? 3 : 1;
-  static constexpr bool LATER = PARTS > 1 && !SCALED;        // infinities of V are added at the end wherever they are
+  // the cache has infinities, which the later parts would make NaN of: those of V are added at the end wherever they are, those of K meet the first part alone
+  static constexpr bool LATER = PARTS > 1 && !SCALED;
   static constexpr int KT = FLOATS ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
   static constexpr int KN = FLOATS ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
   // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on (8 bits read 8 bytes a lane: 128 requests 293 us, so 214)
@@ -266,6 +267,34 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
           for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int part = K::PARTS - 1; part >= 0; --part) x[t][kt] = mfma(k, q[t][i][part], x[t][kt]);
+        }
+      }
+    }
+    if constexpr (K::LATER) {
+      // (the later parts of a query are 0 or of either sign, and make a NaN of an infinity of K: what the first part leaves is multiplied with the finite numbers
+      // alone.  Every score that an infinity spoils so is a NaN)
+      bool bad = false;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int kt = 0; kt < K::KT; ++kt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) bad |= x[t][kt][j] != x[t][kt][j];
+      if (__any(bad)) {
+#pragma unroll
+        for (int kt = 0; kt < K::KT; ++kt) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) x[t][kt] = f32x4{};
+#pragma unroll
+          for (int i = 0; i < K::KP; ++i) {
+            if (c.d != D && K::k_channel(i, g) >= c.d) clear(s.k[kt][i]);
+            const u32x4 k = pairs(s.k[kt][i], 1.f);
+            drop_odd(s.k[kt][i]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int part = K::PARTS - 1; part >= 0; --part) x[t][kt] = mfma(part ? pairs(s.k[kt][i], 1.f) : k, q[t][i][part], x[t][kt]);
+          }
         }
       }
     }

@@ -855,3 +855,79 @@ def test_every_code_and_scale_reads_as_its_number():
         torch.cuda.synchronize()
         assert torch.equal(out[:, 0].cpu().double(), want[::br][:n_blocks])
     assert codes_zero.any()
+
+
+def _by_definition(c, out, lse, scale=None):
+    """Case.check for scores that may be infinite or NaN: a key whose score is -infinity has the weight 0, a token that sees a NaN or +infinity is NaN."""
+    scale = scale or 1.0 / math.sqrt(c.d)
+    u, half = 2.0 ** -24, 2.0 ** -8 if c.dtype == BF16 else 2.0 ** -24
+    out, lse = out.cpu().double(), lse.cpu().double()
+    G, first, kinds = c.Hq // c.H, 0, [0, 0, 0]
+    for i, r in enumerate(c.rows):
+        k, v = (x[first:first + r].transpose(0, 1).repeat_interleave(G, 0) for x in (c.k, c.v))
+        first += r
+        for t in range(c.tokens[i]):
+            tok, seen = c.start[i] + t, r - c.tokens[i] + t + 1
+            terms = c.q[tok][:, None] * k[:, :seen] * scale
+            s = terms.sum(-1)
+            for h in range(c.Hq):
+                where = "request %d token %d head %d" % (i, t, h)
+                at = s[h] > -math.inf
+                if s[h].isnan().any() or (s[h] == math.inf).any():
+                    kinds[0] += 1
+                    assert out[tok, h].isnan().all() and not torch.isfinite(lse[tok, h]) and lse[tok, h] != -math.inf, where
+                elif not at.any():
+                    kinds[1] += 1
+                    assert (out[tok, h] == 0).all() and lse[tok, h] == -math.inf, where
+                else:
+                    kinds[2] += 1
+                    p, vv = torch.softmax(s[h, at], 0), v[h, :seen][at]
+                    o, a, A = p @ vv, p @ vv.abs(), terms[h, at].abs().sum(-1).max()
+                    e = 2 * u * (c.d + 16) * A + 2.0 ** -22 + (seen + 64) * u
+                    assert ((out[tok, h] - o).abs() <= (2 * e + half) * a + half * o.abs() + 1e-30).all(), where
+                    l = torch.logsumexp(s[h, at], 0)
+                    assert (lse[tok, h] - l).abs() <= 2 * e + 4 * u * l.abs(), where
+    return kinds
+
+
+ODD = [  # every pair of types, one and two tiles of score rows, each head size, and chunks of prompts: (dtype, cache, Hq, H, d, block, lengths, tokens)
+    (BF16, BF16, 8, 2, 128, 16, [300, 40], [1, 1]), (BF16, BF16, 8, 2, 64, 16, [300, 70], [30, 20]), (BF16, E4M3, 8, 2, 128, 64, [300, 40], [1, 1]), (BF16, E4M3, 8, 2, 192, 16, [200, 40], [9, 1]),
+    (F32, F32, 8, 2, 128, 16, [300, 40], [1, 1]), (F32, F32, 8, 2, 64, 16, [300, 70], [30, 20]), (F32, E4M3, 8, 2, 128, 16, [300, 40], [1, 1]), (F32, E4M3, 8, 2, 64, 64, [300, 70], [30, 20]),
+    (F32, E4M3, 6, 2, 256, 16, [90, 600], [20, 3]), (F32, BF16, 8, 2, 128, 16, [300, 40], [1, 1]), (F32, BF16, 8, 2, 64, 64, [300, 70], [30, 20]), (F32, BF16, 6, 2, 256, 16, [90, 600], [20, 3]),
+    (F32, BF16, 28, 4, 96, 48, [700, 1], [8, 1]), (F32, BF16, 2, 2, 24, 16, [2100], [1]), (BF16, BF16, 32, 32, 128, 16, [300, 100, 70, 90], [40, 50, 60, 90]),
+    (BF16, E4M3, 32, 32, 64, 64, [150, 64, 70, 90], [64, 64, 70, 80]),
+]
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("what", [-math.inf, math.inf, math.nan])
+@pytest.mark.parametrize("dtype,kind,Hq,H,d,br,rows,tokens", ODD)
+def test_infinite_and_nan_keys_have_the_weights_of_their_scores(dtype, kind, Hq, H, d, br, rows, tokens, what, split):
+    print("case:", dtype, kind, Hq, H, d, br, rows, tokens, what, split, flush=True)
+
+    def put(k, v):
+        for j in (3, 17, rows[0] // 2, rows[0] - 1):
+            k[j, 0, d // 2] = what
+        k[rows[0] - 1, 1, 0] = what
+        k[2, 1, d - 1] = -what
+    c = Case(dtype, kind, Hq, H, d, br, rows, tokens, special=put)
+    out, lse = c.run(split=split)
+    torch.cuda.synchronize()
+    kinds = _by_definition(c, out, lse)
+    assert kinds[0] and (kinds[2] or Hq == 2)
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("dtype,kind,Hq,H,d,br,rows,tokens", ODD)
+def test_scores_that_are_all_minus_infinity_give_nothing(dtype, kind, Hq, H, d, br, rows, tokens, split):
+    print("case:", dtype, kind, Hq, H, d, br, rows, tokens, split, flush=True)
+
+    def put(k, v):
+        k[:rows[0], 0, 0] = -math.inf
+    c = Case(dtype, kind, Hq, H, d, br, rows, tokens, special=put)
+    c.q[:, :, 0] = (c.q[:, :, 0].abs() + 0.5).to(dtype).double()
+    c.qd.copy_(c.q.to(dtype))
+    out, lse = c.run(split=split)
+    torch.cuda.synchronize()
+    kinds = _by_definition(c, out, lse)
+    assert kinds[0 if kind == E4M3 else 1] and kinds[2]          # (a row of 8 bits with an infinity stands for NaN)
