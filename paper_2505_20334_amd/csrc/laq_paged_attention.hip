@@ -35,7 +35,9 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 acc) {
 }
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0); }
 
-// Eight floats as sums of three bf16 each, each the nearest of what is left: nothing is (down to 2^-126).
+// Eight floats as sums of three bf16 each, each the nearest of what is left: nothing is (down to 2^-126).  ODD: an infinity or a NaN is its first part, and nothing is left
+// of it (for queries; weights are at most 2^8, or NaN, which may be three).
+template <bool ODD>
 __device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4* parts) {
   float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
@@ -44,8 +46,9 @@ __device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4* parts) {
     for (int i = 0; i < 4; ++i) {
       const uint32_t both = pack2(x[2 * i], x[2 * i + 1]);
       parts[p][i] = both;
-      x[2 * i] -= __uint_as_float(both << 16);
-      x[2 * i + 1] -= __uint_as_float(both & 0xffff0000u);
+      const float first = __uint_as_float(both << 16), second = __uint_as_float(both & 0xffff0000u);
+      x[2 * i] = ODD && p == 0 && first - first != 0.f ? 0.f : x[2 * i] - first;
+      x[2 * i + 1] = ODD && p == 0 && second - second != 0.f ? 0.f : x[2 * i + 1] - second;
     }
 }
 
@@ -152,7 +155,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
         q[t][i][0] = in ? *reinterpret_cast<const u32x4*>(src + at) : u32x4{};
       } else {
         const f32x4 a4 = in ? *reinterpret_cast<const f32x4*>(src + at) : f32x4{}, b4 = in ? *reinterpret_cast<const f32x4*>(src + at + 4) : f32x4{};
-        split(a4, b4, q[t][i]);
+        split<true>(a4, b4, q[t][i]);
       }
     }
   }
@@ -427,7 +430,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
           if constexpr (K::PARTS == 1)
             w[t][0] = u32x4{pack2(x[t][h][0], x[t][h][1]), pack2(x[t][h][2], x[t][h][3]), pack2(x[t][h + 1][0], x[t][h + 1][1]), pack2(x[t][h + 1][2], x[t][h + 1][3])};
           else
-            split(x[t][h], x[t][h + 1], w[t]);
+            split<false>(x[t][h], x[t][h + 1], w[t]);
         }
 #pragma unroll
         for (int i = 0; i < K::VP; ++i) {

@@ -931,3 +931,21 @@ def test_scores_that_are_all_minus_infinity_give_nothing(dtype, kind, Hq, H, d, 
     torch.cuda.synchronize()
     kinds = _by_definition(c, out, lse)
     assert kinds[0 if kind == E4M3 else 1] and kinds[2]          # (a row of 8 bits with an infinity stands for NaN)
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("what", [-math.inf, math.inf, math.nan])
+@pytest.mark.parametrize("dtype,kind,Hq,H,d,br,rows,tokens", ODD)
+def test_infinite_and_nan_queries_have_the_weights_of_their_scores(dtype, kind, Hq, H, d, br, rows, tokens, what, split):
+    print("case:", dtype, kind, Hq, H, d, br, rows, tokens, what, split, flush=True)
+
+    def put(k, v):
+        k[:, 0, 5] = -k[:, 0, 5].abs() - 0.5           # (one sign: all scores of a query with an infinity there are infinities of one sign)
+    c = Case(dtype, kind, Hq, H, d, br, rows, tokens, special=put)
+    for tok in (0, len(c.q) - 1):
+        c.q[tok, 0, 5] = c.q[tok, Hq - 1, d - 2] = what
+    c.qd.copy_(c.q.to(dtype))
+    out, lse = c.run(split=split)
+    torch.cuda.synchronize()
+    kinds = _by_definition(c, out, lse)
+    assert kinds[1 if what == math.inf else 0] and (kinds[2] or Hq == 2)
