@@ -35,20 +35,30 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 acc) {
 }
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0); }
 
-// Eight floats as sums of three bf16 each, each the nearest of what is left: nothing is (down to 2^-126).  ODD: an infinity or a NaN is its first part, and nothing is left
-// of it (for queries; weights are at most 2^8, or NaN, which may be three).
+// Eight floats as sums of three bf16 each, each the nearest of what is left: nothing is (down to 2^-126).  ODD, for queries: the first part of a number beyond bf16's largest is
+// that one, an infinity or a NaN is its first part, and nothing is left of it (weights are at most 2^8, or NaN, whose parts may be three).
 template <bool ODD>
 __device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4* parts) {
-  float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  constexpr float MOST = 0x1.fep127f;
+  float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}, first[8];
+  bool is[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    is[i] = !ODD || __builtin_fabsf(x[i]) < __builtin_inff();
+    first[i] = ODD && is[i] ? __builtin_amdgcn_fmed3f(x[i], -MOST, MOST) : x[i];
+  }
 #pragma unroll
   for (int p = 0; p < 3; ++p)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t both = pack2(x[2 * i], x[2 * i + 1]);
+      const uint32_t both = p == 0 ? pack2(first[2 * i], first[2 * i + 1]) : pack2(x[2 * i], x[2 * i + 1]);
       parts[p][i] = both;
-      const float first = __uint_as_float(both << 16), second = __uint_as_float(both & 0xffff0000u);
-      x[2 * i] = ODD && p == 0 && first - first != 0.f ? 0.f : x[2 * i] - first;
-      x[2 * i + 1] = ODD && p == 0 && second - second != 0.f ? 0.f : x[2 * i + 1] - second;
+      x[2 * i] -= __uint_as_float(both << 16);
+      x[2 * i + 1] -= __uint_as_float(both & 0xffff0000u);
+      if (ODD && p == 0) {
+        x[2 * i] = is[2 * i] ? x[2 * i] : 0.f;
+        x[2 * i + 1] = is[2 * i + 1] ? x[2 * i + 1] : 0.f;
+      }
     }
 }
 

@@ -949,3 +949,19 @@ def test_infinite_and_nan_queries_have_the_weights_of_their_scores(dtype, kind, 
     torch.cuda.synchronize()
     kinds = _by_definition(c, out, lse)
     assert kinds[1 if what == math.inf else 0] and (kinds[2] or Hq == 2)
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("kind,Hq,H,d,br,rows,tokens", [x[1:] for x in ODD if x[0] == F32])
+def test_queries_beyond_the_largest_number_of_bf16(kind, Hq, H, d, br, rows, tokens, split):
+    print("case:", kind, Hq, H, d, br, rows, tokens, split, flush=True)
+
+    def put(k, v):
+        k *= 2.0 ** -100
+    c = Case(F32, kind, Hq, H, d, br, rows, tokens, special=put)
+    c.q[:, :, 3] = torch.tensor([3.4e38, -3.4028e38]).repeat(Hq // 2).double()
+    c.q[0, 0, 3] = torch.finfo(F32).max
+    c.qd.copy_(c.q.to(F32))
+    c.q = c.q.float().double()
+    scale = 2.0 ** -26                                 # (scores of about 2^28)
+    c.check(*c.run(split=split, scale=scale), scale=scale)
