@@ -87,14 +87,14 @@ struct AttPlan {
 // The ranges of columns that several workgroups share.  A workgroup has two places: 2w for a column that began in another workgroup's share, 2w + 1 for one
 // that begins in its own and goes on; a place has mz[tile] (m and z), sums[tile][d] and a mark.  A workgroup that is done with a range writes the launch's nonce
 // there, after its sums have arrived, and then looks at the marks of all ranges of the column: who finds all of them joins the ranges, in their order, and
-// clears the marks, so that a replayed launch, whose nonce is the same, finds none of its own; whatever else lies in the workspace is no mark.  Two may find all
-// of them (both write the same); one that comes to look when another has begun to clear finds that it is not needed.  (Counting in by compare and swap: 64
-// workgroups of a column take turns, one request of 32768 rows x 8 heads 61 us.)
+// clears the marks, so that a replayed launch, whose nonce is the same, finds none of its own.  The workspace comes as the allocator left it: one of its words passes for a
+// launch's mark once in 2^64 (laq_marks.h).  Two may find all of them (both write the same); one that comes to look when another has begun to clear finds that it is not
+// needed.  (Counting in by compare and swap: 64 workgroups of a column take turns, one request of 32768 rows x 8 heads 61 us.)
 struct Partials {
   unsigned long long* marks;
   float2* mz;
   float* sums;
-  uint32_t nonce;
+  unsigned long long nonce;
 };
 
 // chunks of a prompt: whether that kernel takes a call, and the call

@@ -20,9 +20,7 @@
 //                 eight keys of one channel; it reads eight channels of its eight keys, and a permutation of 8 x 8 numbers in registers, two a
 //                 instruction, makes the operands of eight products.  fp32 (16 x 16 x 4): one key a lane, so the pieces are operands as they are
 // A lane's pieces of V are VN channels: its product row m of product e of piece h is channel (16 h + m) VN + e.
-#include <atomic>
-#include <chrono>
-
+#include "laq_marks.h"
 #include "laq_paged_columns.h"
 
 namespace laq {
@@ -615,13 +613,12 @@ bool paged_attention_fits(const PagedView& c, int dtype, const PagedAttention& a
 
 hipError_t launch_paged_attention(const PagedView& c, int dtype, const PagedAttention& a, void* ws, hipStream_t st) {
   if (paged_prompt_call(c, a.Hq, dtype, a.n, a.n_tokens)) return launch_paged_prompt(c, a, st);
-  static std::atomic<uint32_t> launches{(uint32_t)(std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull >> 32)};
+  static MarkNumbers numbers;
   const AttPlan p = plan_of(c, a.Hq, dtype, a.n, a.n_tokens, a.start != nullptr, a.max_rows, ws != nullptr);
   const Bytes b = bytes_of(c, p);
   char* const at = static_cast<char*>(ws);
   Partials part{reinterpret_cast<unsigned long long*>(at), reinterpret_cast<float2*>(at + b.marks), reinterpret_cast<float*>(at + b.marks + b.mz), 0};
-  if (ws)
-    do part.nonce = launches.fetch_add(1); while (part.nonce == 0);          // 0 is a mark that was cleared
+  if (ws) part.nonce = numbers.next();
   if (dtype == LAQ_BF16)
     return c.type == LAQ_BF16 ? by_size<uint16_t, uint16_t>(c, a, p, part, st) : by_size<uint16_t, E4m3>(c, a, p, part, st);
   switch (c.type) {

@@ -331,7 +331,7 @@ __device__ __forceinline__ void join_ranges(const PagedView& c, const PagedAtten
   const auto place_of = [&](int k) { return 2 * (first + k) + (k == 0); };
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (what this wave stored has arrived)
   __syncthreads();
-  if (threadIdx.x == 0) __hip_atomic_store(part.marks + s.place(), (unsigned long long)part.nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (threadIdx.x == 0) __hip_atomic_store(part.marks + s.place(), part.nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   bool all = true;
