@@ -3,6 +3,7 @@
 
 #include <type_traits>
 
+#include "laq_find.h"
 #include "laq_paged.h"
 
 namespace laq {
@@ -45,16 +46,13 @@ __device__ __forceinline__ int64_t first_column(const PagedAttention& a, int G, 
 // The last request that begins at column `slot` or before it: 64 looked at at a time.
 __device__ __forceinline__ int find_request(const PagedAttention& a, int G, int tile, int slot) {
   if (!a.start) return min(slot / ((G + tile - 1) / tile), a.n - 1);
-  int lo = 0, n = a.n;
+  Find f{0, a.n};
   const int lane = threadIdx.x & 63;
-  while (n > 1) {
-    const int step = (n + 63) / 64, i = lo + lane * step;
-    const bool before = lane * step < n && first_column(a, G, tile, i) <= slot;
-    const int at = max(__popcll(__ballot(before)) - 1, 0) * step;
-    lo += at;
-    n = max(min(step, n - at), 1);
+  while (f.n > 1) {
+    const bool before = f.looks(lane) && first_column(a, G, tile, f.lo + lane * f.step()) <= slot;
+    f.narrow((int)__popcll(__ballot(before)));
   }
-  return __builtin_amdgcn_readfirstlane(min(lo, a.n - 1));
+  return uniform(f.lo);
 }
 
 // What a column is: a tile of score rows of a request.

@@ -965,3 +965,21 @@ def test_queries_beyond_the_largest_number_of_bf16(kind, Hq, H, d, br, rows, tok
     c.q = c.q.float().double()
     scale = 2.0 ** -26                                 # (scores of about 2^28)
     c.check(*c.run(split=split, scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("dtype,kind,Hq,H,d,n,each", [(BF16, BF16, 8, 2, 64, 3, 3), (F32, E4M3, 8, 2, 128, 3, 9), (BF16, E4M3, 8, 1, 192, 80, 2), (BF16, BF16, 32, 32, 128, 4, 35), (BF16, E4M3, 32, 32, 64, 4, 64),
+                                                      (BF16, BF16, 4, 2, 72, 70, 18)])
+def test_starts_that_make_no_sense_leave_everything_around_the_output_alone(dtype, kind, Hq, H, d, n, each):
+    print("case:", dtype, kind, Hq, H, d, n, each, flush=True)
+    c = Case(dtype, kind, Hq, H, d, 16, [each + i * 13 % 90 for i in range(n)], [each] * n)
+    T, big = n * each, (1 << 31) - 1
+    assert (_laq().laq_cache_attention_workspace_bytes(c.cache, Hq, dtype, n, T, 100) == 0) == (each in (35, 64, 18))      # (both kernels)
+    for start in ([0, T, 0, T], [T, 0], [-5, T // 2, T // 2 + 1, 100 * T], [big], [0], [-big, big], [0, T + 1], [T - 1, T, big, -big, T - 2], [T // 2, T // 3, T // 4, T], [0, T] + [T] * (n - 1)):
+        values = (start * (n + 1))[:n + 1]
+        c.start_d = torch.tensor(values, dtype=torch.int32, device=DEV)
+        for split in (True, False):
+            bounds, lse = torch.full((T + 60, Hq, d), 5.0, dtype=dtype, device=DEV), torch.full((T + 64, Hq), 5.0, device=DEV)
+            c.run(out=bounds[30:30 + T], lse=lse[32:32 + T], split=split)
+            torch.cuda.synchronize()
+            assert (bounds[:30] == 5.0).all() and (bounds[30 + T:] == 5.0).all() and (lse[:32] == 5.0).all() and (lse[32 + T:] == 5.0).all(), (start, split)
+    assert (bounds[30:30 + T] != 5.0).any()            # (the last one: request 0 has all tokens)
