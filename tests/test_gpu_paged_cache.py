@@ -983,3 +983,21 @@ def test_starts_that_make_no_sense_leave_everything_around_the_output_alone(dtyp
             torch.cuda.synchronize()
             assert (bounds[:30] == 5.0).all() and (bounds[30 + T:] == 5.0).all() and (lse[:32] == 5.0).all() and (lse[32 + T:] == 5.0).all(), (start, split)
     assert (bounds[30:30 + T] != 5.0).any()            # (the last one: request 0 has all tokens)
+
+
+CHUNKS = [  # more calls that the kernel of whole prompts takes, each token compared: (cache, Hq, H, d, block, lengths, tokens)
+    # numbers of score rows of a group that are no power of two, more than four tiles of a request on average, head sizes that are rounded up
+    (BF16, 56, 8, 128, 256, [513], [513]), (E4M3, 112, 16, 128, 16, [430, 64], [150, 64]), (BF16, 112, 16, 80, 64, [300, 150], [150, 130]),
+    (E4M3, 32, 32, 80, 16, [200, 130, 50, 90], [130, 129, 60, 0]), (BF16, 32, 32, 80, 32, [200, 130, 50, 90], [130, 129, 50, 1]),
+    # columns in the order of lengths: 256 / H of a KV head to a round, the second round backwards.  More than one round, more than two, none whole; no room for one
+    (BF16, 64, 32, 64, 16, [700, 200, 90, 300], [300, 200, 90, 64]), (BF16, 64, 64, 32, 64, [900, 300, 500], [300, 129, 40]), (E4M3, 64, 64, 24, 16, [150, 300, 600, 600, 5], [140, 300, 520, 129, 5]),
+    (BF16, 64, 64, 72, 16, [520, 150, 150, 600], [520, 150, 150, 129]), (BF16, 260, 260, 16, 16, [300, 41], [140, 40]), (E4M3, 128, 128, 72, 64, [131, 300, 70], [131, 257, 1]),
+]
+
+
+@pytest.mark.parametrize("kind,Hq,H,d,br,rows,tokens", CHUNKS)
+def test_chunks_in_any_order_of_lengths(kind, Hq, H, d, br, rows, tokens):
+    print("case:", kind, Hq, H, d, br, rows, tokens, flush=True)
+    c = Case(BF16, kind, Hq, H, d, br, rows, tokens, token_major=br == 64, fused=br == 32)
+    assert _laq().laq_cache_attention_workspace_bytes(c.cache, Hq, BF16, len(rows), sum(tokens), max(rows)) == 0      # (that kernel shares nothing out)
+    c.check(*c.run())
