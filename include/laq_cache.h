@@ -148,8 +148,8 @@ int laq_cache_load(const laq_cache *cache, int32_t dtype, int64_t n_tokens, cons
  *                 16-byte aligned.  With and without it the last bits of `out` may differ
  * A call that needs more than 2^24 workgroups is LAQ_ERR_UNSUPPORTED.  What the rows behind r, other blocks of the pool and rows that a token does
  * not see hold (infinities and NaN too) does not reach out or lse.
- * bf16: the products of q and K are exact, sums, maxima and weights are fp32, weights are rounded to bf16 for the product with V, out
- * is rounded once.  fp32: products and sums in fp32; over caches of bf16 and 8 bits, which are exact in bf16, as bf16 products of queries and weights that are
+ * bf16: the products of q and K are exact, sums, maxima and weights are fp32; for the product with V a weight is the sum of two bf16 (2^-16), in chunks of a prompt, and over
+ * 8 bits where requests have more than 16 score rows on average, one (2^-8); out is rounded once.  fp32: products and sums in fp32; over caches of bf16 and 8 bits, which are exact in bf16, as bf16 products of queries and weights that are
  * the sums of three bf16 (2^-24; parts below 2^-126 count as 0).  Weights are up to 2^8 before they are divided by their sum: sums over
  * numbers of V beyond 2^88 may overflow.  Visible scores that are all -infinity give 0 and an lse of -infinity.  An infinity in V that is seen with a weight so small that fp32
  * has 0 for it may give a NaN.

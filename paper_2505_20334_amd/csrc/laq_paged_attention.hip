@@ -33,9 +33,9 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 acc) {
 }
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 acc) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0); }
 
-// Eight floats as sums of three bf16 each, each the nearest of what is left: nothing is (down to 2^-126).  ODD, for queries: the first part of a number beyond bf16's largest is
-// that one, an infinity or a NaN is its first part, and nothing is left of it (weights are at most 2^8, or NaN, whose parts may be three).
-template <bool ODD>
+// Eight floats as sums of N bf16 each, each the nearest of what is left: of three nothing is (down to 2^-126).  ODD, for queries: the first part of a number beyond bf16's largest
+// is that one, an infinity or a NaN is its first part, and nothing is left of it (weights are at most 2^8, or NaN, whose parts may all be).
+template <int N, bool ODD>
 __device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4* parts) {
   constexpr float MOST = 0x1.fep127f;
   float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}, first[8];
@@ -46,7 +46,7 @@ __device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4* parts) {
     first[i] = ODD && is[i] ? __builtin_amdgcn_fmed3f(x[i], -MOST, MOST) : x[i];
   }
 #pragma unroll
-  for (int p = 0; p < 3; ++p)
+  for (int p = 0; p < N; ++p)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t both = p == 0 ? pack2(first[2 * i], first[2 * i + 1]) : pack2(x[2 * i], x[2 * i + 1]);
@@ -78,8 +78,12 @@ struct Kinds {
   // fp32: products of fp32 where the cache is, otherwise of bf16, in which the cache's numbers are exact, with queries and weights as sums of three
   static constexpr bool FLOATS = std::is_same<E, float>::value;
   static constexpr int PARTS = F32 && !FLOATS ? 3 : 1;
+  // Parts of a weight for the product with V.  Of bf16 queries two, which leave 2^-16 of it: results are away from exact ones by no more than their own rounding, 0.0017 of themselves
+  // (one part: 0.0018 to 0.0023).  Memory's time hides the second products: 128 requests 371 us, in 8 bits 207, 520 rows 12, 32 x 8 tokens 61, each +-1 % (two of 8192 rows, 256
+  // tokens 166 -> 173); but not where 8 bits are converted for two tiles of score rows (32 x 8 tokens 50 -> 53): one there
+  static constexpr int WEIGHTS = FLOATS ? 1 : F32 ? 3 : SCALED && NT == 2 ? 1 : 2;
   // the cache has infinities, which the later parts would make NaN of: those of V are added at the end wherever they are, those of K meet the first part alone
-  static constexpr bool LATER = PARTS > 1 && !SCALED;
+  static constexpr bool LATER_K = PARTS > 1 && !SCALED, LATER_V = WEIGHTS > 1 && !SCALED;
   static constexpr int KT = FLOATS ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
   static constexpr int KN = FLOATS ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
   // A read of K is 16 bytes, KW pieces side by side: piece i of lane group g has the numbers from here on (8 bits read 8 bytes a lane: 128 requests 293 us, so 214)
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
         q[t][i][0] = in ? *reinterpret_cast<const u32x4*>(src + at) : u32x4{};
       } else {
         const f32x4 a4 = in ? *reinterpret_cast<const f32x4*>(src + at) : f32x4{}, b4 = in ? *reinterpret_cast<const f32x4*>(src + at + 4) : f32x4{};
-        split<true>(a4, b4, q[t][i]);
+        split<K::PARTS, true>(a4, b4, q[t][i]);
       }
     }
   }
@@ -281,7 +285,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
         }
       }
     }
-    if constexpr (K::LATER) {
+    if constexpr (K::LATER_K) {
       // (the later parts of a query are 0 or of either sign, and make a NaN of an infinity of K: what the first part leaves is multiplied with the finite numbers
       // alone.  Every score that an infinity spoils so is a NaN)
       bool bad = false;
@@ -393,7 +397,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
           }
         }
     }
-    if constexpr (K::LATER) {
+    if constexpr (K::LATER_V) {
       // (the later parts of a weight are 0 or negative, and make a NaN of an infinity)
       u16x2 most{};
 #pragma unroll
@@ -432,14 +436,10 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
     } else {
 #pragma unroll
       for (int h = 0; h < K::KT; h += 2) {
-        u32x4 w[NT][K::PARTS];
+        u32x4 w[NT][K::WEIGHTS];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          if constexpr (K::PARTS == 1)
-            w[t][0] = u32x4{pack2(x[t][h][0], x[t][h][1]), pack2(x[t][h][2], x[t][h][3]), pack2(x[t][h + 1][0], x[t][h + 1][1]), pack2(x[t][h + 1][2], x[t][h + 1][3])};
-          else
-            split<false>(x[t][h], x[t][h + 1], w[t]);
-        }
+        for (int t = 0; t < NT; ++t)
+          split<K::WEIGHTS, false>(x[t][h], x[t][h + 1], w[t]);
 #pragma unroll
         for (int i = 0; i < K::VP; ++i) {
           // [key][channel pair] to [channel][key pair]
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int part = K::PARTS - 1; part >= 0; --part) o[t][i * K::VN + e] = mfma(f, w[t][part], o[t][i * K::VN + e]);
+              for (int part = K::WEIGHTS - 1; part >= 0; --part) o[t][i * K::VN + e] = mfma(f, w[t][part], o[t][i * K::VN + e]);
           }
         }
       }
@@ -510,7 +510,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
       }
       if (any_odd) {
         const int upto = min(to - 1, col.last(r, G));
-        for (int key = K::LATER ? from : max(from, first_last + 1); key <= upto; ++key) {
+        for (int key = K::LATER_V ? from : max(from, first_last + 1); key <= upto; ++key) {
           const int page = (int)((uint32_t)key / (uint32_t)c.block_rows), off = key - page * c.block_rows, block = table[page];
           if (block < 0 || block >= c.n_blocks) continue;
           const E* v = vx + block * c.block + (int64_t)off * c.row;

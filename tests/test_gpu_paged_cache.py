@@ -1001,3 +1001,30 @@ def test_chunks_in_any_order_of_lengths(kind, Hq, H, d, br, rows, tokens):
     c = Case(BF16, kind, Hq, H, d, br, rows, tokens, token_major=br == 64, fused=br == 32)
     assert _laq().laq_cache_attention_workspace_bytes(c.cache, Hq, BF16, len(rows), sum(tokens), max(rows)) == 0      # (that kernel shares nothing out)
     c.check(*c.run())
+
+
+EXACT = [  # the calls of bf16 whose weights keep more than bf16's bits: (cache, Hq, H, d, block, lengths, tokens)
+    (BF16, 32, 8, 128, 64, [520], [1]), (BF16, 8, 8, 64, 16, [1, 2, 15, 16, 17, 31, 33, 64, 65, 700], [1] * 10), (BF16, 8, 2, 256, 64, [63, 1000], [1, 1]), (BF16, 28, 4, 96, 48, [3000, 700], [1, 1]),
+    (E4M3, 32, 8, 128, 64, [520, 2100], [1, 1]), (E4M3, 16, 2, 192, 16, [95, 0, 600], [1, 1, 1]), (E4M3, 8, 2, 64, 48, [900, 40], [4, 4]), (BF16, 8, 2, 128, 64, [600, 9, 40, 8], [8, 8, 1, 8]),
+    (BF16, 8, 2, 64, 16, [2000], [20]),
+]
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("kind,Hq,H,d,br,rows,tokens", EXACT)
+def test_the_output_is_what_is_rounded_to_bf16(kind, Hq, H, d, br, rows, tokens, split):
+    """Case.check's bounds, but for the weights: two parts of bf16, each rounded by 2^-8 at most, leave 2^-16 of a weight, and the result is rounded once."""
+    print("case:", kind, Hq, H, d, br, rows, tokens, split, flush=True)
+    c = Case(BF16, kind, Hq, H, d, br, rows, tokens)
+    out, _ = c.run(split=split)
+    out, u, first = out.cpu().double(), 2.0 ** -24, 0
+    for i, r in enumerate(rows):
+        k, v = (x[first:first + r].transpose(0, 1).contiguous() for x in (c.k, c.v))
+        first += r
+        for t in range(tokens[i]):
+            seen = r - tokens[i] + t + 1
+            o, _, a, A = fp4_plain.attention(c.q[c.start[i] + t], k, v, seen, 1.0 / math.sqrt(d))
+            e = (2 * u * (d + 16) * A + 2.0 ** -22 + (seen + 64) * u)[:, None] if seen > 0 else 0.0
+            tol = (2 * e + 2.0 ** -16) * a * (1 + 2.0 ** -8) + 2.0 ** -8 * o.abs() + 1e-30
+            off = (out[c.start[i] + t] - o).abs()
+            assert (off <= tol).all(), "request %d token %d: %d of %d off" % (i, t, int((off > tol).sum()), off.numel())
