@@ -269,7 +269,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
 #pragma unroll
       for (int i = 0; i < K::KP; ++i) {
         if constexpr (K::FLOATS) {
-          f32x4 k = floats(s.k[kt][i], 0, ks);
+          f32x4 k = floats(s.k[kt][i]);
           if (c.d != D && K::k_channel(i, g) >= c.d) k = f32x4{};
 #pragma unroll
           for (int t = 0; t < NT; ++t)
@@ -424,14 +424,11 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < K::VP; ++i) {
+          const f32x4 v = floats(s.v[0][j][i]);
 #pragma unroll
-          for (int h = 0; h < K::VN; h += 4) {
-            const f32x4 v = floats(s.v[0][j][i], h / 4, K::SCALED ? scale_of_v(s, 0, j) : 1.f);
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int t = 0; t < NT; ++t) o[t][i * K::VN + h + e] = mfma(v[e], x[t][0][j], o[t][i * K::VN + h + e]);
-          }
+            for (int t = 0; t < NT; ++t) o[t][i * K::VN + e] = mfma(v[e], x[t][0][j], o[t][i * K::VN + e]);
         }
     } else {
 #pragma unroll
@@ -531,7 +528,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
     }
   }
   if (!p.shares) return;
-  if (cut) join_ranges<Q, ATT_THREADS, NT == 1 ? 8 : 4, 1>(c, a, part, sh, col, G, p.tile, turns, &sums[0][0][0]);
+  if (cut) join_ranges<Q, ATT_THREADS, NT == 1 ? 8 : 4>(c, a, part, sh, col, G, p.tile, turns, &sums[0][0][0]);
   if (!next_column<TURN>(c, a, G, p.tile, turns, turns_here, sh)) return;
   __syncthreads();                                           // (the LDS is free)
   }

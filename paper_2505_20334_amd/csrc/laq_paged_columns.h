@@ -89,17 +89,8 @@ __device__ __forceinline__ u32x4 pairs(const Raw<E4m3, 8>& r, float s) {
   return u32x4{pair_of(r.x[0], s, false), pair_of(r.x[0], s, true), pair_of(r.x[1], s, false), pair_of(r.x[1], s, true)};
 }
 __device__ __forceinline__ u32x2 pairs(const Raw<E4m3, 4>& r, float s) { return u32x2{pair_of(r.x, s, false), pair_of(r.x, s, true)}; }
-// As fp32: numbers 4 part and on.
-__device__ __forceinline__ f32x4 floats(const Raw<float, 4>& r, int, float) { return __builtin_bit_cast(f32x4, r.x); }
-__device__ __forceinline__ f32x4 floats(const Raw<uint16_t, 4>& r, int, float) {
-  return __builtin_bit_cast(f32x4, (u32x4{r.x[0] << 16, r.x[0] & 0xffff0000u, r.x[1] << 16, r.x[1] & 0xffff0000u}));
-}
-__device__ __forceinline__ f32x4 floats(const Raw<uint16_t, 8>& r, int part, float) { return floats(Raw<uint16_t, 4>{u32x2{r.x[2 * part], r.x[2 * part + 1]}}, 0, 0.f); }
-__device__ __forceinline__ f32x4 floats(const Raw<E4m3, 4>& r, int, float s) {
-  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(r.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(r.x, true);
-  return f32x4{a[0] * s, a[1] * s, b[0] * s, b[1] * s};
-}
-__device__ __forceinline__ f32x4 floats(const Raw<E4m3, 8>& r, int part, float s) { return floats(Raw<E4m3, 4>{r.x[part]}, 0, s); }
+// As fp32.
+__device__ __forceinline__ f32x4 floats(const Raw<float, 4>& r) { return __builtin_bit_cast(f32x4, r.x); }
 
 // Infinities and NaN among numbers of V.
 template <typename E, int N>
@@ -320,9 +311,8 @@ __device__ __forceinline__ bool next_column(const PagedView& c, const PagedAtten
   return true;
 }
 
-// The workgroup has stored its range of a column: joins the ranges if it finds that all of them are there.  U ranges of I pieces of four channels are asked for at
-// a time; lds: room for THREADS * 6 numbers.
-template <typename Q, int THREADS, int U, int I>
+// The workgroup has stored its range of a column: joins the ranges if it finds that all of them are there.  U ranges are asked for at a time; lds: room for THREADS * 6 numbers.
+template <typename Q, int THREADS, int U>
 __device__ __forceinline__ void join_ranges(const PagedView& c, const PagedAttention& a, const Partials& part, const Share& s, const Column& col, int G, int tile, int turns,
                                             float* lds) {
   const int first = s.share_of(s.begin), count = s.share_of(s.begin + turns - 1) - first + 1;
@@ -340,51 +330,34 @@ __device__ __forceinline__ void join_ranges(const PagedView& c, const PagedAtten
   // four channels of a row a thread, and as many groups of ranges as there are threads for
   const int per = c.d / 4, items = col.rows * per, groups = max(1, min(count, THREADS / items));
   f32x2* const lds_mz = reinterpret_cast<f32x2*>(lds + 4 * THREADS);
-  for (int i0 = 0; i0 < items; i0 += groups > 1 ? items : THREADS * I) {
-    const int grp = groups > 1 ? threadIdx.x / items : 0, item0 = groups > 1 ? threadIdx.x % items : i0 + threadIdx.x;
-    float top[I], z[I];
-    f32x4 y[I];
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-      top[i] = MINUS_INF;
-      z[i] = 0.f;
-      y[i] = f32x4{};
-    }
-    if (item0 < items && grp < groups) {
+  for (int i0 = 0; i0 < items; i0 += groups > 1 ? items : THREADS) {
+    const int grp = groups > 1 ? threadIdx.x / items : 0, item = groups > 1 ? threadIdx.x % items : i0 + threadIdx.x;
+    const int r = item / per, at = (item - r * per) * 4;
+    float top = MINUS_INF, z = 0.f;
+    f32x4 y{};
+    if (item < items && grp < groups) {
       for (int k = grp; k < count; k += U * groups) {
-        f32x2 mz[I][U], s0[I][U], s1[I][U];
+        f32x2 mz[U], s0[U], s1[U];
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
-          const int item = min(item0 + i * THREADS, items - 1), r = item / per, at = (item - r * per) * 4;
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int64_t row = (int64_t)place_of(min(k + u * groups, count - 1)) * tile + r;
-            mz[i][u] = load_pair(part.mz + row);
-            s0[i][u] = load_pair(part.sums + row * c.d + at);
-            s1[i][u] = load_pair(part.sums + row * c.d + at + 2);
-          }
+        for (int u = 0; u < U; ++u) {
+          const int64_t row = (int64_t)place_of(min(k + u * groups, count - 1)) * tile + r;
+          mz[u] = load_pair(part.mz + row);
+          s0[u] = load_pair(part.sums + row * c.d + at);
+          s1[u] = load_pair(part.sums + row * c.d + at + 2);
         }
 #pragma unroll
-        for (int i = 0; i < I; ++i)
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (k + u * groups < count) join(top[i], z[i], y[i], mz[i][u][0], mz[i][u][1], f32x4{s0[i][u][0], s0[i][u][1], s1[i][u][0], s1[i][u][1]}, a.scale2);
+        for (int u = 0; u < U; ++u)
+          if (k + u * groups < count) join(top, z, y, mz[u][0], mz[u][1], f32x4{s0[u][0], s0[u][1], s1[u][0], s1[u][1]}, a.scale2);
       }
     }
     if (groups > 1) {
-      *reinterpret_cast<f32x4*>(lds + 4 * threadIdx.x) = y[0];
-      lds_mz[threadIdx.x] = f32x2{top[0], z[0]};
+      *reinterpret_cast<f32x4*>(lds + 4 * threadIdx.x) = y;
+      lds_mz[threadIdx.x] = f32x2{top, z};
       __syncthreads();
-      for (int k = 1; item0 < items && grp == 0 && k < groups; ++k)
-        join(top[0], z[0], y[0], lds_mz[k * items + item0][0], lds_mz[k * items + item0][1], *reinterpret_cast<const f32x4*>(lds + 4 * (k * items + item0)), a.scale2);
+      for (int k = 1; item < items && grp == 0 && k < groups; ++k)
+        join(top, z, y, lds_mz[k * items + item][0], lds_mz[k * items + item][1], *reinterpret_cast<const f32x4*>(lds + 4 * (k * items + item)), a.scale2);
     }
-    if (grp == 0) {
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        const int item = item0 + i * THREADS, r = item / per;
-        if (item < items && (i == 0 || groups == 1)) put_out<Q>(c, a, col, s.head, G, r, (item - r * per) * 4, top[i], z[i], y[i]);
-      }
-    }
+    if (grp == 0 && item < items) put_out<Q>(c, a, col, s.head, G, r, at, top, z, y);
   }
 }
 
