@@ -1028,3 +1028,75 @@ def test_the_output_is_what_is_rounded_to_bf16(kind, Hq, H, d, br, rows, tokens,
             tol = (2 * e + 2.0 ** -16) * a * (1 + 2.0 ** -8) + 2.0 ** -8 * o.abs() + 1e-30
             off = (out[c.start[i] + t] - o).abs()
             assert (off <= tol).all(), "request %d token %d: %d of %d off" % (i, t, int((off > tol).sum()), off.numel())
+
+
+@pytest.mark.parametrize("dtype,kind,T,Hq,H,d,rot,layout", [
+    (BF16, BF16, 513, 8, 2, 128, 128, "half"), (F32, E4M3, 2049, 5, 1, 72, 20, "half"), (BF16, E4M3, 5003, 3, 2, 256, 66, "half"), (F32, BF16, 8193, 4, 4, 64, 64, "interleaved"),
+    (BF16, F32, 8195, 2, 1, 192, 192, "half"), (BF16, E4M3, 16381, 32, 8, 128, 128, "half"), (F32, F32, 16381, 28, 4, 96, 40, "half"), (F32, E4M3, 16381, 28, 4, 96, 48, "interleaved")])
+def test_long_batches_have_the_bits_of_short_ones(dtype, kind, T, Hq, H, d, rot, layout):
+    """Rotated, appended and read back in one call each and 500 tokens at a time, which other shapes of the launch do; the largest go past the caches."""
+    laq = _laq()
+    print("case:", dtype, kind, T, Hq, H, d, rot, layout, flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(T + d)
+    qkv = torch.randn(T, Hq + 2 * H, d, generator=gen, device=DEV).to(dtype)
+    q, k, v = qkv.split((Hq, H, H), 1)
+    positions = torch.randint(-1000, 1 << 20, (T,), generator=gen, device=DEV).int()
+    n_blocks = -(-T // 32) + 2
+    slots = torch.randperm(n_blocks * 32, generator=gen, device=DEV)[:T].int()
+    slots[7::101] = -1
+    rope = laq.Rope(laq.laq_rope_frequencies(rot, device=DEV), layout, 1.1)
+    at_once, in_parts = _pool(n_blocks, H, 32, d, kind), _pool(n_blocks, H, 32, d, kind)
+    got = laq.laq_cache_append(at_once, k, v, slots, q=q, positions=positions, rope=rope)
+    got_q, got_k = laq.laq_rope(q, k, positions, rope)
+    loaded = laq.laq_cache_load(at_once, slots, dtype)
+    for t in range(0, T, 500):
+        s = slice(t, t + 500)
+        want = laq.laq_cache_append(in_parts, k[s], v[s], slots[s], q=q[s], positions=positions[s], rope=rope)
+        want_q, want_k = laq.laq_rope(q[s], k[s], positions[s], rope)
+        assert torch.equal(got[s], want) and torch.equal(got_q[s], want) and torch.equal(got_q[s], want_q) and torch.equal(got_k[s], want_k), t
+        assert all(torch.equal(x[s], y) for x, y in zip(loaded, laq.laq_cache_load(at_once, slots[s], dtype))), t
+    for x, y in zip(at_once, in_parts):
+        assert x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    # in place
+    both = laq.laq_rope(q, k, positions, rope, q_out=q, k_out=k)
+    torch.cuda.synchronize()
+    assert torch.equal(both[0], got_q) and torch.equal(both[1], got_k)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, E4M3])
+def test_many_compacted_rows_have_the_bits_of_appended_ones(kind):
+    """128 MiB of rows, which are read past the caches."""
+    laq = _laq()
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    n, H, d, L, budgets, br = 3, 8, 128, 6200, [6100, 6200, 6001], 64
+    k, v = torch.randn(n, H, L, d, generator=gen, device=DEV), torch.randn(n, H, L, d, generator=gen, device=DEV)
+    idx = [torch.stack([torch.randperm(L, generator=gen, device=DEV)[:b].sort().values for _ in range(H)]).int() for b in budgets]
+    n_blocks = -(-sum(budgets) // br)
+    slots = torch.randperm(n_blocks * br, generator=gen, device=DEV)[:sum(budgets)].int()
+    cache, want = _pool(n_blocks, H, br, d, kind), _pool(n_blocks, H, br, d, kind)
+    laq.laq_cache_compact(cache, k, v, torch.cat([x.flatten() for x in idx]), budgets, slots)
+    first = 0
+    for i, b in enumerate(budgets):
+        rows = idx[i].long()[..., None].expand(-1, -1, d)
+        laq.laq_cache_append(want, *(x[i].gather(1, rows).transpose(0, 1) for x in (k, v)), slots[first:first + b])
+        first += b
+    torch.cuda.synchronize()
+    for x, y in zip(cache, want):
+        assert x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("kind,Hq,H,d,n,long,chunk,pad", [(BF16, 32, 8, 128, 20, 3000, 512, 0), (E4M3, 32, 8, 128, 9, 700, 300, 40), (BF16, 8, 2, 64, 70, 400, 1200, 7), (BF16, 32, 8, 128, 16, 900, 1, 240)])
+def test_chunks_beside_decoding_requests_and_padding(kind, Hq, H, d, n, long, chunk, pad):
+    laq = _laq()
+    print("case:", kind, Hq, H, d, n, long, chunk, pad, flush=True)
+    tokens = [1] * n
+    tokens[n // 2] = chunk
+    c = Case(BF16, kind, Hq, H, d, 64, [chunk + 100 if i == n // 2 else 1 + i * 389 % long for i in range(n)], tokens)
+    T = c.start[-1]
+    out, lse = torch.full((T + pad, Hq, d), 5.0, dtype=BF16, device=DEV), torch.full((T + pad, Hq), 5.0, device=DEV)
+    c.qd = torch.cat([c.qd, torch.full((pad, Hq, d), math.nan, dtype=BF16, device=DEV)])
+    assert laq.laq_cache_attention_workspace_bytes(c.cache, Hq, BF16, n, T + pad, max(c.rows)) == 0      # (the average number of tokens is that of chunks)
+    c.run(out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert (out[T:] == 5).all() and (lse[T:] == 5).all()
+    c.check(out[:T], lse[:T])
