@@ -8,8 +8,7 @@
 // Weights are rounded to bf16 for the product with V: results are 0.0023 of themselves away from exact ones, of which their own rounding is 0.0017.  In two parts it would be that alone,
 // but the products are what takes the time here: 4 x 512 tokens 227 -> 286 us, 8 bits 253 -> 297, a prompt of 4096 tokens 161 -> 204.
 //
-// 4 x 512 tokens x 32 heads over 2100 to 8704 rows 229 us, 814 TFLOP/s; a prompt of 4096 tokens 161 us, 855 TFLOP/s; 8 bits 249 us.  (In the other kernel, whose waves read their keys from the
-// caches for 64 score rows each, 470 and 580.)  Bound: the instructions beside the products (for 32 products of a stage and wave 190 vector instructions, 32 of them exponentials, 90
+// 4 x 512 tokens x 32 heads over 2100 to 8704 rows 229 us, 814 TFLOP/s; a prompt of 4096 tokens 161 us, 855 TFLOP/s; 8 bits 249 us.  Bound: the instructions beside the products (for 32 products of a stage and wave 190 vector instructions, 32 of them exponentials, 90
 // scalar ones and 56 of LDS; vector units and matrix cores are each busy 35 % of the time), with two waves a SIMD to fill each other's waits, and, in a call like the first, columns of the longest request that run on alone when those beside them have ended.
 // Sharing the keys out evenly as the other kernel does was slower: sums of 128 rows of every cut column go through memory, and tokens early in a prompt see few keys (331 and 365 us against 297 and 236 then).
 #include "laq_paged_columns.h"
@@ -364,14 +363,22 @@ int64_t columns_of(int G, int n, int64_t n_tokens) { return n_tokens * G / TILE 
 }  // namespace
 
 // With more score rows of a request than the other kernel's tile and enough columns to keep the device busy.  This kernel : the one that shares keys out, us, 32
-// heads on 8: 32 requests of 1000 to 2000 rows, 10 tokens 66 : 80 (d = 64 49 : 43, so there from 64 score rows on), 16 tokens 67 : 82, 32 tokens 87 : 139; 16 of 1000 to 4096, 64 tokens 126 : 210.  128 workgroups: four requests of 8192 rows, 128 tokens 235 : 317,
-// 16 of 2048, 20 tokens 64 : 80, but two of 8192, 256 tokens 234 : 167 and one of 16384, 512 tokens 456 : 310 (many tiles of a request read its keys from the caches
-// there); 64: eight of 4096, 32 tokens 122 : 93, one of 16384, 256 tokens 456 : 171.
+// heads on 8, requests of equal numbers of tokens, blocks of 64 rows.
+// bf16: 32 requests of 1000 to 2000 rows, 10 tokens 54 : 78, 16 tokens 56 : 85, 32 tokens 62 : 141; 16 of 1000 to 4096, 64 tokens 103 : 212.  128 workgroups: 16 of 2048 rows, 20 tokens
+// 54 : 81, four of 8192, 128 tokens 189 : 186, but two, 256 tokens 189 : 176 and one of 16384, 512 tokens 365 : 320 (many tiles of a request read its keys from the caches
+// there); 160: two of 8192 189 : 213, one of 16384 367 : 391.  d = 64: 128 workgroups, 16 of 2048, 9 tokens 35 : 33 (blocks of 16 rows 47 : 32), eight of 4096, 64 tokens 65 : 84, so from 64
+// score rows on (of calls of fewer with more workgroups some lose by it: 256, 9 tokens 30 : 38, 512 59 : 92).
+// 8 bits, which every wave of this one converts again: 128 workgroups, 16 of 2048, 9 tokens 59 : 33, eight of 4096, 33 tokens 124 : 71; 192: one of 16384 469 : 391, two of 8192 240 : 217,
+// four 240 : 238, eight of 4096 125 : 137; 224: one of 16384 469 : 452, two of 8192 240 : 256; 256: 238 : 283 and 16 of 2048 69 : 112.  d = 64: 192, two of 8192 142 : 111, eight of 4096
+// 76 : 73; 256, two 143 : 139, eight 76 : 89.
+// The host knows no lengths, so it is the average number of tokens that chooses, padding counted, and for all requests: where decoding requests come with a chunk, none of their
+// keys is shared out.  63 of 1000 to 8192 rows beside 512 tokens over 4096 247 us (in two calls 191 + 87), but with one of 131072 rows among them 2556 (264 + 87); 16 of 1000 to
+// 8192 rows in a batch padded to 256 tokens 165 (not padded 62).
 bool paged_prompt_call(const PagedView& c, int Hq, int dtype, int n, int64_t n_tokens) {
   if (dtype != LAQ_BF16 || c.d > 128) return false;
   const int G = Hq / c.Hkv;
   const int64_t rows = (n_tokens + n - 1) / n * G, tiles = (rows + TILE - 1) / TILE, columns = tiles * n * c.Hkv;
-  return rows >= (c.d <= 64 ? 64 : 33) && columns >= (tiles <= 4 ? 128 : 160) && columns_of(G, n, n_tokens) * c.Hkv < (1 << 24);
+  return rows >= (c.d <= 64 ? 64 : 33) && columns >= (c.type == LAQ_E4M3 ? 200 : tiles <= 4 ? 128 : 160) && columns_of(G, n, n_tokens) * c.Hkv < (1 << 24);
 }
 
 hipError_t launch_paged_prompt(const PagedView& c, const PagedAttention& a, hipStream_t st) {

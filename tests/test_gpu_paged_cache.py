@@ -895,7 +895,7 @@ ODD = [  # every pair of types, one and two tiles of score rows, each head size,
     (F32, F32, 8, 2, 128, 16, [300, 40], [1, 1]), (F32, F32, 8, 2, 64, 16, [300, 70], [30, 20]), (F32, E4M3, 8, 2, 128, 16, [300, 40], [1, 1]), (F32, E4M3, 8, 2, 64, 64, [300, 70], [30, 20]),
     (F32, E4M3, 6, 2, 256, 16, [90, 600], [20, 3]), (F32, BF16, 8, 2, 128, 16, [300, 40], [1, 1]), (F32, BF16, 8, 2, 64, 64, [300, 70], [30, 20]), (F32, BF16, 6, 2, 256, 16, [90, 600], [20, 3]),
     (F32, BF16, 28, 4, 96, 48, [700, 1], [8, 1]), (F32, BF16, 2, 2, 24, 16, [2100], [1]), (BF16, BF16, 32, 32, 128, 16, [300, 100, 70, 90], [40, 50, 60, 90]),
-    (BF16, E4M3, 32, 32, 64, 64, [150, 64, 70, 90], [64, 64, 70, 80]),
+    (BF16, E4M3, 64, 64, 64, 64, [150, 64, 70, 90], [64, 64, 70, 80]),
 ]
 
 
@@ -967,7 +967,7 @@ def test_queries_beyond_the_largest_number_of_bf16(kind, Hq, H, d, br, rows, tok
     c.check(*c.run(split=split, scale=scale), scale=scale)
 
 
-@pytest.mark.parametrize("dtype,kind,Hq,H,d,n,each", [(BF16, BF16, 8, 2, 64, 3, 3), (F32, E4M3, 8, 2, 128, 3, 9), (BF16, E4M3, 8, 1, 192, 80, 2), (BF16, BF16, 32, 32, 128, 4, 35), (BF16, E4M3, 32, 32, 64, 4, 64),
+@pytest.mark.parametrize("dtype,kind,Hq,H,d,n,each", [(BF16, BF16, 8, 2, 64, 3, 3), (F32, E4M3, 8, 2, 128, 3, 9), (BF16, E4M3, 8, 1, 192, 80, 2), (BF16, BF16, 32, 32, 128, 4, 35), (BF16, E4M3, 64, 64, 64, 4, 64),
                                                       (BF16, BF16, 4, 2, 72, 70, 18)])
 def test_starts_that_make_no_sense_leave_everything_around_the_output_alone(dtype, kind, Hq, H, d, n, each):
     print("case:", dtype, kind, Hq, H, d, n, each, flush=True)
@@ -987,8 +987,8 @@ def test_starts_that_make_no_sense_leave_everything_around_the_output_alone(dtyp
 
 CHUNKS = [  # more calls that the kernel of whole prompts takes, each token compared: (cache, Hq, H, d, block, lengths, tokens)
     # numbers of score rows of a group that are no power of two, more than four tiles of a request on average, head sizes that are rounded up
-    (BF16, 56, 8, 128, 256, [513], [513]), (E4M3, 112, 16, 128, 16, [430, 64], [150, 64]), (BF16, 112, 16, 80, 64, [300, 150], [150, 130]),
-    (E4M3, 32, 32, 80, 16, [200, 130, 50, 90], [130, 129, 60, 0]), (BF16, 32, 32, 80, 32, [200, 130, 50, 90], [130, 129, 50, 1]),
+    (BF16, 56, 8, 128, 256, [513], [513]), (E4M3, 140, 20, 128, 16, [430, 64], [150, 64]), (BF16, 112, 16, 80, 64, [300, 150], [150, 130]),
+    (E4M3, 64, 64, 80, 16, [200, 130, 50, 90], [130, 129, 60, 0]), (BF16, 32, 32, 80, 32, [200, 130, 50, 90], [130, 129, 50, 1]),
     # columns in the order of lengths: 256 / H of a KV head to a round, the second round backwards.  More than one round, more than two, none whole; no room for one
     (BF16, 64, 32, 64, 16, [700, 200, 90, 300], [300, 200, 90, 64]), (BF16, 64, 64, 32, 64, [900, 300, 500], [300, 129, 40]), (E4M3, 64, 64, 24, 16, [150, 300, 600, 600, 5], [140, 300, 520, 129, 5]),
     (BF16, 64, 64, 72, 16, [520, 150, 150, 600], [520, 150, 150, 129]), (BF16, 260, 260, 16, 16, [300, 41], [140, 40]), (E4M3, 128, 128, 72, 64, [131, 300, 70], [131, 257, 1]),
@@ -1085,7 +1085,7 @@ def test_many_compacted_rows_have_the_bits_of_appended_ones(kind):
         assert x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
-@pytest.mark.parametrize("kind,Hq,H,d,n,long,chunk,pad", [(BF16, 32, 8, 128, 20, 3000, 512, 0), (E4M3, 32, 8, 128, 9, 700, 300, 40), (BF16, 8, 2, 64, 70, 400, 1200, 7), (BF16, 32, 8, 128, 16, 900, 1, 240)])
+@pytest.mark.parametrize("kind,Hq,H,d,n,long,chunk,pad", [(BF16, 32, 8, 128, 20, 3000, 512, 0), (E4M3, 32, 8, 128, 26, 700, 300, 40), (BF16, 8, 2, 64, 70, 400, 1200, 7), (BF16, 32, 8, 128, 16, 900, 1, 240)])
 def test_chunks_beside_decoding_requests_and_padding(kind, Hq, H, d, n, long, chunk, pad):
     laq = _laq()
     print("case:", kind, Hq, H, d, n, long, chunk, pad, flush=True)
@@ -1100,3 +1100,43 @@ def test_chunks_beside_decoding_requests_and_padding(kind, Hq, H, d, n, long, ch
     torch.cuda.synchronize()
     assert (out[T:] == 5).all() and (lse[T:] == 5).all()
     c.check(out[:T], lse[:T])
+
+
+CHUNKS8 = [  # 8 bits in the kernel of whole prompts: (Hq, H, d, block, lengths, tokens)
+    (64, 64, 128, 64, [300, 200, 40, 129, 37], [40, 64, 40, 65, 1]), (64, 64, 128, 16, [300, 64, 40, 41], [40, 33, 40, 35]), (64, 64, 96, 48, [300, 140, 50, 0], [129, 128, 50, 3]),
+    (64, 64, 24, 16, [150, 64, 70, 90], [64, 64, 70, 80]), (64, 64, 64, 32, [500, 300, 70, 90], [64, 64, 70, 80]), (64, 16, 128, 256, [700, 300, 129, 600], [130, 120, 110, 100]),
+    (56, 8, 72, 80, [520], [520]), (6, 3, 72, 16, [40 + i for i in range(70)], [17 + i % 5 for i in range(70)]), (80, 2, 128, 128, [30 + 2 * i for i in range(130)], [1] * 130),
+]
+
+
+@pytest.mark.parametrize("Hq,H,d,br,rows,tokens", CHUNKS8)
+def test_chunks_over_8_bits(Hq, H, d, br, rows, tokens):
+    print("case:", Hq, H, d, br, rows, tokens, flush=True)
+    c = Case(BF16, E4M3, Hq, H, d, br, rows, tokens, token_major=br == 64, fused=br == 48)
+    assert _laq().laq_cache_attention_workspace_bytes(c.cache, Hq, BF16, len(rows), sum(tokens), max(rows)) == 0
+    c.check(*c.run())
+    # blocks that are not there
+    for i, page, bad in ((0, 0, -1), (len(rows) - 1, 0, c.n_blocks), (0, 1, 2 ** 31 - 1)):
+        if page < c.width - 1:
+            c.table[i, page] = bad
+            c.hidden[i] |= set(range(br * page, br * page + br))
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("d,br", [(128, 16), (128, 64), (40, 32)])
+@pytest.mark.parametrize("at", [299, 260, 270, 100, 290])
+def test_odd_rows_of_chunks_over_8_bits_reach_those_that_see_them_alone(at, d, br, what):
+    def put(k, v):
+        v[at, 3, d // 2] = what
+        k[300 + 60, 5, 7] = what
+    c = Case(BF16, E4M3, 64, 64, d, br, [300, 100, 70, 90], [40, 64, 65, 90], special=put)
+    assert _laq().laq_cache_attention_workspace_bytes(c.cache, 64, BF16, 4, 259, 300) == 0
+    out, lse = c.run()
+    torch.cuda.synchronize()
+    want = torch.zeros(out.shape[:2], dtype=torch.bool)
+    want[max(0, at - 260):40, 3] = True                # a row of 8 bits with an infinity or a NaN stands for NaN
+    want[40 + 24:40 + 64, 5] = True                    # (key 60 of the second request, whose 64 tokens are its rows 36 to 99)
+    assert torch.equal(out.isnan().all(-1).cpu(), want) and torch.equal((~torch.isfinite(out)).any(-1).cpu(), want)
+    want[:, 3] = False
+    assert torch.equal(~torch.isfinite(lse).cpu(), want)
