@@ -126,13 +126,14 @@ int laq_cache_compact(const laq_shape *shape, const void *k, const void *v, cons
 int laq_cache_load(const laq_cache *cache, int32_t dtype, int64_t n_tokens, const int32_t *slots, void *k, void *v, void *stream);
 
 /*
- * Attention over the cache: tokens of n requests attend to the rows that their request holds, the tokens' own rows (the last ones) among
+ * Attention over the cache: tokens of n requests (1 at least) attend to the rows that their request holds, the tokens' own rows (the last ones) among
  * them, each to those up to its own.
  *   Hq, dtype, scale  query heads (a multiple of the cache's Hkv, <= 65535), laq_dtype of q and out, logit scale (<= 0: 1/sqrt(d)).  LAQ_BF16 goes with
  *                 caches of LAQ_BF16 and LAQ_E4M3 (LAQ_ERR_UNSUPPORTED with LAQ_F32), LAQ_F32 with all
  *   n_tokens      tokens of the batch; n_tokens * Hq < 2^31
  *   start         int32 [n + 1]: tokens start[i] .. start[i+1]-1 are those of request i, in order; ascending, start[0] = 0.
- *                 Tokens from start[n] on (padding) are left alone.  NULL: one token per request (n_tokens = n)
+ *                 Tokens from start[n] on (padding) are left alone.  NULL: one token per request (n_tokens = n).  Of numbers in another order
+ *                 nothing is touched but out, lse and ws, and what they hold afterwards is not defined
  *   q             [n_tokens, Hq, d]: q->heads = Hq
  *   block_table   int32 [n, blocks_per_inst]; rows of blocks whose number is not one of the pool are not there for anybody
  *   rows          int32 [n]: rows that request i holds; at most blocks_per_inst * block_rows count
@@ -142,17 +143,22 @@ int laq_cache_load(const laq_cache *cache, int32_t dtype, int64_t n_tokens, cons
  *                 out = sum_j softmax_j(scale * <q, K_j>) V_j over these.  0 where there are none
  *   lse           fp32 [n_tokens, Hq], may be NULL: log sum_j exp(scale * <q, K_j>) (-infinity where there are none): with it two
  *                 attentions over different rows can be joined
- *   ws / ws_bytes optional device scratch.  With at least laq_cache_attention_workspace_bytes() bytes (same arguments; 0 for chunks of a
- *                 prompt; it does not grow with max_rows) the keys of all requests are shared out evenly among as many workgroups as the
- *                 device holds; without it a KV head's keys are read by one workgroup for every 16 or 32 score rows.  LAQ_ERR_WORKSPACE if given but smaller or not
- *                 16-byte aligned.  With and without it the last bits of `out` may differ
+ *   ws / ws_bytes optional device scratch, as it comes.  With at least laq_cache_attention_workspace_bytes() bytes (same arguments; it does not grow with
+ *                 max_rows) the keys of all requests are shared out evenly among as many workgroups as the device holds; without it a KV head's
+ *                 keys are read by one workgroup for every 16 or 32 score rows.  0 bytes: the batch is taken for chunks of a prompt (bf16, d <= 128,
+ *                 more than 32 score rows per request on average, padding counted, and enough workgroups), where a workgroup reads a KV head's keys
+ *                 for 128 score rows.  That is so for every request of the batch: decoding requests of long caches beside a chunk, and decoding
+ *                 batches with much padding, take less time in calls of their own and without it.  LAQ_ERR_WORKSPACE if given but
+ *                 smaller or not 16-byte aligned.  With and without it the last bits of `out` may differ
  * A call that needs more than 2^24 workgroups is LAQ_ERR_UNSUPPORTED.  What the rows behind r, other blocks of the pool and rows that a token does
  * not see hold (infinities and NaN too) does not reach out or lse.
- * bf16: the products of q and K are exact, sums, maxima and weights are fp32; for the product with V a weight is the sum of two bf16 (2^-16), in chunks of a prompt, and over
- * 8 bits where requests have more than 16 score rows on average, one (2^-8); out is rounded once.  fp32: products and sums in fp32; over caches of bf16 and 8 bits, which are exact in bf16, as bf16 products of queries and weights that are
- * the sums of three bf16 (2^-24; parts below 2^-126 count as 0).  Weights are up to 2^8 before they are divided by their sum: sums over
- * numbers of V beyond 2^88 may overflow.  Visible scores that are all -infinity give 0 and an lse of -infinity.  An infinity in V that is seen with a weight so small that fp32
- * has 0 for it may give a NaN.
+ * bf16: the products of q and K are exact, sums, maxima and weights are fp32; for the product with V a weight is the sum of two bf16 (2^-16), in
+ * chunks of a prompt, and over 8 bits where requests have more than 16 score rows on average, one (2^-8); out is rounded once.
+ * fp32: products and sums in fp32; over caches of bf16 and 8 bits, which are exact in bf16, as bf16 products of queries and weights that are the sums of
+ * three bf16 (2^-24; parts below 2^-126 count as 0).
+ * Weights are up to 2^8 before they are divided by their sum: sums over numbers of V beyond 2^88 may overflow.  A score of -infinity, from an infinity in q
+ * or in K, has the weight 0, and visible scores that are all -infinity give 0 and an lse of -infinity; one of +infinity or NaN makes NaN of its token.  An infinity
+ * in V that is seen with a weight so small that fp32 has 0 for it may give a NaN.
  */
 size_t laq_cache_attention_workspace_bytes(const laq_cache *cache, int32_t Hq, int32_t dtype, int32_t n, int64_t n_tokens, int32_t max_rows);
 int laq_cache_attention(const laq_cache *cache, int32_t dtype, float scale, int32_t n, int64_t n_tokens, const int32_t *start, const laq_heads *q,

@@ -8,9 +8,9 @@
 // m moves only when a score is more than 8 above it, so that the usual step has no maximum over lanes).  The waves are folded at the end through LDS, the
 // ranges of a column by the workgroup that finds all of them finished, in a fixed order.
 //
-// Bound: memory.  128 requests x 8 heads x 1000 to 8192 rows of d = 128: bf16 2.43 GB in 369 us, 6.6 TB/s; 8 bits 1.22 GB in 208 us, 5.9 TB/s; 96 x 6144 rows of bf16 6.7 TB/s; the
-// vector units are busy 10 % of the time, the matrix cores 4 % (four requests of 32768 to 131071 rows in 8 bits: 28 and 7 %).  Small calls: dependent trips to memory, about 11 us for 520 rows: lengths (2), table (2), keys (1.5), fold (1),
-// sums and marks of the ranges (3).  fp32 caches with more than 16 score rows: the matrix cores' fp32 rate, an eighth of bf16's for these products.
+// Bound: memory.  128 requests x 8 heads x 1000 to 8192 rows of d = 128: bf16 2.43 GB in 371 us, 6.6 TB/s; 8 bits 1.22 GB in 208 us, 5.9 TB/s; 96 x 6144 rows of bf16 6.7 TB/s; the
+// vector units are busy 16 % of the time, the matrix cores 6 % (four requests of 32768 to 131071 rows in 8 bits: 32 and 11 %).  Small calls: dependent trips to memory, about 11 us for 520 rows: lengths (2.4), table and asking for keys (2.6),
+// keys and products (1.9), fold (0.9), sums, marks and join (3).  fp32 caches with more than 16 score rows: the matrix cores' fp32 rate, an eighth of bf16's for these products.
 //
 // No LDS on the way of K and V, and registers for one step: K's are read again as soon as the scores are made, V's as soon as the sums are, so that about a step of a
 // wave is on its way at any time and its code is there once (two steps in turn, twice the registers and the code: four long requests in 8 bits 191 us, so 172).  Products have the keys as the first operand's rows, so that a lane has four keys of one score row (column n =
