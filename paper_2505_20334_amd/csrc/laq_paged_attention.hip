@@ -82,7 +82,7 @@ struct Kinds {
   // (one part: 0.0018 to 0.0023).  Memory's time hides the second products: 128 requests 371 us, in 8 bits 207, 520 rows 12, 32 x 8 tokens 61, each +-1 % (two of 8192 rows, 256
   // tokens 166 -> 173); but not where 8 bits are converted for two tiles of score rows (32 x 8 tokens 50 -> 53): one there
   static constexpr int WEIGHTS = FLOATS ? 1 : F32 ? 3 : SCALED && NT == 2 ? 1 : 2;
-  // the cache has infinities, which the later parts would make NaN of: those of V are added at the end wherever they are, those of K meet the first part alone
+  // the cache has infinities, which the later parts would make NaN of: they meet the first part alone
   static constexpr bool LATER_K = PARTS > 1 && !SCALED, LATER_V = WEIGHTS > 1 && !SCALED;
   static constexpr int KT = FLOATS ? 1 : SCALED ? 4 : 2;        // tiles of 16 keys a step
   static constexpr int KN = FLOATS ? 4 : 8, KP = D / (4 * KN);  // numbers of a piece of K; pieces of a lane's key row
@@ -397,8 +397,8 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
           }
         }
     }
+    bool odd_v = false;                                              // an infinity or a NaN in V of the step
     if constexpr (K::LATER_V) {
-      // (the later parts of a weight are 0 or negative, and make a NaN of an infinity)
       u16x2 most{};
 #pragma unroll
       for (int kt = 0; kt < K::KT; ++kt)
@@ -408,16 +408,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
           for (int i = 0; i < K::VP; ++i)
 #pragma unroll
             for (int w = 0; w < K::VN / 2; ++w) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, s.v[kt][j][i].x[w] & 0x7fff7fffu));
-      const bool bad = most[0] >= 0x7f80 || most[1] >= 0x7f80;
-      if (__any(bad)) {
-        odd |= bad;
-#pragma unroll
-        for (int kt = 0; kt < K::KT; ++kt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < K::VP; ++i) drop_odd(s.v[kt][j][i]);
-      }
+      odd_v = __any(most[0] >= 0x7f80 || most[1] >= 0x7f80);
     }
     if constexpr (K::FLOATS) {
 #pragma unroll
@@ -437,24 +428,38 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
 #pragma unroll
         for (int t = 0; t < NT; ++t)
           split<K::WEIGHTS, false>(x[t][h], x[t][h + 1], w[t]);
-#pragma unroll
-        for (int i = 0; i < K::VP; ++i) {
-          // [key][channel pair] to [channel][key pair]
+        // [key][channel pair] to [channel][key pair], and the weights times them.  ODD: V's infinities and NaN alone, the weights' first part
+        const auto products = [&](int i, auto odd_only) {
+          constexpr bool ODD = decltype(odd_only)::value;
           using P = decltype(pairs(s.v[0][0][0], 1.f));
           P v[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = pairs(s.v[h + j / 4][j % 4][i], K::SCALED ? scale_of_v(s, h + j / 4, j % 4) : 1.f);
 #pragma unroll
           for (int e = 0; e < K::VN; ++e) {
+            const auto word = [&](int j) { return ODD ? v[j][e / 2] ^ without_odd(v[j][e / 2], E{}) : v[j][e / 2]; };
             u32x4 f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(v[2 * j + 1][e / 2], v[2 * j][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+            for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(word(2 * j + 1), word(2 * j), e & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int part = K::WEIGHTS - 1; part >= 0; --part) o[t][i * K::VN + e] = mfma(f, w[t][part], o[t][i * K::VN + e]);
+              for (int part = ODD ? 0 : K::WEIGHTS - 1; part >= 0; --part) o[t][i * K::VN + e] = mfma(f, w[t][part], o[t][i * K::VN + e]);
+          }
+        };
+        if constexpr (K::LATER_V) {
+          // (the later parts of a weight are 0 or negative, and make a NaN of an infinity: V's odd numbers are multiplied with the first part alone, then V without them)
+          if (odd_v) {
+#pragma unroll
+            for (int i = 0; i < K::VP; ++i) {
+              products(i, std::true_type{});
+#pragma unroll
+              for (int j = 0; j < 8; ++j) drop_odd(s.v[h + j / 4][j % 4][i]);
+            }
           }
         }
+#pragma unroll
+        for (int i = 0; i < K::VP; ++i) products(i, std::false_type{});
       }
     }
     load_v(s);
@@ -507,7 +512,7 @@ __global__ __launch_bounds__(ATT_THREADS, (Kinds<Q, E, D, NT, WIDE>::RESIDENT)) 
       }
       if (any_odd) {
         const int upto = min(to - 1, col.last(r, G));
-        for (int key = K::LATER_V ? from : max(from, first_last + 1); key <= upto; ++key) {
+        for (int key = max(from, first_last + 1); key <= upto; ++key) {
           const int page = (int)((uint32_t)key / (uint32_t)c.block_rows), off = key - page * c.block_rows, block = table[page];
           if (block < 0 || block >= c.n_blocks) continue;
           const E* v = vx + block * c.block + (int64_t)off * c.row;

@@ -1140,3 +1140,28 @@ def test_odd_rows_of_chunks_over_8_bits_reach_those_that_see_them_alone(at, d, b
     assert torch.equal(out.isnan().all(-1).cpu(), want) and torch.equal((~torch.isfinite(out)).any(-1).cpu(), want)
     want[:, 3] = False
     assert torch.equal(~torch.isfinite(lse).cpu(), want)
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("dtype,kind,Hq,H,d,br,rows,tokens", [x for x in ODD if x[1] != E4M3 and x[4] > 24])
+def test_infinities_in_v_that_all_see(dtype, kind, Hq, H, d, br, rows, tokens, split):
+    print("case:", dtype, kind, Hq, H, d, br, rows, tokens, split, flush=True)
+
+    def put(k, v):
+        first = rows[0] - tokens[0]                    # (keys up to here are seen by every token of request 0)
+        for j, e, what in ((0, 3, math.inf), (first, 4, -math.inf), (first // 2, 5, math.nan), (1, 6, math.inf), (first // 3, 6, -math.inf), (first // 4, d - 1, math.inf), (2, d - 1, math.inf)):
+            v[j, 0, e] = what
+    c = Case(dtype, kind, Hq, H, d, br, rows, tokens, special=put)
+    out, lse = c.run(split=split)
+    torch.cuda.synchronize()
+    got, G = out.cpu()[:tokens[0], :Hq // H], Hq // H
+    assert (got[..., 3] == math.inf).all() and (got[..., 4] == -math.inf).all() and got[..., 5].isnan().all() and got[..., 6].isnan().all() and (got[..., d - 1] == math.inf).all()
+    odd = torch.zeros(out.shape, dtype=torch.bool)
+    odd[:tokens[0], :G, [3, 4, 5, 6, d - 1]] = True
+    assert torch.equal(~torch.isfinite(out.cpu()), odd)
+    c.v = c.v.nan_to_num(0, 0, 0)                      # and the others have their values
+    for tok in range(tokens[0]):
+        k, v = (x[:rows[0]].transpose(0, 1).contiguous() for x in (c.k, c.v))
+        o, _, _, _ = fp4_plain.attention(c.q[tok], k, v, rows[0] - tokens[0] + tok + 1, 1.0 / math.sqrt(d))
+        out[tok] = torch.where(odd[tok], o.to(dtype), out[tok].cpu()).to(DEV)
+    c.check(out, lse)
